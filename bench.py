@@ -86,7 +86,7 @@ def parse():
 
 
 CSRC = os.path.join(ROOT, "paper_2609_23536_amd", "csrc")
-GEMM_SOURCES = ("gemm_fp8.hip", "gemm_ring.hip", "gemm_dispatch.hip", "gemm_util.h")
+GEMM_SOURCES = ("gemm_fp8.hip", "gemm_ring.hip", "gemm_loops.h", "gemm_dispatch.hip", "gemm_util.h")
 
 
 def gemm_source_sha256(csrc=CSRC):

@@ -53,7 +53,7 @@
 //
 // Determinism: no atomics and no split reduction; the same inputs produce the
 // same bits, which the split-vs-full-backward check relies on.
-#include "gemm_util.h"
+#include "gemm_loops.h"
 #include "scale_update.h"
 
 namespace qe {
@@ -89,14 +89,10 @@ __global__ __launch_bounds__(256) void gemm_tn_w4_kernel(GemmParams g, int tiles
   static_assert((BM == 256 || BM == 192) && (BN == 256 || BN == 224 || BN == 192), "tile sizes");
   constexpr int NW = 4, TM = BM / 2, TN = BN / 2;
   constexpr int I = TM / 16, J = TN / 16;    // 16 x 16 MFMA blocks per wave sub-tile
-  constexpr int IA = I / 2, IB = I - IA;     // block rows of phase A and phase B
-  constexpr int QA = IA * J, QB = IB * J;    // MFMAs per phase
   constexpr int CHA = BM / 32, CHB = BN / 32;  // 16-byte LDS-bound loads per lane per K tile
-  constexpr int ND = CHA + CHB;              // LDS-bound loads per K tile
   constexpr int STAGE = (BM + BN) * BK;
   constexpr int EP = TN + 4;                 // epilogue staging row, in floats (padded)
   static_assert(NW * 32 * EP * 4 <= 2 * STAGE, "epilogue staging fits in the stages");
-  static_assert(CHA * NW * 1024 == BM * BK, "LDS-bound load d of a tile lands at stage + 4096 d");
   // two K stages, then one 1 KB block per wave that absorbs the loads issued
   // past the last full K tile (so the loop issues them unconditionally)
   __shared__ __attribute__((aligned(16))) uint8_t smem[2 * STAGE + NW * 1024];
@@ -127,10 +123,6 @@ __global__ __launch_bounds__(256) void gemm_tn_w4_kernel(GemmParams g, int tiles
   const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
 
   const int64_t M = g.m, N = g.n, K = g.k;
-  const int KT = int(K / BK);
-  const int64_t ktail = K - int64_t(KT) * BK;
-  const int T = KT + (ktail > 0 ? 1 : 0);
-
   const int lrow = lane >> 3;
   uint32_t oa[CHA], ob[CHB];
 #pragma unroll
@@ -145,200 +137,8 @@ __global__ __launch_bounds__(256) void gemm_tn_w4_kernel(GemmParams g, int tiles
     const int lch = (lane & 7) ^ row_swizzle(row);
     ob[c] = chunk_offset(min(n0 + row, N - 1), g.ldb, lch, K);
   }
-  const uint32_t lds_base = uint32_t(reinterpret_cast<uintptr_t>(smem));
-  const uint32_t wblk = __builtin_amdgcn_readfirstlane(lds_base + uint32_t(wave) * 1024u);
-  const uint32_t wdummy = __builtin_amdgcn_readfirstlane(lds_base + uint32_t(2 * STAGE) + uint32_t(wave) * 1024u);
-
-  auto issue = [&](int kt, int buf) {
-    if (kt < KT) {
-      const uint8_t *ga = g.a + int64_t(kt) * BK;
-      const uint8_t *gb = g.b + int64_t(kt) * BK;
-      const uint32_t sa = wblk + uint32_t(buf * STAGE);
-      const uint32_t sb = sa + uint32_t(BM * BK);
-#pragma unroll
-      for (int c = 0; c < CHA; ++c)
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(oa[c]), "s"(ga),
-                     "s"(sa + uint32_t(c * NW * 1024)) : "memory", "m0");
-#pragma unroll
-      for (int c = 0; c < CHB; ++c)
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(ob[c]), "s"(gb),
-                     "s"(sb + uint32_t(c * NW * 1024)) : "memory", "m0");
-    } else {  // the last, partial K tile, through registers: bytes at or past K are zero
-      uint8_t *dA = smem + buf * STAGE;
-      uint8_t *dB = dA + BM * BK;
-      const uint32_t k0 = uint32_t(KT) * BK;
-#pragma unroll
-      for (int c = 0; c < CHA; ++c) {
-        const int row = 8 * (wave + NW * c) + lrow;
-        const int64_t gk = int64_t(k0) + ((lane & 7) ^ row_swizzle(row)) * 16;
-        const uint4 va = gk < K ? mask_tail(*reinterpret_cast<const uint4 *>(g.a + (oa[c] + k0)), K - gk) : make_uint4(0u, 0u, 0u, 0u);
-        *reinterpret_cast<uint4 *>(dA + (wave + NW * c) * 1024 + lane * 16) = va;
-      }
-#pragma unroll
-      for (int c = 0; c < CHB; ++c) {
-        const int row = 8 * (wave + NW * c) + lrow;
-        const int64_t gk = int64_t(k0) + ((lane & 7) ^ row_swizzle(row)) * 16;
-        const uint4 vb = gk < K ? mask_tail(*reinterpret_cast<const uint4 *>(g.b + (ob[c] + k0)), K - gk) : make_uint4(0u, 0u, 0u, 0u);
-        *reinterpret_cast<uint4 *>(dB + (wave + NW * c) * 1024 + lane * 16) = vb;
-      }
-    }
-  };
-
-  // 16-row fragments: lane l reads row (l & 15), the 32 bytes 32 (l >> 4) .. +31
-  // of the K tile, i.e. logical chunks 2 (l >> 4) and the next.  The swizzle
-  // term depends on (l & 15) only, so every fragment is base + constant.
-  const int fr = lane & 15, fq = lane >> 4;
-  const uint32_t f_lo = uint32_t(fr) * BK + uint32_t((2 * fq) ^ row_swizzle(fr)) * 16;
-  const uint32_t f_hi = uint32_t(fr) * BK + uint32_t((2 * fq + 1) ^ row_swizzle(fr)) * 16;
-  auto frag = [&](const uint8_t *base) -> v8i {
-    const uint4 lo = *reinterpret_cast<const uint4 *>(base + f_lo);
-    const uint4 hi = *reinterpret_cast<const uint4 *>(base + f_hi);
-    return v8i{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
-  };
-  auto read_a = [&](int buf, int i, v8i (&fa)[I]) { fa[i] = frag(smem + buf * STAGE + (wm * TM + i * 16) * BK); };
-  auto read_b = [&](int buf, int j, v8i (&fb)[J]) {
-    fb[j] = frag(smem + buf * STAGE + (BM + wn * TN + j * 16) * BK);
-  };
-
   v4f acc[I][J];
-#pragma unroll
-  for (int i = 0; i < I; ++i)
-#pragma unroll
-    for (int j = 0; j < J; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-
-  auto mfma = [&](int i, int j, const v8i (&fa)[I], const v8i (&fb)[J]) {
-    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i], acc[i][j], FB, FA, 0, 0, 0, 0);
-  };
-  // LDS-bound loads inside the K loop, two instructions each: load d of a K
-  // tile lands at stage + 4096 d, so M0 steps by a uniform stride, and the
-  // step is issued before an MFMA and the load after it (the MFMA is the wait
-  // state M0 needs).  Past the last full K tile the loads still run, from
-  // tile 0 into the wave's dummy block with stride 0: no branch per load (and
-  // no byte past a row of less than 128, see chunk_offset).
-  auto dma_m0 = [&](int d, uint32_t base, uint32_t stride) {
-    if (d == 0)
-      asm volatile("s_mov_b32 m0, %0" ::"s"(base) : "m0");
-    else
-      asm volatile("s_add_u32 m0, m0, %0" ::"s"(stride) : "m0", "scc");
-  };
-  auto dma_load = [&](int d, const uint8_t *ga, const uint8_t *gb) {
-    if (d < CHA)
-      asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(oa[d]), "s"(ga) : "memory");
-    else
-      asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(ob[d - CHA]), "s"(gb) : "memory");
-  };
-
-  // Phase A of a tile from stage `buf`: column-major MFMAs over block rows
-  // 0 .. IA-1 (B fragment j is first needed at MFMA j * IA, so the fragments
-  // read last in the previous phase B are needed last); A fragments IA .. I-1
-  // of the same tile are read after the first MFMAs (one per even slot), long
-  // before phase B needs them.  The tile's B fragments are all in registers
-  // by now, so the same stage's B half already takes the B part of the tile
-  // two K tiles ahead (`kt3`), spread over the phase: a K step and a half
-  // before it is read.
-  auto b_slot = [](int q, int k) { return (k * QA) / CHB + 1 == q; };
-  auto phase_a = [&](int buf, bool dmab, int kt3, v8i (&fa)[I], v8i (&fb)[J]) {
-    const uint8_t *gb = dmab ? g.b + int64_t(kt3) * BK : g.b;
-    const uint32_t base = dmab ? wblk + uint32_t(buf * STAGE + BM * BK) : wdummy;
-    const uint32_t stride = dmab ? uint32_t(NW * 1024) : 0u;
-#pragma unroll
-    for (int q = 0; q < QA; ++q) {
-      int d = -1;  // the B-part load of this slot (folds to a constant once unrolled)
-#pragma unroll
-      for (int k = 0; k < CHB; ++k) d = b_slot(q, k) ? k : d;
-      __builtin_amdgcn_sched_barrier(0);
-      if (d >= 0) dma_m0(d, base, stride);
-      __builtin_amdgcn_sched_barrier(0);
-      mfma(q % IA, q / IA, fa, fb);
-      __builtin_amdgcn_sched_barrier(0);
-      if (d >= 0) dma_load(CHA + d, g.a, gb);
-      if (q % 2 == 0 && q / 2 < IB) read_a(buf, IA + q / 2, fa);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  // Phase B of a tile: column-major MFMAs over block rows IA .. I-1.  After
-  // the last use of B fragment j, the next tile's B fragment j is read from
-  // stage `nbuf` into the same registers; the next tile's A fragments
-  // 0 .. IA-1 are read in the first slots (their registers are free since
-  // phase A).  `dma` issues the A part of tile `kt2` into stage `buf`.
-  // Slots of phase B, one kind of memory instruction each where possible: the
-  // next tile's A fragments after MFMAs 0, 4, 8, ..; LDS-bound loads after
-  // MFMAs q = 1, 2 (mod 4), so the A part is issued in the first half of the
-  // phase; B fragments after the last use of each (q = 3 (mod 4) when IB =
-  // 4).  Loads that do not fit go to the latest q = 0 (mod 4) slots past the A
-  // reads.  (Measured: the A part spread over all of phase B instead, equal;
-  // the B part packed into the first half of phase A, 0.5% slower.)
-  auto load_slot = [](int q) -> bool {
-    constexpr int n12 = (QB / 4) * 2;
-    if (q % 4 == 1 || q % 4 == 2) return (q / 4) * 2 + (q % 4 - 1) < CHA;
-    if (q % 4 == 0 && CHA > n12) return q / 4 >= IA && QB / 4 - 1 - q / 4 < CHA - n12;
-    return false;
-  };
-  auto phase_b = [&](int nbuf, bool dma, int kt2, int buf, v8i (&fa)[I], v8i (&fb)[J]) {
-    static_assert(QB % 4 == 0, "phase B slots come in fours");
-    const uint8_t *ga = dma ? g.a + int64_t(kt2) * BK : g.a;
-    const uint8_t *gb = dma ? g.b + int64_t(kt2) * BK : g.b;
-    const uint32_t base = dma ? wblk + uint32_t(buf * STAGE) : wdummy;
-    const uint32_t stride = dma ? uint32_t(NW * 1024) : 0u;
-#pragma unroll
-    for (int q = 0; q < QB; ++q) {
-      const int j = q / IB, i = IA + q % IB;
-      const bool ld = load_slot(q);
-      int d = 0;  // loads in earlier slots (folds to a constant once unrolled)
-#pragma unroll
-      for (int r = 0; r < q; ++r) d += load_slot(r) ? 1 : 0;
-      __builtin_amdgcn_sched_barrier(0);
-      if (ld) dma_m0(d, base, stride);
-      __builtin_amdgcn_sched_barrier(0);  // M0 is written before the MFMA, never next to the load
-      mfma(i, j, fa, fb);
-      __builtin_amdgcn_sched_barrier(0);
-      if (ld) dma_load(d, ga, gb);
-      if (q % 4 == 0 && q / 4 < IA) read_a(nbuf, q / 4, fa);
-      if (q % IB == IB - 1) read_b(nbuf, j, fb);  // last use of B fragment j was this MFMA
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  };
-
-  if (T > 0) {
-    v8i fa[I], fb[J];
-    issue(0, 0);
-    if (KT > 1) {
-      // both first K tiles are full: tile 1's LDS-bound loads stay in flight
-      // while the wave waits for its tile-0 loads (the ND most recent ones
-      // are tile 1's; the counter completes in order)
-      issue(1, 1);
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND) : "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < J; ++j) read_b(0, j, fb);
-#pragma unroll
-    for (int i = 0; i < IA; ++i) read_a(0, i, fa);
-    if (T > 1 && KT <= 1) issue(1, 1);  // tile 1 is the partial tail: through registers
-    __syncthreads();                       // every wave holds tile 0's B fragments: stage 0's B half is free
-    phase_a(0, 2 < KT, 2, fa, fb);         // and takes tile 2's B part
-    // tile 1 complete; the CHB most recent loads (tile 2's B part) may still
-    // be in flight: the counter completes in order
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
-    __syncthreads();                       // tile 1 published; tile 0 fully read
-    for (int t = 0; t < T; ++t) {
-      const int buf = t & 1;
-      const bool dma = t + 2 < KT;
-      if (t + 2 < T && !dma) issue(t + 2, buf);
-      // phase B of tile t, with tile t+2's A part; reads of tile t+1 (in the
-      // last iteration they read a stale stage that is never used: always in
-      // bounds, and branch-free here)
-      phase_b(buf ^ 1, dma, t + 2, buf, fa, fb);
-      if (t + 1 < T) {
-        __syncthreads();                   // tile t+1's B fragments read by every wave
-        phase_a(buf ^ 1, t + 3 < KT, t + 3, fa, fb);  // with tile t+3's B part
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
-        __syncthreads();                   // tile t+2 published; tile t+1 fully read
-      }
-    }
-  }
+  large_k_loop<FA, FB, BM, BN>(g.a, g.b, oa, ob, K, smem, acc);
 
   // Epilogue through LDS: the MFMA layout gives each lane one row and a column
   // quad per 16 x 16 block, so store instructions would touch 16 rows x 64 B.

@@ -23,22 +23,11 @@
 // vector-aligned went one element per lane before; MI355X, us: 4100 x 4100 x
 // 1040 into rows of 4103, BF16 46 -> 34, FP32 46 -> 39, accumulated 60 -> 49;
 // 8191 x 8191 x 2049 FP32 219 -> 181, accumulated 254 -> 216.)
-#include "gemm_util.h"
+#include "gemm_loops.h"
 #include "scale_update.h"
 
 namespace qe {
 namespace {
-
-// Bytes [0, valid) of a 32-byte fragment kept, the rest zeroed.
-__device__ __forceinline__ v8i mask_frag(v8i f, int valid) {
-#pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const int nb = valid - 4 * q;
-    const int k = nb <= 0 ? 0 : (nb >= 4 ? 4 : nb);
-    f[q] &= int(uint32_t((uint64_t(1) << (8 * k)) - 1u));
-  }
-  return f;
-}
 
 // Two workgroups per compute unit where the LDS holds two.  Their 256 registers
 // per lane then suffice without a spill, the 128 x 128 tile with 224, as long as
@@ -52,13 +41,10 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void gemm_
   constexpr int NW = 4, TM = BM / 2, TN = BN / 2;
   constexpr int I = TM / 16, J = TN / 16;
   constexpr int CHA = BM / 32, CHB = BN / 32;  // LDS-bound loads per lane per K tile
-  constexpr int L = CHA + CHB;
-  constexpr int Q = I * J;                     // MFMAs per wave and K tile
   constexpr int STAGE = (BM + BN) * BK;
   constexpr int ER = 64;                       // output rows staged at a time
   constexpr int EP = BN + 4;                   // staging row, in floats (padded)
   static_assert(ER * EP * 4 <= S * STAGE, "epilogue staging fits in the stages");
-  static_assert((S - 1) * L < 64, "the load counter holds 63");
   __shared__ __attribute__((aligned(16))) uint8_t smem[S * STAGE];
   static_assert(sizeof(smem) >= (kMaxHistory + kUpdateThreads / 64) * 4, "history staging fits in the stages");
 
@@ -86,10 +72,6 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void gemm_
   const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
 
   const int64_t M = g.m, N = g.n;
-  const int K = int(g.k);
-  const int ktail = K % BK;
-  const int T = K / BK + (ktail > 0 ? 1 : 0);
-
   // Load c of a wave fills 8 rows x 128 bytes; lane l fetches the chunk that
   // the swizzle puts at row 8 b + l / 8, physical chunk l % 8.
   const int lrow = lane >> 3;
@@ -104,169 +86,9 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void gemm_
     const int row = 8 * (wave + NW * c) + lrow;
     ob[c] = uint32_t(min(n0 + row, N - 1) * g.ldb) + ((lane & 7) ^ row_swizzle(row)) * 16;
   }
-  const uint32_t lds_base = uint32_t(reinterpret_cast<uintptr_t>(smem));
-  const uint32_t wblk = __builtin_amdgcn_readfirstlane(lds_base + uint32_t(wave) * 1024u);
-
-  auto load16 = [](uint32_t off, const uint8_t *base, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds)
-                 : "memory", "m0");
-  };
-  auto issue = [&](int t, uint32_t stage) {
-    const uint8_t *ga = g.a + int64_t(t) * BK;
-    const uint8_t *gb = g.b + int64_t(t) * BK;
-    const uint32_t sa = wblk + stage, sb = sa + uint32_t(BM * BK);
-    if (ktail == 0 || t + 1 < T) {
-#pragma unroll
-      for (int c = 0; c < CHA; ++c) load16(oa[c], ga, sa + uint32_t(c * NW * 1024));
-#pragma unroll
-      for (int c = 0; c < CHB; ++c) load16(ob[c], gb, sb + uint32_t(c * NW * 1024));
-    } else {  // chunks past the row's last 16 bytes re-read its last chunk; the fragments mask them
-      const int last = (ktail - 1) >> 4;
-#pragma unroll
-      for (int c = 0; c < CHA; ++c) {
-        const int row = 8 * (wave + NW * c) + lrow;
-        const int ch = (lane & 7) ^ row_swizzle(row);
-        load16(oa[c] - uint32_t(max(ch - last, 0) * 16), ga, sa + uint32_t(c * NW * 1024));
-      }
-#pragma unroll
-      for (int c = 0; c < CHB; ++c) {
-        const int row = 8 * (wave + NW * c) + lrow;
-        const int ch = (lane & 7) ^ row_swizzle(row);
-        load16(ob[c] - uint32_t(max(ch - last, 0) * 16), gb, sb + uint32_t(c * NW * 1024));
-      }
-    }
-  };
-
-  // 16-row fragments: lane l holds row (l & 15), bytes 32 (l >> 4) .. +31 of
-  // the K tile (the layout of the large tiles).
-  const int fr = lane & 15, fq = lane >> 4;
-  const uint32_t f_lo = uint32_t(fr) * BK + uint32_t((2 * fq) ^ row_swizzle(fr)) * 16;
-  const uint32_t f_hi = uint32_t(fr) * BK + uint32_t((2 * fq + 1) ^ row_swizzle(fr)) * 16;
-  auto frag = [&](uint32_t base) -> v8i {
-    const uint4 lo = *reinterpret_cast<const uint4 *>(smem + base + f_lo);
-    const uint4 hi = *reinterpret_cast<const uint4 *>(smem + base + f_hi);
-    return v8i{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
-  };
-  struct Frags {
-    v8i a[I], b[J];
-  };
-  auto read = [&](uint32_t stage, Frags &f) {
-#pragma unroll
-    for (int i = 0; i < I; ++i) f.a[i] = frag(stage + uint32_t((wm * TM + i * 16) * BK));
-#pragma unroll
-    for (int j = 0; j < J; ++j) f.b[j] = frag(stage + uint32_t((BM + wn * TN + j * 16) * BK));
-  };
-  auto mask = [&](Frags &f) {
-    const int valid = ktail - 32 * fq;
-#pragma unroll
-    for (int i = 0; i < I; ++i) f.a[i] = mask_frag(f.a[i], valid);
-#pragma unroll
-    for (int j = 0; j < J; ++j) f.b[j] = mask_frag(f.b[j], valid);
-  };
-
   v4f acc[I][J];
-#pragma unroll
-  for (int i = 0; i < I; ++i)
-#pragma unroll
-    for (int j = 0; j < J; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-
-  auto mfma = [&](int i, int j, const Frags &f) {
-    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f.b[j], f.a[i], acc[i][j], FB, FA, 0, 0, 0, 0);
-  };
-  uint32_t rd = 0;  // stage of tile t
-  // Step t: fragments of tile t are in `cur`; tile t + 1's are read into `nxt`.
-  // main_step (tile t + S exists and is full): after each MFMA, in a fixed
-  // order, one LDS-bound load and one fragment read where they are due, so the
-  // three pipes (MFMA, LDS, address) work side by side in a single wave.
-  auto main_step = [&](int t, const Frags &cur, Frags &nxt) {
-    // tile t + 1 complete: of the tiles issued so far, t + 2 .. t + S - 1 may
-    // still be in flight (the counter completes in order)
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * L) : "memory");
-    __syncthreads();  // tile t + 1 published; every wave holds tile t's fragments
-    const uint8_t *ga = g.a + int64_t(t + S) * BK;
-    const uint8_t *gb = g.b + int64_t(t + S) * BK;
-    const uint32_t sa = wblk + rd;  // tile t's stage takes tile t + S; load d lands at sa + 4096 d
-    rd = rd + STAGE == uint32_t(S * STAGE) ? 0u : rd + STAGE;
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int d = 0; d < L; ++d)
-        if (d * Q / L == q) {
-          if (d == 0)
-            asm volatile("s_mov_b32 m0, %0" ::"s"(sa) : "m0");
-          else
-            asm volatile("s_add_u32 m0, m0, %0" ::"n"(NW * 1024) : "m0", "scc");
-        }
-      __builtin_amdgcn_sched_barrier(0);  // M0 is written before the MFMA, never next to the load
-      mfma(q / J, q % J, cur);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int d = 0; d < L; ++d)
-        if (d * Q / L == q) {
-          if (d < CHA)
-            asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(oa[d]), "s"(ga) : "memory");
-          else
-            asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(ob[d - CHA]), "s"(gb) : "memory");
-        }
-#pragma unroll
-      for (int r = 0; r < I + J; ++r)
-        if (r * Q / (I + J) == q) {
-          if (r < I)
-            nxt.a[r] = frag(rd + uint32_t((wm * TM + r * 16) * BK));
-          else
-            nxt.b[r - I] = frag(rd + uint32_t((BM + wn * TN + (r - I) * 16) * BK));
-        }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  // The last steps: no tile, or the partial one, left to issue.  (Past the last
-  // tile a stale stage is read and never used, so that the reads stay
-  // branch-free and the compiler can wait for them one by one.)
-  auto last_step = [&](int t, const Frags &cur, Frags &nxt) {
-    if (t + S <= T)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * L) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const uint32_t freed = rd;
-    rd = rd + STAGE == uint32_t(S * STAGE) ? 0u : rd + STAGE;
-    read(rd, nxt);
-    __builtin_amdgcn_sched_barrier(0);
-    if (t + S < T) issue(t + S, freed);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int q = 0; q < Q; ++q) mfma(q / J, q % J, cur);
-    __builtin_amdgcn_sched_barrier(0);
-    if (t + 2 == T && ktail != 0) mask(nxt);
-  };
-
-  if (T > 0) {
-    Frags f0, f1;
-#pragma unroll
-    for (int t = 0; t < S; ++t)
-      if (t < T) issue(t, uint32_t(t * STAGE));
-    if (T >= S)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 1) * L) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    read(0, f0);
-    if (T == 1 && ktail != 0) mask(f0);
-    int t = 0;
-    for (; t + 1 + S < K / BK; t += 2) {
-      main_step(t, f0, f1);
-      main_step(t + 1, f1, f0);
-    }
-    for (; t + 1 < T; t += 2) {
-      last_step(t, f0, f1);
-      last_step(t + 1, f1, f0);
-    }
-    if (t < T) {
-#pragma unroll
-      for (int q = 0; q < Q; ++q) mfma(q / J, q % J, f0);
-    }
-  }
+  ring_k_loop<FA, FB, BM, BN, S>(g.a, g.b, oa, ob, int(g.k), smem, acc);
+  const int fr = lane & 15, fq = lane >> 4;  // the lane holds row fr, columns 4 fq .. of every 16 x 16 block
 
   // Epilogue: BM / 64 passes of 64 rows through LDS.  Accumulating, a pass
   // reads its destination before it stages its rows, all loads in flight.

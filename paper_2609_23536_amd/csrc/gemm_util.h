@@ -1,6 +1,7 @@
 // Device helpers shared by the FP8 GEMM kernels.
 #pragma once
 
+#include "bf16.h"
 #include "kernels.h"
 
 namespace qe {
@@ -67,17 +68,6 @@ __device__ __forceinline__ uint4 mask_tail(uint4 v, int64_t valid) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-
-// Two floats to two bf16 (round to nearest even, NaN stays a quiet NaN with
-// its sign and top payload bits) with the gfx950 packed conversion; bit-equal
-// to the integer form (u + 0x7fff + ((u >> 16) & 1)) >> 16 on every input,
-// which was checked on MI355X over all exponents, boundaries, denormals and NaNs.
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t bf16x2_bits(float lo, float hi) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
-}
-__device__ __forceinline__ uint16_t bf16_bits(float f) { return uint16_t(bf16x2_bits(f, 0.0f)); }
 
 __device__ __forceinline__ int pow2_exponent(const float *p) { return int((__float_as_uint(*p) >> 23) & 0xffu) - 127; }
 

@@ -222,6 +222,9 @@ qe_status qe_fp8_gemm_tn(const uint8_t *a, qe_fp8_fmt fmt_a, int64_t lda, const 
  * (a graph captured earlier keeps the shapes it was captured with).  The
  * shapes all give the same bits: the same 16x16x128 MFMA with the same
  * reduction bytes per lane, the same order along K, no split reduction.
+ * qe_fp8_gemm_act and qe_fp8_gemm_gated choose among 256x256, 192x256 and the
+ * small shapes; there QE_TILE_192x256 forces that shape, any other value but
+ * QE_TILE_AUTO 256x256.
  * Errors: QE_ERR_INVALID_ARG for a value outside the enum. */
 typedef enum {
   QE_TILE_AUTO = 0,
@@ -232,6 +235,103 @@ typedef enum {
   QE_TILE_256x224 = 5
 } qe_gemm_tile;
 qe_status qe_set_gemm_tile(qe_gemm_tile tile);
+
+/* ------------------------------------------------------------------------
+ * Between two linears: epilogues, the gated feed-forward, what its backward
+ * keeps and the gradient through the activation (stateless, stream-ordered,
+ * allocation-free; they can be captured into a graph by the caller)
+ * ------------------------------------------------------------------------ */
+
+/* act(z): z; max(z, 0); z Phi(z); z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2;
+ * z / (1 + e^-z).  NaN in, NaN out; an infinite z gives what the formula gives
+ * (+inf stays, -inf is NaN except for QE_ACT_NONE and QE_ACT_RELU). */
+typedef enum { QE_ACT_NONE = 0, QE_ACT_RELU = 1, QE_ACT_GELU = 2, QE_ACT_GELU_TANH = 3, QE_ACT_SILU = 4 } qe_act;
+
+/* An activation kept for the backward pass: [rows, cols] values, row stride ld
+ * elements.  QE_SAVED_BF16: data holds BF16 (2-byte aligned).  QE_SAVED_I8: an 8-bit
+ * checkpoint: data holds one int8 code per value (any alignment), exps one byte
+ * per 32 consecutive columns of a row, row stride ld_exps >= ceil(cols / 32).
+ * Of a group with a = max |x|, s = floor(log2(127 / a)) clamped to [-126, 126]
+ * (126 for a = 0), code = x 2^s rounded to nearest even, byte = 127 - s and the
+ * restored value code 2^-s, exact in BF16 and FP32: off by at most half a step
+ * 2^-s, which lies between a / 127 and a / 63.5.  A group that holds a NaN or
+ * an infinity restores as NaN (byte 255, codes 0). */
+typedef enum { QE_SAVED_NONE = 0, QE_SAVED_BF16 = 1, QE_SAVED_I8 = 2 } qe_saved_kind;
+typedef struct {
+  void *data;
+  int64_t ld;
+  uint8_t *exps;
+  int64_t ld_exps;
+  int32_t kind; /* qe_saved_kind */
+  int32_t reserved;
+} qe_saved;
+
+/* What an FP8 product does with its sum before it stores it; zero-initialised
+ * it does nothing.  bias: n values, residual: [m, n] with row stride
+ * ld_residual >= n (both QE_F32 or QE_BF16, aligned to their element, NULL for
+ * none); saved receives the pre-activation. */
+typedef struct {
+  const void *bias;
+  const void *residual;
+  int64_t ld_residual;
+  int32_t bias_dtype, residual_dtype; /* qe_dtype */
+  int32_t act;                        /* qe_act */
+  int32_t reserved;
+  qe_saved saved;
+} qe_epilogue;
+
+/* FP8 product with bias, activation and residual in its epilogue:
+ *   Z = (a_scale_inv * b_scale_inv) * sum_r A[i][r] * B[j][r] + bias[j]
+ *   c[i][j] = act(Z) + residual[i][j]
+ * in FP32, rounded once.  epi_host == NULL: the sum alone.  c may be the
+ * residual itself (same type and stride).  Operands and layout rules as for
+ * qe_fp8_gemm_tn, except that lda and ldb are below 2^23 and m, n below 2^31;
+ * operands of any total size run in one launch.  A row of c is one token: m may
+ * be 1.  Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
+qe_status qe_fp8_gemm_act(const uint8_t *a, qe_fp8_fmt fmt_a, int64_t lda, const uint8_t *b, qe_fp8_fmt fmt_b, int64_t ldb,
+                          int64_t m, int64_t n, int64_t k, const float *a_scale_inv, const float *b_scale_inv,
+                          const qe_epilogue *epi_host, void *c, qe_dtype c_dtype, int64_t ldc, qe_stream stream);
+
+/* Gated feed-forward: both projections, the activation and the product in one
+ * kernel: with G = X Wg^T and U = X Wu^T (scaled as above), h = act(G) * U,
+ * [m, n], in FP32, rounded once.  x: m x k codes; w_gate, w_up: n x k codes each,
+ * of one format and row stride (the halves of a fused [2n, k] weight are w and
+ * w + n * ldw).  gate_host / up_host, both NULL or of one kind, receive G and
+ * U for qe_act_grad.  Layout rules as for qe_fp8_gemm_act.
+ * Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
+qe_status qe_fp8_gemm_gated(const uint8_t *x, qe_fp8_fmt fmt_x, int64_t ldx, const uint8_t *w_gate, const uint8_t *w_up,
+                            qe_fp8_fmt fmt_w, int64_t ldw, int64_t m, int64_t n, int64_t k, const float *x_scale_inv,
+                            const float *gate_scale_inv, const float *up_scale_inv, qe_act act, void *h, qe_dtype h_dtype,
+                            int64_t ldh, const qe_saved *gate_host, const qe_saved *up_host, qe_stream stream);
+
+/* Gradient through the activation of the two products above, from what they
+ * saved.  u_host == NULL: dZ = dd * act'(Z), [rows, cols].  Else, with z_host the
+ * gates: dG = dd * U * act'(G) and dU = dd * act(G) side by side, [rows, 2 cols]
+ * (the output gradient of a fused [2 cols, k] weight).  relu'(0) = 0.
+ * meta_host (may be NULL) is the gradient role's delayed-scaling state: as in
+ * qe_quantize_fp8, q_row and q_col (either may be NULL) receive the codes at the
+ * role's scale and their transpose, max |dZ| is folded into its amax, and
+ * scale_inv_snapshot, if set, the scale_inv used.  dz, if set, receives the
+ * values themselves.  dbias, if set (u_host NULL only), receives their column sums
+ * (QE_PLACE_INIT) or is increased by them (QE_PLACE_ACCUM), in FP32 and in an
+ * order that does not change from call to call; workspace then holds
+ * ceil(rows / 64) * cols floats, whose contents do not matter before or after.
+ * Outputs may not overlap inputs or each other.  rows or cols may be 0 (dbias is
+ * then set to 0, or kept).
+ * Errors: QE_ERR_INVALID_ARG (also codes or a snapshot without a meta); QE_ERR_HIP. */
+qe_status qe_act_grad(const void *dd, qe_dtype dd_dtype, int64_t ld_dd, int64_t rows, int64_t cols, qe_act act,
+                      const qe_saved *z_host, const qe_saved *u_host, const qe_fp8_meta *meta_host, uint8_t *q_row,
+                      int64_t ld_row, uint8_t *q_col, int64_t ld_col, float *scale_inv_snapshot, void *dz,
+                      qe_dtype dz_dtype, int64_t ld_dz, float *dbias, qe_place_mode dbias_mode, float *workspace,
+                      qe_stream stream);
+
+/* Store an activation x [rows, cols] (QE_F32 or QE_BF16, row stride ld) in an
+ * 8-bit checkpoint, and restore it (saved_host->kind must be QE_SAVED_I8).
+ * Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
+qe_status qe_act_save(const void *x, qe_dtype x_dtype, int64_t ld, int64_t rows, int64_t cols, const qe_saved *saved_host,
+                      qe_stream stream);
+qe_status qe_act_restore(const qe_saved *saved_host, int64_t rows, int64_t cols, void *x, qe_dtype x_dtype, int64_t ld,
+                         qe_stream stream);
 
 /* ------------------------------------------------------------------------
  * Stage context: layers, tape slots, versions, arena, executor

@@ -19,7 +19,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libqe.so")
 
 HIP_SOURCES = ["api.hip", "quantize.hip", "scale_update.hip", "gemm_fp8.hip", "gemm_ring.hip", "gemm_dispatch.hip",
-               "grad_copy.hip", "amax.hip"]
+               "grad_copy.hip", "amax.hip", "act_gemm.hip", "act_grad.hip", "act_save.hip"]
 CXX_SOURCES = ["contract.cpp"]
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",

@@ -1,0 +1,137 @@
+// Activations, their slopes and the 8-bit checkpoint format, as device
+// functions of the kernels that read or write them (act_gemm.hip,
+// act_grad.hip, act_save.hip).
+#pragma once
+
+#include "fp8_enc.h"
+
+namespace qe {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------- activations
+// With p(t) = 1 / (1 + e^-t):
+//   silu(z) = z p(z)                       silu'(z) = p (1 + z (1 - p))
+//   gelu(z) = z Phi(z)                     gelu'(z) = Phi + z phi(z)
+//   gelu_tanh(z) = z p(2 c (z + b z^3))    since (1 + tanh t) / 2 = p(2 t),
+//   gelu_tanh'(z) = P + z P (1 - P) 2 c (1 + 3 b z^2),  c = sqrt(2 / pi), b = 0.044715
+// e^-t is the hardware's 2^x (1 ulp) of a once rounded product, and the
+// quotient the hardware's reciprocal (1 ulp): a relative error of about
+// (2 + |t|) 2^-24, far below the BF16 the values are usually rounded to.
+__device__ __forceinline__ float sigmoid(float t) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t * -1.44269504088896340736f));
+}
+constexpr float kGelu2C = 1.59576912160573071176f;  // 2 sqrt(2 / pi)
+constexpr float kGeluB = 0.044715f;
+constexpr float kGeluFar = 256.0f;  // z^2 from which P is 0 or 1 in 32 bits; keeps z P (1 - P) z^2 off 0 * inf
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+  if constexpr (ACT == kActRelu) return z < 0.0f ? 0.0f : z;  // NaN stays
+  if constexpr (ACT == kActGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752440f));
+  if constexpr (ACT == kActGeluTanh) return z * sigmoid(kGelu2C * z * (1.0f + kGeluB * fminf(z * z, kGeluFar)));
+  if constexpr (ACT == kActSilu) return z * sigmoid(z);
+  return z;
+}
+
+// value and slope
+template <int ACT>
+__device__ __forceinline__ void act_both(float z, float &v, float &d) {
+  if constexpr (ACT == kActRelu) {
+    v = z < 0.0f ? 0.0f : z;
+    d = z > 0.0f ? 1.0f : 0.0f;
+  } else if constexpr (ACT == kActGelu) {
+    const float cdf = 0.5f + 0.5f * erff(z * 0.70710678118654752440f);
+    v = z * cdf;
+    d = cdf + z * (0.39894228040143267794f * __builtin_amdgcn_exp2f(z * z * -0.72134752044448170368f));
+  } else if constexpr (ACT == kActGeluTanh) {
+    const float q = fminf(z * z, kGeluFar);
+    const float p = sigmoid(kGelu2C * z * (1.0f + kGeluB * q));
+    v = z * p;
+    d = p + v * (1.0f - p) * (kGelu2C * (1.0f + 3.0f * kGeluB * q));
+  } else if constexpr (ACT == kActSilu) {
+    const float p = sigmoid(z);
+    v = z * p;
+    d = p + v * (1.0f - p);
+  } else {
+    v = z;
+    d = 1.0f;
+  }
+}
+
+// Calls f.operator()<ACT>() for the (uniform) activation `act`.
+template <typename F>
+__device__ __forceinline__ void act_switch(int act, F &&f) {
+  switch (act) {
+    case kActRelu: f(std::integral_constant<int, kActRelu>{}); break;
+    case kActGelu: f(std::integral_constant<int, kActGelu>{}); break;
+    case kActGeluTanh: f(std::integral_constant<int, kActGeluTanh>{}); break;
+    case kActSilu: f(std::integral_constant<int, kActSilu>{}); break;
+    default: f(std::integral_constant<int, kActNone>{}); break;
+  }
+}
+
+// ----------------------------------------------------------- 8-bit checkpoint
+// 32 columns of a row share a step 2^-s, s = floor(log2(127 / amax)) clamped to
+// [-126, 126]; a value is the int8 code rne(x 2^s), so |code| <= 127 and the
+// error is at most half a step, amax / 127 at most.  The group's byte is
+// 127 - s, the step's exponent field: amax's own exponent field less 6, one
+// more where its mantissa is above 127/64 (the carry of the addition below).
+// An infinity or a NaN makes the byte 255, whose step is infinite: code * step
+// and the restoring fma below are then NaN for the whole group.
+// Steps that are powers of two keep the restored values exact in BF16 and FP32
+// (a code has seven bits), scaling exact, and the byte count at 33/32.
+constexpr int kSaveGroup = 32;
+
+__device__ __forceinline__ uint32_t save_exponent(uint32_t amax) {
+  const int e = int((amax + 0x1ffffu) >> 23) - 6;
+  return amax >= 0x7f800000u ? 255u : uint32_t(e < 1 ? 1 : e);
+}
+
+// Four values -> four int8 codes.  x 2^s is exact; adding 1.5 * 2^23 rounds it
+// to nearest even and leaves the code in the sum's low byte.
+__device__ __forceinline__ uint32_t save_codes(f32x4 x, uint32_t byte) {
+  const float mult = __uint_as_float((254u - byte) << 23);  // 2^s
+  constexpr float kRound = 12582912.0f;
+  const uint32_t b0 = __float_as_uint(__builtin_fmaf(x[0], mult, kRound)), b1 = __float_as_uint(__builtin_fmaf(x[1], mult, kRound));
+  const uint32_t b2 = __float_as_uint(__builtin_fmaf(x[2], mult, kRound)), b3 = __float_as_uint(__builtin_fmaf(x[3], mult, kRound));
+  const uint32_t lo = __builtin_amdgcn_perm(b1, b0, 0x0c0c0400u), hi = __builtin_amdgcn_perm(b3, b2, 0x04000c0cu);
+  return byte == 255u ? 0u : lo | hi;
+}
+
+// Code j of a word, restored: the code as an unsigned byte u = code + 128 has a
+// hardware conversion, and u step - 128 step is exact.  `word` has its sign
+// bits flipped (w ^ 0x80808080).
+template <int J>
+__device__ __forceinline__ float restore_code(uint32_t word, float step, float off) {
+  return __builtin_fmaf(float((word >> (8 * J)) & 0xffu), step, off);  // off = -128 step
+}
+__device__ __forceinline__ f32x4 restore4(uint32_t codes, uint32_t byte) {
+  const float step = __uint_as_float(byte << 23), off = -128.0f * step;
+  const uint32_t w = codes ^ 0x80808080u;
+  return f32x4{restore_code<0>(w, step, off), restore_code<1>(w, step, off), restore_code<2>(w, step, off),
+             restore_code<3>(w, step, off)};
+}
+
+// Maximum over the 4 (8) lanes of an aligned group of lanes, in all of them.
+__device__ __forceinline__ uint32_t max_lanes4(uint32_t v) {
+  uint32_t o = uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0xb1, 0xf, 0xf, true));  // lane ^ 1
+  v = o > v ? o : v;
+  o = uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x4e, 0xf, 0xf, true));  // lane ^ 2
+  return o > v ? o : v;
+}
+__device__ __forceinline__ uint32_t max_lanes8(uint32_t v) {
+  v = max_lanes4(v);
+  const uint32_t o = uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x141, 0xf, 0xf, true));  // 7 - lane within eight
+  return o > v ? o : v;
+}
+
+__device__ __forceinline__ uint32_t amax4(f32x4 x) {
+  const uint32_t a = abs_bits(x[0]), b = abs_bits(x[1]), c = abs_bits(x[2]), d = abs_bits(x[3]);
+  const uint32_t e = a > b ? a : b, f = c > d ? c : d;
+  return e > f ? e : f;
+}
+
+}  // namespace
+}  // namespace qe

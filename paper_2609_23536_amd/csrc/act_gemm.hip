@@ -1,0 +1,358 @@
+// FP8 products whose epilogue goes on past the sum (gfx950):
+//     plain:  Z = 2^(ea + eb) A B^T + bias,  D = act(Z) + residual
+//     gated:  G = 2^(ea + eg) A Bg^T,  U = 2^(ea + eu) A Bu^T,  D = act(G) * U
+// and, for a backward pass, Z (or G and U) saved beside D in BF16 or 8 bits
+// (act.h).  Everything after the sums stays in registers and FP32; D is rounded
+// once.
+//
+// The K loops are those of the plain GEMM (gemm_loops.h).  A gated tile of BN
+// operand rows holds BN/2 rows of either projection, in alternating blocks of
+// 16: an MFMA block column of gates is followed by the block column of the same
+// outputs' ups, in the same wave, so one pass over A serves both projections
+// and act(G) * U needs nothing from another wave.  Loads: 16-row blocks alternate
+// with bit 4 of the LDS row, which for every load of a wave is bit 1 of the wave, so
+// a wave loads from one projection only, whose base is a scalar.
+//
+// Operands are addressed from the tile's own first row, so that neither they
+// nor the outputs have a size limit past a tile's: a row stride below 2^23
+// bytes (256 rows of it are 2^31).
+//
+// Epilogue: accumulators go through LDS (as in the plain GEMM) and come back row
+// by row, four columns a lane; the eight lanes of a 32-column group share its
+// maximum by lane permutes.  Large tiles do this per wave (32 rows at a time),
+// small ones per workgroup (64 rows at a time).
+#include "act.h"
+#include "gemm_loops.h"
+
+namespace qe {
+namespace {
+
+typedef unsigned int u32_at1 __attribute__((aligned(1)));
+typedef float f32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned int u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
+
+// Four values from row-major storage of either type; nv of them exist.
+__device__ __forceinline__ v4f load_quad(const void *base, bool bf16, int64_t at, int nv) {
+  v4f r = {0.f, 0.f, 0.f, 0.f};
+  if (bf16) {
+    const uint16_t *p = static_cast<const uint16_t *>(base) + at;
+    if (nv == 4) {
+      const u32x2_at2 w = *reinterpret_cast<const u32x2_at2 *>(p);
+      r = v4f{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+              __uint_as_float(w.y & 0xffff0000u)};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < nv) r[e] = bf16_to_f32(p[e]);
+    }
+  } else {
+    const float *p = static_cast<const float *>(base) + at;
+    if (nv == 4) {
+      r = *reinterpret_cast<const f32x4_at4 *>(p);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < nv) r[e] = p[e];
+    }
+  }
+  return r;
+}
+
+__device__ __forceinline__ void store_quad(void *base, bool bf16, int64_t at, int nv, v4f v) {
+  if (bf16) {
+    const uint32_t lo = bf16x2_bits(v[0], v[1]), hi = bf16x2_bits(v[2], v[3]);
+    uint16_t *p = static_cast<uint16_t *>(base) + at;
+    if (nv == 4) {
+      *reinterpret_cast<u32x2_at2 *>(p) = u32x2_at2{lo, hi};
+    } else {
+      if (nv > 0) p[0] = uint16_t(lo);
+      if (nv > 1) p[1] = uint16_t(lo >> 16);
+      if (nv > 2) p[2] = uint16_t(hi);
+    }
+  } else {
+    float *p = static_cast<float *>(base) + at;
+    if (nv == 4) {
+      *reinterpret_cast<f32x4_at4 *>(p) = f32x4_at4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < nv) p[e] = v[e];
+    }
+  }
+}
+
+// Saves a quad of row `row`, columns col .. col + 3 (nv of them exist, none on
+// a row that is not `live`).  All eight lanes of a 32-column group are here
+// together, with col a multiple of 4.
+__device__ __forceinline__ void save_quad(const SavedRef &s, int64_t row, int64_t col, int nv, v4f z) {
+  if (s.kind == kSavedBF16) {
+    store_quad(s.data, true, row * s.ld + col, nv, z);
+    return;
+  }
+  if (nv < 4) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = e < nv ? z[e] : 0.0f;
+  }
+  const uint32_t byte = save_exponent(max_lanes8(amax4(z)));
+  const uint32_t codes = save_codes(z, byte);
+  uint8_t *p = static_cast<uint8_t *>(s.data) + row * s.ld + col;
+  if (nv == 4) {
+    *reinterpret_cast<u32_at1 *>(p) = codes;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < nv) p[e] = uint8_t(codes >> (8 * e));
+  }
+  if (nv > 0 && (col & (kSaveGroup - 1)) == 0) s.exps[row * s.ld_exps + col / kSaveGroup] = uint8_t(byte);
+}
+
+// Sums of ROWS output rows from row0, OW outputs each from column col0, staged
+// in LDS as rows of EP floats (gated: 16 gates, the same outputs' 16 ups, ..),
+// finished and stored by LANES lanes, this one being lane `t`.
+template <bool GATED, int ROWS, int OW, int LANES, int EP>
+__device__ __forceinline__ void finish_rows(const ActGemmParams &g, const float *ep, int t, int64_t row0, int64_t col0) {
+  constexpr int LPR = OW / 4;              // lanes per row
+  constexpr int RS = LANES / LPR;          // rows per step
+  constexpr int STEPS = ROWS / RS;
+  constexpr int Q = STEPS < 8 ? STEPS : 8;  // steps whose loads are in flight together
+  static_assert(OW % 32 == 0 && LANES % LPR == 0 && ROWS % RS == 0 && STEPS % Q == 0, "whole steps");
+  const int rl = t / LPR, cl = (t % LPR) * 4;
+  const int64_t col = col0 + cl;
+  const int nv = int(g.n - col < 0 ? 0 : (g.n - col > 4 ? 4 : g.n - col));
+  const float *src = ep + rl * EP + (GATED ? (cl / 16) * 32 + cl % 16 : cl);
+  v4f bias = {0.f, 0.f, 0.f, 0.f};
+  if (!GATED && g.bias != nullptr) bias = load_quad(g.bias, g.bias_bf16 != 0, col, nv);
+#pragma unroll 1
+  for (int s0 = 0; s0 < STEPS; s0 += Q) {
+    v4f z[Q], u[Q], r[Q];
+    int live[Q];  // columns of the step that exist
+#pragma unroll
+    for (int q = 0; q < Q; ++q) live[q] = row0 + rl + (s0 + q) * RS < g.m ? nv : 0;
+    if (!GATED && g.residual != nullptr) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+        r[q] = load_quad(g.residual, g.residual_bf16 != 0, (row0 + rl + (s0 + q) * RS) * g.ld_residual + col, live[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      z[q] = *reinterpret_cast<const v4f *>(src + (s0 + q) * (RS * EP)) + bias;
+      if constexpr (GATED) u[q] = *reinterpret_cast<const v4f *>(src + (s0 + q) * (RS * EP) + 16);
+    }
+    if (g.z.kind != kSavedNone) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        save_quad(g.z, row0 + rl + (s0 + q) * RS, col, live[q], z[q]);
+        if constexpr (GATED) save_quad(g.u, row0 + rl + (s0 + q) * RS, col, live[q], u[q]);
+      }
+    }
+    act_switch(g.act, [&](auto act) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[q][e] = act_value<decltype(act)::value>(z[q][e]);
+    });
+    if constexpr (GATED) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) z[q] *= u[q];
+    } else if (g.residual != nullptr) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) z[q] += r[q];
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+      store_quad(g.c, g.c_bf16 != 0, (row0 + rl + (s0 + q) * RS) * g.ldc + col, live[q], z[q]);
+  }
+}
+
+// f(0), f(1), .. f(N - 1) as constants: accumulators indexed by a loop variable
+// that is left in the code would go to memory.
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F &&f) {
+  if constexpr (N > 0) {
+    static_for<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
+
+struct TilePlace {
+  int64_t m0, n0;  // first row, first output column
+};
+
+// The tile of this workgroup: the order of the plain GEMM (kGroupM, xcd_remap).
+__device__ __forceinline__ TilePlace place(int tiles_m, int tiles_n, int bm, int bno) {
+  const int pid = xcd_remap(blockIdx.x, tiles_m * tiles_n);
+  const int in_group = kGroupM * tiles_n;
+  const int first_m = pid / in_group * kGroupM;
+  const int gsize = min(tiles_m - first_m, kGroupM);
+  return {int64_t(first_m + (pid % in_group) % gsize) * bm, int64_t((pid % in_group) / gsize) * bno};
+}
+
+// Operand B of a tile: its base for this wave, and the B row (from n0) of LDS row r.
+template <bool GATED>
+__device__ __forceinline__ const uint8_t *b_base(const ActGemmParams &g, int64_t n0) {
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  return (GATED && (wave & 2) != 0 ? g.b2 : g.b) + n0 * g.ldb;
+}
+template <bool GATED>
+__device__ __forceinline__ int b_row(int r) {
+  return GATED ? (r >> 5) * 16 + (r & 15) : r;
+}
+
+template <bool GATED, int FA, int FB, int BM, int BN>
+__global__ __launch_bounds__(256) void act_large_kernel(ActGemmParams g, int tiles_m, int tiles_n) {
+  constexpr int NW = 4, TM = BM / 2, TN = BN / 2, BNO = GATED ? BN / 2 : BN;
+  constexpr int I = TM / 16, J = TN / 16;
+  constexpr int CHA = BM / 32, CHB = BN / 32;
+  constexpr int STAGE = (BM + BN) * BK;
+  constexpr int EP = TN + 4;
+  static_assert(J % 2 == 0 && NW * 32 * EP * 4 <= 2 * STAGE, "block columns in pairs, staging within the stages");
+  __shared__ __attribute__((aligned(16))) uint8_t smem[2 * STAGE + NW * 1024];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave >> 1, wn = wave & 1;
+  const TilePlace at = place(tiles_m, tiles_n, BM, BNO);
+  uint32_t oa[CHA], ob[CHB];
+#pragma unroll
+  for (int c = 0; c < CHA; ++c) {
+    const int row = 8 * (wave + NW * c) + (lane >> 3);
+    oa[c] = chunk_offset(min(int64_t(row), g.m - 1 - at.m0), g.lda, (lane & 7) ^ row_swizzle(row), g.k);
+  }
+#pragma unroll
+  for (int c = 0; c < CHB; ++c) {
+    const int row = 8 * (wave + NW * c) + (lane >> 3);
+    ob[c] = chunk_offset(min(int64_t(b_row<GATED>(row)), g.n - 1 - at.n0), g.ldb, (lane & 7) ^ row_swizzle(row), g.k);
+  }
+  v4f acc[I][J];
+  large_k_loop<FA, FB, BM, BN>(g.a + at.m0 * g.lda, b_base<GATED>(g, at.n0), oa, ob, g.k, smem, acc);
+
+  __syncthreads();  // every wave is done reading the last stage
+  float *ep = reinterpret_cast<float *>(smem) + wave * 32 * EP;
+  const int fr = lane & 15, fq = lane >> 4;
+  const int e0 = pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b_scale_inv);
+  const int e1 = GATED ? pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b2_scale_inv) : e0;
+  static_for<TM / 32>([&](auto block) {
+    constexpr int i = decltype(block)::value;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const v4f a = acc[2 * i + h][j];
+        const int e = j % 2 == 0 ? e0 : e1;
+        *reinterpret_cast<v4f *>(ep + (h * 16 + fr) * EP + j * 16 + 4 * fq) =
+            v4f{__builtin_ldexpf(a[0], e), __builtin_ldexpf(a[1], e), __builtin_ldexpf(a[2], e), __builtin_ldexpf(a[3], e)};
+      }
+    // same wave writes then reads its own LDS rows: LDS operations of one wave complete in order
+    finish_rows<GATED, 32, GATED ? TN / 2 : TN, 64, EP>(g, ep, lane, at.m0 + wm * TM + i * 32,
+                                                        at.n0 + wn * (GATED ? TN / 2 : TN));
+  });
+}
+
+template <bool GATED, int FA, int FB, int BM, int BN, int S>
+__global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void act_ring_kernel(ActGemmParams g, int tiles_m,
+                                                                                           int tiles_n) {
+  constexpr int NW = 4, TM = BM / 2, TN = BN / 2, BNO = GATED ? BN / 2 : BN;
+  constexpr int I = TM / 16, J = TN / 16;
+  constexpr int CHA = BM / 32, CHB = BN / 32;
+  constexpr int STAGE = (BM + BN) * BK;
+  constexpr int ER = 64, EP = BN + 4;
+  static_assert(J % 2 == 0 && ER * EP * 4 <= S * STAGE, "block columns in pairs, staging within the stages");
+  __shared__ __attribute__((aligned(16))) uint8_t smem[S * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave >> 1, wn = wave & 1;
+  const TilePlace at = place(tiles_m, tiles_n, BM, BNO);
+  uint32_t oa[CHA], ob[CHB];
+#pragma unroll
+  for (int c = 0; c < CHA; ++c) {
+    const int row = 8 * (wave + NW * c) + (lane >> 3);
+    oa[c] = uint32_t(min(int64_t(row), g.m - 1 - at.m0) * g.lda) + ((lane & 7) ^ row_swizzle(row)) * 16;
+  }
+#pragma unroll
+  for (int c = 0; c < CHB; ++c) {
+    const int row = 8 * (wave + NW * c) + (lane >> 3);
+    ob[c] = uint32_t(min(int64_t(b_row<GATED>(row)), g.n - 1 - at.n0) * g.ldb) + ((lane & 7) ^ row_swizzle(row)) * 16;
+  }
+  v4f acc[I][J];
+  ring_k_loop<FA, FB, BM, BN, S>(g.a + at.m0 * g.lda, b_base<GATED>(g, at.n0), oa, ob, int(g.k), smem, acc);
+
+  float *ep = reinterpret_cast<float *>(smem);
+  const int fr = lane & 15, fq = lane >> 4;
+  const int e0 = pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b_scale_inv);
+  const int e1 = GATED ? pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b2_scale_inv) : e0;
+  constexpr int RW = ER < TM ? ER : TM;  // rows a wave stages per pass
+#pragma unroll
+  for (int p = 0; p < BM / ER; ++p) {
+    __syncthreads();  // the last reads of the stages (or of the previous pass) are done
+    if (TM < ER || wm == p * ER / TM) {
+#pragma unroll
+      for (int i = 0; i < RW / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const v4f a = acc[TM < ER ? i : (p * ER % TM) / 16 + i][j];
+          const int e = j % 2 == 0 ? e0 : e1;
+          *reinterpret_cast<v4f *>(ep + ((TM < ER ? wm * TM : 0) + i * 16 + fr) * EP + wn * TN + j * 16 + 4 * fq) =
+              v4f{__builtin_ldexpf(a[0], e), __builtin_ldexpf(a[1], e), __builtin_ldexpf(a[2], e), __builtin_ldexpf(a[3], e)};
+        }
+    }
+    __syncthreads();
+    finish_rows<GATED, ER, BNO, 256, EP>(g, ep, tid, at.m0 + p * ER, at.n0);
+  }
+}
+
+template <bool GATED, int FA, int FB>
+hipError_t launch_tile(int tile, const ActGemmParams &p, hipStream_t s) {
+  const dim3 block(256);
+  int tm = 0, tn = 0;
+  auto grid = [&](int bm, int bn) {
+    tm = int((p.m + bm - 1) / bm);
+    tn = int((p.n + (GATED ? bn / 2 : bn) - 1) / (GATED ? bn / 2 : bn));
+    return dim3(unsigned(tm) * unsigned(tn));
+  };
+#define QE_RING(BM, BN, S) \
+  { const dim3 n = grid(BM, BN); return klaunch(act_ring_kernel<GATED, FA, FB, BM, BN, S>, n, block, 0, s, p, tm, tn); }
+#define QE_LARGE(BM, BN) \
+  { const dim3 n = grid(BM, BN); return klaunch(act_large_kernel<GATED, FA, FB, BM, BN>, n, block, 0, s, p, tm, tn); }
+  switch (tile) {
+    case kTile64x64: QE_RING(64, 64, 4)
+    case kTile128x64: QE_RING(128, 64, 3)
+    case kTile128x64Deep: QE_RING(128, 64, 6)
+    case kTile64x128: QE_RING(64, 128, 3)
+    case kTile64x128Deep: QE_RING(64, 128, 6)
+    case kTile128x128: QE_RING(128, 128, 2)
+    case kTile128x128Deep: QE_RING(128, 128, 4)
+    case kTile192x256: QE_LARGE(192, 256)
+    default: QE_LARGE(256, 256)
+  }
+#undef QE_RING
+#undef QE_LARGE
+}
+
+template <bool GATED>
+hipError_t launch_fmts(int tile, const ActGemmParams &p, hipStream_t s) {
+  if (p.fmt_a == 0 && p.fmt_b == 0) return launch_tile<GATED, 0, 0>(tile, p, s);
+  if (p.fmt_a == 1 && p.fmt_b == 0) return launch_tile<GATED, 1, 0>(tile, p, s);
+  if (p.fmt_a == 0 && p.fmt_b == 1) return launch_tile<GATED, 0, 1>(tile, p, s);
+  return launch_tile<GATED, 1, 1>(tile, p, s);
+}
+
+}  // namespace
+
+hipError_t launch_act_gemm(const ActGemmParams &p, hipStream_t s) {
+  if (p.m <= 0 || p.n <= 0) return hipSuccess;
+  const bool gated = p.b2 != nullptr;
+  // The plain GEMM's cost model, on a product of as many operand rows.
+  GemmParams g;
+  memset(&g, 0, sizeof(g));
+  g.m = p.m;
+  g.n = gated ? 2 * p.n : p.n;
+  g.k = p.k;
+  g.c = p.c;
+  g.ldc = p.ldc;
+  g.out = p.c_bf16 ? 1 : 0;
+  constexpr unsigned kShapes = 1u << kTile256x256 | 1u << kTile192x256 | 1u << kTile64x64 | 1u << kTile128x64 |
+                               1u << kTile128x64Deep | 1u << kTile64x128 | 1u << kTile64x128Deep | 1u << kTile128x128 |
+                               1u << kTile128x128Deep;
+  const int force = gemm_tile_override();
+  const int tile = force == kTileAuto ? choose_gemm_tile(g, kShapes) : (force == kTile192x256 ? kTile192x256 : kTile256x256);
+  return gated ? launch_fmts<true>(tile, p, s) : launch_fmts<false>(tile, p, s);
+}
+
+}  // namespace qe

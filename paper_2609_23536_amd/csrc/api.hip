@@ -786,6 +786,41 @@ qe::MetaRef meta_ref(const qe_fp8_meta &m) {
   return r;
 }
 
+// ------------------------------------------------------------------ activations
+bool valid_act(int a) { return a >= QE_ACT_NONE && a <= QE_ACT_SILU; }
+
+// A saved activation of [rows, cols] values, rows and cols above 0.
+bool saved_ok(const qe_saved &s, int64_t cols) {
+  if (s.data == nullptr || s.ld < cols) return false;
+  if (s.kind == QE_SAVED_BF16) return uintptr_t(s.data) % 2 == 0;
+  return s.kind == QE_SAVED_I8 && s.exps != nullptr && s.ld_exps >= (cols + 31) / 32;
+}
+
+qe::SavedRef saved_ref(const qe_saved *s) {
+  qe::SavedRef r;
+  memset(&r, 0, sizeof(r));
+  if (s != nullptr && s->kind != QE_SAVED_NONE) {
+    r.data = s->data;
+    r.ld = s->ld;
+    r.exps = s->exps;
+    r.ld_exps = s->ld_exps;
+    r.kind = s->kind;
+  }
+  return r;
+}
+
+// Operands of the products with an epilogue: codes as for qe_fp8_gemm_tn, with
+// 32-bit offsets inside a tile of 256 rows, and a grid that fits.
+bool act_gemm_ok(const qe::ActGemmParams &p) {
+  constexpr int64_t kMaxLd = int64_t(1) << 23;
+  if (p.a == nullptr || p.b == nullptr || p.c == nullptr || p.a_scale_inv == nullptr || p.b_scale_inv == nullptr) return false;
+  if (p.lda % 16 || p.ldb % 16 || p.lda < rup16(p.k) || p.ldb < rup16(p.k) || p.lda >= kMaxLd || p.ldb >= kMaxLd) return false;
+  if (uintptr_t(p.a) % 16 || uintptr_t(p.b) % 16 || uintptr_t(p.b2) % 16) return false;
+  if (uintptr_t(p.c) % (p.c_bf16 ? 2 : 4)) return false;
+  constexpr int64_t kMaxDim = int64_t(1) << 31;
+  return p.m < kMaxDim && p.n < kMaxDim && ((p.m + 63) / 64) * ((p.n + 31) / 32) < kMaxDim;
+}
+
 }  // namespace
 
 extern "C" {
@@ -934,6 +969,172 @@ qe_status qe_fp8_gemm_tn(const uint8_t *a, qe_fp8_fmt fmt_a, int64_t lda, const 
   if (uintptr_t(c) % (c_dtype == QE_F32 ? 4 : 2)) return QE_ERR_INVALID_ARG;
   const Call call = gemm_call(a, fmt_a, lda, b, fmt_b, ldb, m, n, k, a_scale_inv, b_scale_inv, c, c_dtype, ldc, mode);
   return qe::launch_gemm(call.g, static_cast<hipStream_t>(stream)) == hipSuccess ? QE_OK : QE_ERR_HIP;
+}
+
+qe_status qe_fp8_gemm_act(const uint8_t *a, qe_fp8_fmt fmt_a, int64_t lda, const uint8_t *b, qe_fp8_fmt fmt_b, int64_t ldb,
+                          int64_t m, int64_t n, int64_t k, const float *a_scale_inv, const float *b_scale_inv,
+                          const qe_epilogue *epi_host, void *c, qe_dtype c_dtype, int64_t ldc, qe_stream stream) {
+  if (!valid_fmt(fmt_a) || !valid_fmt(fmt_b) || !valid_dtype(c_dtype)) return QE_ERR_INVALID_ARG;
+  if (m < 0 || n < 0 || k < 0 || ldc < n) return QE_ERR_INVALID_ARG;
+  qe::ActGemmParams p;
+  memset(&p, 0, sizeof(p));  // padding too: recorded launches are compared bytewise
+  if (epi_host != nullptr) {
+    const qe_epilogue &e = *epi_host;
+    if (!valid_act(e.act)) return QE_ERR_INVALID_ARG;
+    if (e.bias != nullptr && (!valid_dtype(e.bias_dtype) || !elem_aligned(e.bias, e.bias_dtype))) return QE_ERR_INVALID_ARG;
+    if (e.residual != nullptr && (!valid_dtype(e.residual_dtype) || !elem_aligned(e.residual, e.residual_dtype) ||
+                                  e.ld_residual < n))
+      return QE_ERR_INVALID_ARG;
+    if (e.saved.kind != QE_SAVED_NONE && m > 0 && n > 0 && !saved_ok(e.saved, n)) return QE_ERR_INVALID_ARG;
+    p.act = e.act;
+    p.bias = e.bias;
+    p.bias_bf16 = e.bias_dtype == QE_BF16;
+    p.residual = e.residual;
+    p.residual_bf16 = e.residual_dtype == QE_BF16;
+    p.ld_residual = e.ld_residual;
+    p.z = saved_ref(&e.saved);
+  }
+  if (m == 0 || n == 0) return QE_OK;
+  p.a = a;
+  p.b = b;
+  p.lda = lda;
+  p.ldb = ldb;
+  p.m = m;
+  p.n = n;
+  p.k = k;
+  p.a_scale_inv = a_scale_inv;
+  p.b_scale_inv = b_scale_inv;
+  p.c = c;
+  p.ldc = ldc;
+  p.c_bf16 = c_dtype == QE_BF16;
+  p.fmt_a = fmt_a;
+  p.fmt_b = fmt_b;
+  if (!act_gemm_ok(p)) return QE_ERR_INVALID_ARG;
+  return qe::launch_act_gemm(p, static_cast<hipStream_t>(stream)) == hipSuccess ? QE_OK : QE_ERR_HIP;
+}
+
+qe_status qe_fp8_gemm_gated(const uint8_t *x, qe_fp8_fmt fmt_x, int64_t ldx, const uint8_t *w_gate, const uint8_t *w_up,
+                            qe_fp8_fmt fmt_w, int64_t ldw, int64_t m, int64_t n, int64_t k, const float *x_scale_inv,
+                            const float *gate_scale_inv, const float *up_scale_inv, qe_act act, void *h, qe_dtype h_dtype,
+                            int64_t ldh, const qe_saved *gate_host, const qe_saved *up_host, qe_stream stream) {
+  if (!valid_fmt(fmt_x) || !valid_fmt(fmt_w) || !valid_dtype(h_dtype) || !valid_act(act)) return QE_ERR_INVALID_ARG;
+  if (m < 0 || n < 0 || k < 0 || ldh < n) return QE_ERR_INVALID_ARG;
+  const int32_t kind = gate_host != nullptr ? gate_host->kind : QE_SAVED_NONE;
+  if (kind != (up_host != nullptr ? up_host->kind : QE_SAVED_NONE)) return QE_ERR_INVALID_ARG;
+  if (m == 0 || n == 0) return QE_OK;
+  if (kind != QE_SAVED_NONE && (!saved_ok(*gate_host, n) || !saved_ok(*up_host, n))) return QE_ERR_INVALID_ARG;
+  qe::ActGemmParams p;
+  memset(&p, 0, sizeof(p));
+  p.a = x;
+  p.b = w_gate;
+  p.b2 = w_up;
+  p.lda = ldx;
+  p.ldb = ldw;
+  p.m = m;
+  p.n = n;
+  p.k = k;
+  p.a_scale_inv = x_scale_inv;
+  p.b_scale_inv = gate_scale_inv;
+  p.b2_scale_inv = up_scale_inv;
+  p.c = h;
+  p.ldc = ldh;
+  p.c_bf16 = h_dtype == QE_BF16;
+  p.fmt_a = fmt_x;
+  p.fmt_b = fmt_w;
+  p.act = act;
+  p.z = saved_ref(gate_host);
+  p.u = saved_ref(up_host);
+  if (w_up == nullptr || up_scale_inv == nullptr || !act_gemm_ok(p)) return QE_ERR_INVALID_ARG;
+  return qe::launch_act_gemm(p, static_cast<hipStream_t>(stream)) == hipSuccess ? QE_OK : QE_ERR_HIP;
+}
+
+qe_status qe_act_grad(const void *dd, qe_dtype dd_dtype, int64_t ld_dd, int64_t rows, int64_t cols, qe_act act,
+                      const qe_saved *z_host, const qe_saved *u_host, const qe_fp8_meta *meta_host, uint8_t *q_row,
+                      int64_t ld_row, uint8_t *q_col, int64_t ld_col, float *scale_inv_snapshot, void *dz,
+                      qe_dtype dz_dtype, int64_t ld_dz, float *dbias, qe_place_mode dbias_mode, float *workspace,
+                      qe_stream stream) {
+  if (!valid_dtype(dd_dtype) || !valid_act(act) || rows < 0 || cols < 0 || z_host == nullptr) return QE_ERR_INVALID_ARG;
+  const bool gated = u_host != nullptr;
+  const int64_t width = gated ? 2 * cols : cols;
+  if (gated && u_host->kind != z_host->kind) return QE_ERR_INVALID_ARG;
+  if (meta_host != nullptr ? !meta_ok(meta_host) : (q_row != nullptr || q_col != nullptr || scale_inv_snapshot != nullptr))
+    return QE_ERR_INVALID_ARG;
+  if ((q_row != nullptr && ld_row < width) || (q_col != nullptr && ld_col < rows)) return QE_ERR_INVALID_ARG;
+  if (dz != nullptr && (!valid_dtype(dz_dtype) || !elem_aligned(dz, dz_dtype) || ld_dz < width)) return QE_ERR_INVALID_ARG;
+  if (dbias != nullptr && (gated || uintptr_t(dbias) % 4 || (dbias_mode != QE_PLACE_INIT && dbias_mode != QE_PLACE_ACCUM)))
+    return QE_ERR_INVALID_ARG;
+  if (rows > 0 && cols > 0) {
+    if (dd == nullptr || !elem_aligned(dd, dd_dtype) || ld_dd < cols) return QE_ERR_INVALID_ARG;
+    if (!saved_ok(*z_host, cols) || (gated && !saved_ok(*u_host, cols))) return QE_ERR_INVALID_ARG;
+    if (dbias != nullptr && (workspace == nullptr || uintptr_t(workspace) % 4)) return QE_ERR_INVALID_ARG;
+    constexpr int64_t kMaxDim = int64_t(1) << 31;
+    if (rows >= kMaxDim || cols >= kMaxDim || ((rows + 63) / 64) * ((cols + 127) / 128) >= kMaxDim) return QE_ERR_INVALID_ARG;
+  }
+  qe::ActGradParams p;
+  memset(&p, 0, sizeof(p));
+  p.dd = dd;
+  p.ld_dd = ld_dd;
+  p.rows = rows;
+  p.cols = cols;
+  p.z = saved_ref(z_host);
+  p.u = saved_ref(u_host);
+  if (meta_host != nullptr) {
+    p.scale = meta_host->scale;
+    p.scale_inv = meta_host->scale_inv;
+    p.amax_slot = meta_host->amax_history;
+    p.amax_accum = meta_host->amax_accum;
+    p.fmt = meta_host->fmt;
+  }
+  p.q_row = q_row;
+  p.q_col = q_col;
+  p.ld_row = ld_row;
+  p.ld_col = ld_col;
+  p.snapshot = scale_inv_snapshot;
+  p.dz = dz;
+  p.ld_dz = ld_dz;
+  p.dz_bf16 = dz_dtype == QE_BF16;
+  p.dd_bf16 = dd_dtype == QE_BF16;
+  p.partials = dbias != nullptr ? workspace : nullptr;
+  p.act = act;
+  return qe::launch_act_grad(p, dbias, dbias_mode == QE_PLACE_ACCUM, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? QE_OK
+             : QE_ERR_HIP;
+}
+
+// Shared checks and parameters of qe_act_save and qe_act_restore.
+static qe_status save_params(const void *x, qe_dtype dtype, int64_t ld, int64_t rows, int64_t cols, const qe_saved *saved,
+                             qe::SaveParams *out) {
+  if (!valid_dtype(dtype) || rows < 0 || cols < 0 || ld < cols || saved == nullptr || saved->kind != QE_SAVED_I8)
+    return QE_ERR_INVALID_ARG;
+  if (rows > 0 && cols > 0) {
+    constexpr int64_t kMaxDim = int64_t(1) << 31;
+    if (x == nullptr || !elem_aligned(x, dtype) || !saved_ok(*saved, cols)) return QE_ERR_INVALID_ARG;
+    if (rows >= kMaxDim || cols >= kMaxDim || ((rows + 63) / 64) * ((cols + 127) / 128) >= kMaxDim) return QE_ERR_INVALID_ARG;
+  }
+  memset(out, 0, sizeof(*out));
+  out->x = const_cast<void *>(x);
+  out->ld = ld;
+  out->rows = rows;
+  out->cols = cols;
+  out->saved = saved_ref(saved);
+  out->x_bf16 = dtype == QE_BF16;
+  return QE_OK;
+}
+
+qe_status qe_act_save(const void *x, qe_dtype x_dtype, int64_t ld, int64_t rows, int64_t cols, const qe_saved *saved_host,
+                      qe_stream stream) {
+  qe::SaveParams p;
+  const qe_status st = save_params(x, x_dtype, ld, rows, cols, saved_host, &p);
+  if (st != QE_OK) return st;
+  return qe::launch_act_save(p, static_cast<hipStream_t>(stream)) == hipSuccess ? QE_OK : QE_ERR_HIP;
+}
+
+qe_status qe_act_restore(const qe_saved *saved_host, int64_t rows, int64_t cols, void *x, qe_dtype x_dtype, int64_t ld,
+                         qe_stream stream) {
+  qe::SaveParams p;
+  const qe_status st = save_params(x, x_dtype, ld, rows, cols, saved_host, &p);
+  if (st != QE_OK) return st;
+  return qe::launch_act_restore(p, static_cast<hipStream_t>(stream)) == hipSuccess ? QE_OK : QE_ERR_HIP;
 }
 
 // ------------------------------------------------------------------ context

@@ -103,6 +103,53 @@ static int cu_count() {
   return n;
 }
 
+int choose_gemm_tile(const GemmParams &g, unsigned allowed) {
+  const int64_t cbytes = g.out == 1 ? 2 : 4;
+  const int64_t cus = cu_count();
+  const double T = double((g.k + 127) / 128);
+  auto tiles = [&](int64_t bm, int64_t bn) { return ((g.m + bm - 1) / bm) * ((g.n + bn - 1) / bn); };
+  const bool scalar = !gemm_vec_ok(g);
+  double best = 0.0;
+  int pick = 0;
+  int64_t per_unit = 0;  // of a small pick
+  auto offer = [&](int tile, double cost) {
+    if ((allowed >> tile & 1u) != 0 && (pick == 0 || cost < best)) {
+      best = cost;
+      pick = tile;
+    }
+  };
+  // Large tiles: the narrower ones win where the 256 x 256 grid leaves its
+  // last round mostly empty (N = 6144: 384 tiles = 1.5 rounds, against 512
+  // tiles of 256 x 192 = 2 rounds of 0.89; N = 14336: 896 tiles = 3.5 rounds,
+  // against 1024 of 256 x 224 = 4 of 0.98).
+  auto large = [&](int tile, int64_t bm, int64_t bn, double rel) {
+    const int64_t n = tiles(bm, bn), rounds = (n + cus - 1) / cus;
+    const double f = (g.out == 2 && rounds > 1 ? kLargeF2 : kLargeF[g.out]) + (scalar ? kLargeScalar[g.out] : 0.0);
+    offer(tile, rel * double(rounds) * (f + T * (4 * n <= cus ? 1.0 : 1.2)));
+  };
+  large(kTile256x256, 256, 256, 1.0);
+  large(kTile256x224, 256, 224, kCost224);
+  large(kTile256x192, 256, 192, kCost256x192);
+  large(kTile192x256, 192, 256, kCost192x256);
+  for (const SmallTile &t : kSmall) {
+    const int64_t c = (tiles(t.bm, t.bn) + cus - 1) / cus;
+    const bool deep = t.deep != 0 && c == 1;
+    const int tile = deep ? t.deep : t.tile;
+    offer(tile, t.f + double(c) * (T * (deep ? t.s_deep : t.s + t.s_k * T) + t.e[g.out] + (scalar ? t.scalar : 0.0)));
+    if (pick == tile) per_unit = c;
+  }
+  const bool wide_pitch = g.ldc * cbytes % kWidePitch == 0;
+  if (pick >= kTile64x64 && per_unit > kFewTiles && !scalar && (wide_pitch || g.k > kShortK)) {
+    pick = 0;
+    for (const ManyRounds &t : kManyRounds) {
+      const int64_t n = tiles(t.bm, t.bn);
+      const double round = T * (t.s + t.k * T) + t.e[g.out] + (wide_pitch ? t.p[g.out] : 0.0);
+      offer(t.tile, t.f + double((n + cus - 1) / cus) * round + double(n) / double(cus) * T * t.q);
+    }
+  }
+  return pick;
+}
+
 hipError_t launch_gemm(const GemmParams &g, hipStream_t s, const UpdateParams *fused) {
   UpdateParams none;
   memset(&none, 0, sizeof(none));
@@ -147,51 +194,11 @@ hipError_t launch_gemm(const GemmParams &g, hipStream_t s, const UpdateParams *f
   const int force = g_tile_override.load(std::memory_order_relaxed);
   if (force == kTile256x128) return launch_gemm_ring(force, g, s, u);
   if (force > 0) return launch_gemm_large(force, g, s, u);
-  const int64_t cus = cu_count();
-  const double T = double((g.k + 127) / 128);
-  auto tiles = [&](int64_t bm, int64_t bn) { return ((g.m + bm - 1) / bm) * ((g.n + bn - 1) / bn); };
-  const bool scalar = !gemm_vec_ok(g);
-  double best = 0.0;
-  int pick = 0;
-  int64_t per_unit = 0;  // of a small pick
-  auto offer = [&](int tile, double cost) {
-    if (pick == 0 || cost < best) {
-      best = cost;
-      pick = tile;
-    }
-  };
-  // Large tiles: the narrower ones win where the 256 x 256 grid leaves its
-  // last round mostly empty (N = 6144: 384 tiles = 1.5 rounds, against 512
-  // tiles of 256 x 192 = 2 rounds of 0.89; N = 14336: 896 tiles = 3.5 rounds,
-  // against 1024 of 256 x 224 = 4 of 0.98).
-  auto large = [&](int tile, int64_t bm, int64_t bn, double rel) {
-    const int64_t n = tiles(bm, bn), rounds = (n + cus - 1) / cus;
-    const double f = (g.out == 2 && rounds > 1 ? kLargeF2 : kLargeF[g.out]) + (scalar ? kLargeScalar[g.out] : 0.0);
-    offer(tile, rel * double(rounds) * (f + T * (4 * n <= cus ? 1.0 : 1.2)));
-  };
-  large(kTile256x256, 256, 256, 1.0);
-  large(kTile256x224, 256, 224, kCost224);
-  large(kTile256x192, 256, 192, kCost256x192);
-  large(kTile192x256, 192, 256, kCost192x256);
-  for (const SmallTile &t : kSmall) {
-    const int64_t c = (tiles(t.bm, t.bn) + cus - 1) / cus;
-    const bool deep = t.deep != 0 && c == 1;
-    const int tile = deep ? t.deep : t.tile;
-    offer(tile, t.f + double(c) * (T * (deep ? t.s_deep : t.s + t.s_k * T) + t.e[g.out] + (scalar ? t.scalar : 0.0)));
-    if (pick == tile) per_unit = c;
-  }
-  const bool wide_pitch = g.ldc * cbytes % kWidePitch == 0;
-  if (pick >= kTile64x64 && per_unit > kFewTiles && !scalar && (wide_pitch || g.k > kShortK)) {
-    pick = 0;
-    for (const ManyRounds &t : kManyRounds) {
-      const int64_t n = tiles(t.bm, t.bn);
-      const double round = T * (t.s + t.k * T) + t.e[g.out] + (wide_pitch ? t.p[g.out] : 0.0);
-      offer(t.tile, t.f + double((n + cus - 1) / cus) * round + double(n) / double(cus) * T * t.q);
-    }
-  }
+  const int pick = choose_gemm_tile(g, ~0u);
   return pick >= kTile64x64 ? launch_gemm_ring(pick, g, s, u) : launch_gemm_large(pick, g, s, u);
 }
 
+int gemm_tile_override() { return g_tile_override.load(std::memory_order_relaxed); }
 void set_gemm_tile_override(int tile) { g_tile_override.store(tile, std::memory_order_relaxed); }
 
 }  // namespace qe

@@ -6,6 +6,7 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <type_traits>
 #include <vector>
 
 namespace qe {
@@ -154,6 +155,68 @@ struct GemmParams {
   int32_t pad;
 };
 
+// Activations: the values of qe_act.
+enum Act { kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4 };
+
+// A saved activation (qe_saved): nothing, BF16 values, or int8 codes with one
+// exponent byte for 32 columns of a row.
+enum SavedKind { kSavedNone = 0, kSavedBF16 = 1, kSavedI8 = 2 };
+struct SavedRef {
+  void *data;
+  int64_t ld;
+  uint8_t *exps;
+  int64_t ld_exps;
+  int32_t kind;
+  int32_t pad;
+};
+
+// Product with an epilogue: Z = 2^(ea + eb) A B^T + bias, D = act(Z) + residual;
+// gated (b2 set): D = act(2^(ea + eb) A B^T) * 2^(ea + eb2) A B2^T.
+struct ActGemmParams {
+  const uint8_t *a, *b, *b2;
+  int64_t lda, ldb;
+  int64_t m, n, k;
+  const float *a_scale_inv, *b_scale_inv, *b2_scale_inv;
+  void *c;
+  int64_t ldc;
+  const void *bias;
+  const void *residual;
+  int64_t ld_residual;
+  SavedRef z, u;  // the pre-activation; gated: of both projections
+  int32_t fmt_a, fmt_b;
+  int32_t act;
+  int32_t c_bf16, bias_bf16, residual_bf16;
+};
+
+// Gradient through an activation: dz = dd act'(z), or for a gated pair (u.kind
+// set) dg = dd u act'(z) and du = dd act(z) side by side.
+struct ActGradParams {
+  const void *dd;
+  int64_t ld_dd;
+  int64_t rows, cols;
+  SavedRef z, u;
+  const float *scale, *scale_inv;  // null: no codes
+  float *amax_slot, *amax_accum;
+  uint8_t *q_row, *q_col;
+  int64_t ld_row, ld_col;
+  float *snapshot;
+  void *dz;
+  int64_t ld_dz;
+  float *partials;  // bias gradient: column sums by row tile
+  int32_t act, fmt;
+  int32_t dd_bf16, dz_bf16;
+};
+
+// An activation stored in, or restored from, an 8-bit checkpoint.
+struct SaveParams {
+  void *x;
+  int64_t ld;
+  int64_t rows, cols;
+  SavedRef saved;
+  int32_t x_bf16;
+  int32_t pad;
+};
+
 // dst[n * ld + k] (=, or +=) src[n * k + k'] for the copied-gradient path.
 struct GradCopyParams {
   const float *src;  // [n, k] dense
@@ -229,8 +292,18 @@ enum GemmTile {
 // as in launch_gemm.
 hipError_t launch_gemm_large(int tile, const GemmParams &g, hipStream_t s, const UpdateParams &u);
 hipError_t launch_gemm_ring(int tile, const GemmParams &g, hipStream_t s, const UpdateParams &u);
+// The tile shape the cost model expects to be fastest among those whose bit
+// (1 << GemmTile) is set in `allowed`.
+int choose_gemm_tile(const GemmParams &g, unsigned allowed);
+hipError_t launch_act_gemm(const ActGemmParams &p, hipStream_t s);
+// The gradient's codes and dense values, then (bias non-null) the bias gradient
+// from the partial column sums.
+hipError_t launch_act_grad(const ActGradParams &p, float *dbias, bool accumulate, hipStream_t s);
+hipError_t launch_act_save(const SaveParams &p, hipStream_t s);
+hipError_t launch_act_restore(const SaveParams &p, hipStream_t s);
 // 0: tile shape from the cost model, else one shape for every product
 void set_gemm_tile_override(int tile);
+int gemm_tile_override();
 hipError_t launch_grad_copy(const GradCopyParams &p, hipStream_t s);
 hipError_t launch_amax(const AmaxParams &p, hipStream_t s);
 int amax_blocks(const AmaxParams &p);  // the workgroups launch_amax starts

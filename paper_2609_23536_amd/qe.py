@@ -22,6 +22,9 @@ ROLE_X, ROLE_W, ROLE_DY = 0, 1, 2
 SCALING_DELAYED, SCALING_CURRENT = 0, 1
 AMAX_LINES, AMAX_STRIDE = 64, 64   # amax accumulator: lines x floats between lines
 KC_QUANT, KC_UPDATE, KC_GEMM, KC_COPY, KC_AMAX = 0, 1, 2, 3, 4
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
+SAVED_NONE, SAVED_BF16, SAVED_I8 = 0, 1, 2
+SAVED_GROUP = 32   # columns of a row that share an exponent byte in an 8-bit checkpoint
 GRAPH_INPUTS_REBIND, GRAPH_INPUTS_RECAPTURE, GRAPH_INPUTS_COPY = 0, 1, 2
 
 STATUS = ["OK", "INVALID_ARG", "STALE_REF", "KEY_MISMATCH", "KEY_LIVE", "POOL_FULL", "DUPLICATE_CONSUMER", "ORDER",
@@ -48,6 +51,16 @@ class FP8Meta(C.Structure):
     _fields_ = [("amax_history", C.c_void_p), ("scale", C.c_void_p), ("scale_inv", C.c_void_p),
                 ("history_len", C.c_int32), ("margin", C.c_int32), ("fmt", C.c_int32), ("reserved", C.c_int32),
                 ("amax_accum", C.c_void_p)]
+
+
+class Saved(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("exps", C.c_void_p), ("ld_exps", C.c_int64),
+                ("kind", C.c_int32), ("reserved", C.c_int32)]
+
+
+class Epilogue(C.Structure):
+    _fields_ = [("bias", C.c_void_p), ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("bias_dtype", C.c_int32),
+                ("residual_dtype", C.c_int32), ("act", C.c_int32), ("reserved", C.c_int32), ("saved", Saved)]
 
 
 class Config(C.Structure):
@@ -95,6 +108,14 @@ _SIGS = {
     "qe_quantize_fp8_current_noalloc": [_P, _I32, _I64, _I64, C.POINTER(FP8Meta), _P, _I64, _P, _I64, _P, _P, _P],
     "qe_fp8_gemm_tn": [_P, _I32, _I64, _P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I32, _I64, _I32, _P],
     "qe_set_gemm_tile": [_I32],
+    "qe_fp8_gemm_act": [_P, _I32, _I64, _P, _I32, _I64, _I64, _I64, _I64, _P, _P, C.POINTER(Epilogue), _P, _I32, _I64,
+                        _P],
+    "qe_fp8_gemm_gated": [_P, _I32, _I64, _P, _P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I32, _P, _I32, _I64,
+                          C.POINTER(Saved), C.POINTER(Saved), _P],
+    "qe_act_grad": [_P, _I32, _I64, _I64, _I64, _I32, C.POINTER(Saved), C.POINTER(Saved), C.POINTER(FP8Meta), _P, _I64,
+                    _P, _I64, _P, _P, _I32, _I64, _P, _I32, _P, _P],
+    "qe_act_save": [_P, _I32, _I64, _I64, _I64, C.POINTER(Saved), _P],
+    "qe_act_restore": [C.POINTER(Saved), _I64, _I64, _P, _I32, _I64, _P],
     "qe_ctx_create": [C.POINTER(Config), C.POINTER(_P)],
     "qe_layer_register": [_P, C.POINTER(LayerDesc), C.POINTER(_I32)],
     "qe_layer_meta": [_P, _I32, _I32, C.POINTER(FP8Meta)],
@@ -219,6 +240,51 @@ TILE_AUTO, TILE_256x256, TILE_256x192, TILE_192x256, TILE_256x128, TILE_256x224 
 
 def qe_set_gemm_tile(tile: int) -> str:
     return _st(lib().qe_set_gemm_tile(tile))
+
+
+def make_saved(kind: int, data=None, ld: int = 0, exps=None, ld_exps: int = 0) -> Saved:
+    return Saved(ptr(data), ld, ptr(exps), ld_exps, kind, 0)
+
+
+def make_epilogue(act: int = ACT_NONE, bias=None, bias_dtype: int = F32, residual=None, residual_dtype: int = F32,
+                  ld_residual: int = 0, saved: Optional[Saved] = None) -> Epilogue:
+    return Epilogue(ptr(bias), ptr(residual), ld_residual, bias_dtype, residual_dtype, act, 0,
+                    saved if saved is not None else Saved())
+
+
+def _ref(s):
+    return None if s is None else C.byref(s)
+
+
+def qe_fp8_gemm_act(a, fmt_a: int, lda: int, b, fmt_b: int, ldb: int, m: int, n: int, k: int, a_scale_inv, b_scale_inv,
+                    epilogue: Optional[Epilogue], c, c_dtype: int, ldc: int, stream=None) -> str:
+    return _st(lib().qe_fp8_gemm_act(ptr(a), fmt_a, lda, ptr(b), fmt_b, ldb, m, n, k, ptr(a_scale_inv),
+                                     ptr(b_scale_inv), _ref(epilogue), ptr(c), c_dtype, ldc, stream_handle(stream)))
+
+
+def qe_fp8_gemm_gated(x, fmt_x: int, ldx: int, w_gate, w_up, fmt_w: int, ldw: int, m: int, n: int, k: int, x_scale_inv,
+                      gate_scale_inv, up_scale_inv, act: int, h, h_dtype: int, ldh: int, gate: Optional[Saved] = None,
+                      up: Optional[Saved] = None, stream=None) -> str:
+    return _st(lib().qe_fp8_gemm_gated(ptr(x), fmt_x, ldx, ptr(w_gate), ptr(w_up), fmt_w, ldw, m, n, k,
+                                       ptr(x_scale_inv), ptr(gate_scale_inv), ptr(up_scale_inv), act, ptr(h), h_dtype,
+                                       ldh, _ref(gate), _ref(up), stream_handle(stream)))
+
+
+def qe_act_grad(dd, dd_dtype: int, ld_dd: int, rows: int, cols: int, act: int, z: Saved, u: Optional[Saved] = None,
+                meta: Optional[FP8Meta] = None, q_row=None, ld_row: int = 0, q_col=None, ld_col: int = 0,
+                scale_inv_snapshot=None, dz=None, dz_dtype: int = F32, ld_dz: int = 0, dbias=None,
+                dbias_mode: int = INIT, workspace=None, stream=None) -> str:
+    return _st(lib().qe_act_grad(ptr(dd), dd_dtype, ld_dd, rows, cols, act, _ref(z), _ref(u), _ref(meta), ptr(q_row),
+                                 ld_row, ptr(q_col), ld_col, ptr(scale_inv_snapshot), ptr(dz), dz_dtype, ld_dz,
+                                 ptr(dbias), dbias_mode, ptr(workspace), stream_handle(stream)))
+
+
+def qe_act_save(x, x_dtype: int, ld: int, rows: int, cols: int, saved: Saved, stream=None) -> str:
+    return _st(lib().qe_act_save(ptr(x), x_dtype, ld, rows, cols, _ref(saved), stream_handle(stream)))
+
+
+def qe_act_restore(saved: Saved, rows: int, cols: int, x, x_dtype: int, ld: int, stream=None) -> str:
+    return _st(lib().qe_act_restore(_ref(saved), rows, cols, ptr(x), x_dtype, ld, stream_handle(stream)))
 
 
 def make_meta(hist, scale, scale_inv, fmt: int, margin: int = 0, amax_accum=None) -> FP8Meta:

@@ -109,8 +109,9 @@ __device__ __forceinline__ void save_quad(const SavedRef &s, int64_t row, int64_
 // Sums of ROWS output rows from row0, OW outputs each from column col0, staged
 // in LDS as rows of EP floats (gated: 16 gates, the same outputs' 16 ups, ..),
 // finished and stored by LANES lanes, this one being lane `t`.
-template <bool GATED, int ROWS, int OW, int LANES, int EP>
-__device__ __forceinline__ void finish_rows(const ActGemmParams &g, const float *ep, int t, int64_t row0, int64_t col0) {
+// FULL: all of them exist.
+template <bool GATED, bool FULL, int ROWS, int OW, int LANES, int EP>
+__device__ __forceinline__ void finish_some(const ActGemmParams &g, const float *ep, int t, int64_t row0, int64_t col0) {
   constexpr int LPR = OW / 4;              // lanes per row
   constexpr int RS = LANES / LPR;          // rows per step
   constexpr int STEPS = ROWS / RS;
@@ -118,7 +119,7 @@ __device__ __forceinline__ void finish_rows(const ActGemmParams &g, const float 
   static_assert(OW % 32 == 0 && LANES % LPR == 0 && ROWS % RS == 0 && STEPS % Q == 0, "whole steps");
   const int rl = t / LPR, cl = (t % LPR) * 4;
   const int64_t col = col0 + cl;
-  const int nv = int(g.n - col < 0 ? 0 : (g.n - col > 4 ? 4 : g.n - col));
+  const int nv = FULL ? 4 : int(g.n - col < 0 ? 0 : (g.n - col > 4 ? 4 : g.n - col));
   const float *src = ep + rl * EP + (GATED ? (cl / 16) * 32 + cl % 16 : cl);
   v4f bias = {0.f, 0.f, 0.f, 0.f};
   if (!GATED && g.bias != nullptr) bias = load_quad(g.bias, g.bias_bf16 != 0, col, nv);
@@ -127,7 +128,7 @@ __device__ __forceinline__ void finish_rows(const ActGemmParams &g, const float 
     v4f z[Q], u[Q], r[Q];
     int live[Q];  // columns of the step that exist
 #pragma unroll
-    for (int q = 0; q < Q; ++q) live[q] = row0 + rl + (s0 + q) * RS < g.m ? nv : 0;
+    for (int q = 0; q < Q; ++q) live[q] = FULL || row0 + rl + (s0 + q) * RS < g.m ? nv : 0;
     if (!GATED && g.residual != nullptr) {
 #pragma unroll
       for (int q = 0; q < Q; ++q)
@@ -162,6 +163,14 @@ __device__ __forceinline__ void finish_rows(const ActGemmParams &g, const float 
     for (int q = 0; q < Q; ++q)
       store_quad(g.c, g.c_bf16 != 0, (row0 + rl + (s0 + q) * RS) * g.ldc + col, live[q], z[q]);
   }
+}
+
+template <bool GATED, int ROWS, int OW, int LANES, int EP>
+__device__ __forceinline__ void finish_rows(const ActGemmParams &g, const float *ep, int t, int64_t row0, int64_t col0) {
+  if (row0 + ROWS <= g.m && col0 + OW <= g.n)
+    finish_some<GATED, true, ROWS, OW, LANES, EP>(g, ep, t, row0, col0);
+  else
+    finish_some<GATED, false, ROWS, OW, LANES, EP>(g, ep, t, row0, col0);
 }
 
 // f(0), f(1), .. f(N - 1) as constants: accumulators indexed by a loop variable

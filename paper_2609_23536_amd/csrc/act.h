@@ -26,10 +26,28 @@ constexpr float kGelu2C = 1.59576912160573071176f;  // 2 sqrt(2 / pi)
 constexpr float kGeluB = 0.044715f;
 constexpr float kGeluFar = 256.0f;  // z^2 from which P is 0 or 1 in 32 bits; keeps z P (1 - P) z^2 off 0 * inf
 
+// Phi(z) and e = exp(-z^2 / 2), after Abramowitz and Stegun, Handbook of
+// Mathematical Functions, 7.1.26: with x = |z| / sqrt(2) and t = 1 / (1 + p x),
+// 1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2), off by at most 1.5e-7, so Phi by
+// 7.5e-8.  Without a branch; on the negative side nothing cancels.
+__device__ __forceinline__ float normal_cdf(float z, float &e) {
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.3275911f * 0.70710678118654752440f, 1.0f));
+  e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170368f);
+  float s = __builtin_fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+  s = __builtin_fmaf(t, s, 0.5f * 1.421413741f);
+  s = __builtin_fmaf(t, s, 0.5f * -0.284496736f);
+  s = __builtin_fmaf(t, s, 0.5f * 0.254829592f);
+  s *= t * e;  // Phi(-|z|)
+  return z < 0.0f ? s : 1.0f - s;
+}
+
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
   if constexpr (ACT == kActRelu) return z < 0.0f ? 0.0f : z;  // NaN stays
-  if constexpr (ACT == kActGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752440f));
+  if constexpr (ACT == kActGelu) {
+    float e;
+    return z * normal_cdf(z, e);
+  }
   if constexpr (ACT == kActGeluTanh) return z * sigmoid(kGelu2C * z * (1.0f + kGeluB * fminf(z * z, kGeluFar)));
   if constexpr (ACT == kActSilu) return z * sigmoid(z);
   return z;
@@ -42,9 +60,10 @@ __device__ __forceinline__ void act_both(float z, float &v, float &d) {
     v = z < 0.0f ? 0.0f : z;
     d = z > 0.0f ? 1.0f : 0.0f;
   } else if constexpr (ACT == kActGelu) {
-    const float cdf = 0.5f + 0.5f * erff(z * 0.70710678118654752440f);
+    float e;
+    const float cdf = normal_cdf(z, e);
     v = z * cdf;
-    d = cdf + z * (0.39894228040143267794f * __builtin_amdgcn_exp2f(z * z * -0.72134752044448170368f));
+    d = cdf + z * (0.39894228040143267794f * e);
   } else if constexpr (ACT == kActGeluTanh) {
     const float q = fminf(z * z, kGeluFar);
     const float p = sigmoid(kGelu2C * z * (1.0f + kGeluB * q));
@@ -125,6 +144,15 @@ __device__ __forceinline__ uint32_t max_lanes8(uint32_t v) {
   v = max_lanes4(v);
   const uint32_t o = uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x141, 0xf, 0xf, true));  // 7 - lane within eight
   return o > v ? o : v;
+}
+
+// The same over lanes l, l ^ 16, l ^ 32 and l ^ 48: each exchange leaves one half's
+// values in the first result and the other half's in the second, in all lanes.
+__device__ __forceinline__ uint32_t max_lanes_by16(uint32_t v) {
+  auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = r[0] > r[1] ? r[0] : r[1];
+  r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return r[0] > r[1] ? r[0] : r[1];
 }
 
 __device__ __forceinline__ uint32_t amax4(f32x4 x) {

@@ -28,6 +28,8 @@ namespace qe {
 namespace {
 
 typedef unsigned int u32_at1 __attribute__((aligned(1)));
+typedef uint16_t u16_at1 __attribute__((aligned(1)));
+typedef unsigned int u32x4_at16 __attribute__((ext_vector_type(4)));
 typedef float f32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned int u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
 
@@ -183,6 +185,62 @@ __device__ __forceinline__ void static_for(F &&f) {
   }
 }
 
+// Stores a wave's [32, 4 OWQ] BF16 block, of which the lane holds quad q of row
+// 16 h + (lane & 15), columns 16 q' + 4 (lane >> 4) .., through `ls`: the lanes
+// then write whole row runs, 16 bytes each.  LDS operations of one wave
+// complete in order.
+template <int QUADS>
+__device__ __forceinline__ void store_block_bf16(uint8_t *ls, int lane, uint16_t *dst, int64_t ld, const v4f (&v)[2][QUADS]) {
+  constexpr int RUN = 32 * QUADS, PITCH = RUN + 16, LPR = RUN / 16, RS = 64 / LPR;  // bytes of a row, lanes a row, rows a step
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int q = 0; q < QUADS; ++q)
+      *reinterpret_cast<uint2 *>(ls + (16 * h + (lane & 15)) * PITCH + 32 * q + 8 * (lane >> 4)) =
+          make_uint2(bf16x2_bits(v[h][q][0], v[h][q][1]), bf16x2_bits(v[h][q][2], v[h][q][3]));
+  uint16_t *out = dst + (lane / LPR) * ld + (lane % LPR) * 8;
+#pragma unroll
+  for (int s = 0; s < 32 / RS; ++s)
+    __builtin_nontemporal_store(*reinterpret_cast<const u32x4_at16 *>(ls + (s * RS + lane / LPR) * PITCH + (lane % LPR) * 16),
+                                reinterpret_cast<u32x4_in *>(out + s * RS * ld));
+}
+
+// The same for an 8-bit checkpoint: codes of whole 32-column groups (two quads
+// of four lanes), and their exponent bytes.
+template <int QUADS>
+__device__ __forceinline__ void save_block_i8(uint8_t *ls, int lane, uint8_t *dst, int64_t ld, uint8_t *exps, int64_t ld_exps,
+                                              const v4f (&v)[2][QUADS]) {
+  constexpr int RUN = 16 * QUADS, PITCH = RUN + 16, LPR = RUN / 16, RS = 64 / LPR;
+  static_assert(QUADS % 2 == 0 && QUADS <= 8, "whole groups, their bytes in a word");
+  uint32_t bytes[2][(QUADS + 7) / 8] = {};
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int q = 0; q < QUADS; q += 2) {
+      const uint32_t a = amax4(v[h][q]), b = amax4(v[h][q + 1]);
+      const uint32_t byte = save_exponent(max_lanes_by16(a > b ? a : b));
+      bytes[h][0] |= byte << (4 * q);
+      uint8_t *at = ls + (16 * h + (lane & 15)) * PITCH + 16 * q + 4 * (lane >> 4);
+      *reinterpret_cast<uint32_t *>(at) = save_codes(v[h][q], byte);
+      *reinterpret_cast<uint32_t *>(at + 16) = save_codes(v[h][q + 1], byte);
+    }
+  uint8_t *out = dst + (lane / LPR) * ld + (lane % LPR) * 16;
+#pragma unroll
+  for (int s = 0; s < 32 / RS; ++s)
+    __builtin_nontemporal_store(*reinterpret_cast<const u32x4_at16 *>(ls + (s * RS + lane / LPR) * PITCH + (lane % LPR) * 16),
+                                reinterpret_cast<u32x4_out *>(out + s * RS * ld));
+  if (lane < 32) {  // lanes 0 .. 15 the first block row's bytes, 16 .. 31 the second's
+    uint8_t *e = exps + lane * ld_exps;
+    const uint32_t w = lane < 16 ? bytes[0][0] : bytes[1][0];
+    if constexpr (QUADS == 8)
+      *reinterpret_cast<u32_out *>(e) = w;
+    else if constexpr (QUADS == 4)
+      *reinterpret_cast<u16_at1 *>(e) = uint16_t(w);
+    else
+      *e = uint8_t(w);
+  }
+}
+
 struct TilePlace {
   int64_t m0, n0;  // first row, first output column
 };
@@ -196,11 +254,19 @@ __device__ __forceinline__ TilePlace place(int tiles_m, int tiles_n, int bm, int
   return {int64_t(first_m + (pid % in_group) % gsize) * bm, int64_t((pid % in_group) / gsize) * bno};
 }
 
+// An address that is the same in the whole wave, in scalar registers (the K
+// loops' inline assembly takes it there; the compiler computes it in vector ones).
+__device__ __forceinline__ const uint8_t *uniform(const uint8_t *p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(int(uint32_t(v))), hi = __builtin_amdgcn_readfirstlane(int(v >> 32));
+  return reinterpret_cast<const uint8_t *>(uint64_t(hi) << 32 | lo);
+}
+
 // Operand B of a tile: its base for this wave, and the B row (from n0) of LDS row r.
 template <bool GATED>
 __device__ __forceinline__ const uint8_t *b_base(const ActGemmParams &g, int64_t n0) {
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-  return (GATED && (wave & 2) != 0 ? g.b2 : g.b) + n0 * g.ldb;
+  return uniform((GATED && (wave & 2) != 0 ? g.b2 : g.b) + n0 * g.ldb);
 }
 template <bool GATED>
 __device__ __forceinline__ int b_row(int r) {
@@ -231,15 +297,63 @@ __global__ __launch_bounds__(256) void act_large_kernel(ActGemmParams g, int til
     ob[c] = chunk_offset(min(int64_t(b_row<GATED>(row)), g.n - 1 - at.n0), g.ldb, (lane & 7) ^ row_swizzle(row), g.k);
   }
   v4f acc[I][J];
-  large_k_loop<FA, FB, BM, BN>(g.a + at.m0 * g.lda, b_base<GATED>(g, at.n0), oa, ob, g.k, smem, acc);
+  large_k_loop<FA, FB, BM, BN>(uniform(g.a + at.m0 * g.lda), b_base<GATED>(g, at.n0), oa, ob, g.k, smem, acc);
 
   __syncthreads();  // every wave is done reading the last stage
   float *ep = reinterpret_cast<float *>(smem) + wave * 32 * EP;
   const int fr = lane & 15, fq = lane >> 4;
   const int e0 = pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b_scale_inv);
   const int e1 = GATED ? pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b2_scale_inv) : e0;
+  const bool whole = at.m0 + BM <= g.m && at.n0 + BNO <= g.n;
   static_for<TM / 32>([&](auto block) {
     constexpr int i = decltype(block)::value;
+    if constexpr (GATED) {
+      // Whole tiles finish in the accumulators' own layout, where a lane holds
+      // the gates and the ups of the same outputs, and only what is stored goes
+      // through LDS, in its own few bytes.
+      if (whole) {
+        const int64_t row = at.m0 + wm * TM + i * 32, col = at.n0 + wn * (TN / 2);
+        uint8_t *ls = reinterpret_cast<uint8_t *>(ep);
+        v4f gate[2][J / 2], up[2][J / 2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < J / 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              gate[h][j][e] = __builtin_ldexpf(acc[2 * i + h][2 * j][e], e0);
+              up[h][j][e] = __builtin_ldexpf(acc[2 * i + h][2 * j + 1][e], e1);
+            }
+        if (g.z.kind == kSavedI8) {
+          save_block_i8<J / 2>(ls, lane, static_cast<uint8_t *>(g.z.data) + row * g.z.ld + col, g.z.ld,
+                               g.z.exps + row * g.z.ld_exps + col / kSaveGroup, g.z.ld_exps, gate);
+          save_block_i8<J / 2>(ls, lane, static_cast<uint8_t *>(g.u.data) + row * g.u.ld + col, g.u.ld,
+                               g.u.exps + row * g.u.ld_exps + col / kSaveGroup, g.u.ld_exps, up);
+        } else if (g.z.kind == kSavedBF16) {
+          store_block_bf16<J / 2>(ls, lane, static_cast<uint16_t *>(g.z.data) + row * g.z.ld + col, g.z.ld, gate);
+          store_block_bf16<J / 2>(ls, lane, static_cast<uint16_t *>(g.u.data) + row * g.u.ld + col, g.u.ld, up);
+        }
+        act_switch(g.act, [&](auto act) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < J / 2; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) gate[h][j][e] = act_value<decltype(act)::value>(gate[h][j][e]) * up[h][j][e];
+        });
+        if (g.c_bf16) {
+          store_block_bf16<J / 2>(ls, lane, static_cast<uint16_t *>(g.c) + row * g.ldc + col, g.ldc, gate);
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < J / 2; ++j)
+              *reinterpret_cast<f32x4_at4 *>(static_cast<float *>(g.c) + (row + 16 * h + fr) * g.ldc + col + 16 * j + 4 * fq) =
+                  gate[h][j];
+        }
+        return;
+      }
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -280,7 +394,7 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void act_r
     ob[c] = uint32_t(min(int64_t(b_row<GATED>(row)), g.n - 1 - at.n0) * g.ldb) + ((lane & 7) ^ row_swizzle(row)) * 16;
   }
   v4f acc[I][J];
-  ring_k_loop<FA, FB, BM, BN, S>(g.a + at.m0 * g.lda, b_base<GATED>(g, at.n0), oa, ob, int(g.k), smem, acc);
+  ring_k_loop<FA, FB, BM, BN, S>(uniform(g.a + at.m0 * g.lda), b_base<GATED>(g, at.n0), oa, ob, int(g.k), smem, acc);
 
   float *ep = reinterpret_cast<float *>(smem);
   const int fr = lane & 15, fq = lane >> 4;

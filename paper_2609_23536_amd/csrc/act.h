@@ -103,7 +103,8 @@ __device__ __forceinline__ void act_switch(int act, F &&f) {
 // (a code has seven bits), scaling exact, and the byte count at 33/32.
 constexpr int kSaveGroup = 32;
 
-__device__ __forceinline__ uint32_t save_exponent(uint32_t amax) {
+__device__ __forceinline__ uint32_t save_exponent(float group_max) {
+  const uint32_t amax = abs_bits(group_max);
   const int e = int((amax + 0x1ffffu) >> 23) - 6;
   return amax >= 0x7f800000u ? 255u : uint32_t(e < 1 ? 1 : e);
 }
@@ -133,32 +134,28 @@ __device__ __forceinline__ f32x4 restore4(uint32_t codes, uint32_t byte) {
              restore_code<3>(w, step, off)};
 }
 
+// Maxima that keep a NaN (one instruction for three operands on gfx950).
+__device__ __forceinline__ float nan_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float amax4(f32x4 x) {
+  return nan_max(nan_max(__builtin_fabsf(x[0]), __builtin_fabsf(x[1])), nan_max(__builtin_fabsf(x[2]), __builtin_fabsf(x[3])));
+}
+
 // Maximum over the 4 (8) lanes of an aligned group of lanes, in all of them.
-__device__ __forceinline__ uint32_t max_lanes4(uint32_t v) {
-  uint32_t o = uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0xb1, 0xf, 0xf, true));  // lane ^ 1
-  v = o > v ? o : v;
-  o = uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x4e, 0xf, 0xf, true));  // lane ^ 2
-  return o > v ? o : v;
+template <int CTRL>
+__device__ __forceinline__ float max_dpp(float v) {
+  return nan_max(v, __uint_as_float(uint32_t(__builtin_amdgcn_mov_dpp(int(__float_as_uint(v)), CTRL, 0xf, 0xf, true))));
 }
-__device__ __forceinline__ uint32_t max_lanes8(uint32_t v) {
-  v = max_lanes4(v);
-  const uint32_t o = uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x141, 0xf, 0xf, true));  // 7 - lane within eight
-  return o > v ? o : v;
-}
+__device__ __forceinline__ float max_lanes4(float v) { return max_dpp<0x4e>(max_dpp<0xb1>(v)); }  // lane ^ 1, lane ^ 2
+__device__ __forceinline__ float max_lanes8(float v) { return max_dpp<0x141>(max_lanes4(v)); }     // 7 - lane within eight
 
 // The same over lanes l, l ^ 16, l ^ 32 and l ^ 48: each exchange leaves one half's
 // values in the first result and the other half's in the second, in all lanes.
-__device__ __forceinline__ uint32_t max_lanes_by16(uint32_t v) {
-  auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = r[0] > r[1] ? r[0] : r[1];
-  r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return r[0] > r[1] ? r[0] : r[1];
-}
-
-__device__ __forceinline__ uint32_t amax4(f32x4 x) {
-  const uint32_t a = abs_bits(x[0]), b = abs_bits(x[1]), c = abs_bits(x[2]), d = abs_bits(x[3]);
-  const uint32_t e = a > b ? a : b, f = c > d ? c : d;
-  return e > f ? e : f;
+__device__ __forceinline__ float max_lanes_by16(float v) {
+  uint32_t b = __float_as_uint(v);
+  auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  b = __float_as_uint(nan_max(__uint_as_float(r[0]), __uint_as_float(r[1])));
+  r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return nan_max(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 }  // namespace

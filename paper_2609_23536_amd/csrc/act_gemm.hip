@@ -217,8 +217,7 @@ __device__ __forceinline__ void save_block_i8(uint8_t *ls, int lane, uint8_t *ds
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int q = 0; q < QUADS; q += 2) {
-      const uint32_t a = amax4(v[h][q]), b = amax4(v[h][q + 1]);
-      const uint32_t byte = save_exponent(max_lanes_by16(a > b ? a : b));
+      const uint32_t byte = save_exponent(max_lanes_by16(nan_max(amax4(v[h][q]), amax4(v[h][q + 1]))));
       bytes[h][0] |= byte << (4 * q);
       uint8_t *at = ls + (16 * h + (lane & 15)) * PITCH + 16 * q + 4 * (lane >> 4);
       *reinterpret_cast<uint32_t *>(at) = save_codes(v[h][q], byte);

@@ -23,63 +23,96 @@
 namespace qe {
 namespace {
 
+typedef unsigned int u32x4_f32 __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x4_in __attribute__((ext_vector_type(4), aligned(4)));
+
+// Eight values of a row as they are stored, zero where they do not exist.
+template <bool BF16>
+struct RawEight {
+  u32x4_in w[BF16 ? 1 : 2];
+};
+// Eight saved values: BF16, or codes and the byte of their group.
+template <int KIND>
+struct RawSaved {
+  RawEight<true> v;
+};
+template <>
+struct RawSaved<kSavedI8> {
+  u32x2_out w;
+  uint32_t byte;
+};
 
 struct Eight {
   float v[8];
 };
 
-// Values at .. at + 7 of a row, of which nv exist (the others read as zero).
-__device__ __forceinline__ Eight load_bf16(const void *base, int64_t at, int nv) {
-  Eight r;
-  const uint16_t *p = static_cast<const uint16_t *>(base) + at;
-  if (nv == 8) {
-    const u32x4_in w = *reinterpret_cast<const u32x4_in *>(p);
+// Elements at .. at + 7; nv of them exist.  Loads are non-temporal: nothing here is read twice.
+template <bool BF16, bool FULL>
+__device__ __forceinline__ RawEight<BF16> load_raw(const void *base, int64_t at, int nv) {
+  RawEight<BF16> r;
+  if (FULL || nv == 8) {
+    const char *p = static_cast<const char *>(base) + at * (BF16 ? 2 : 4);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      r.v[2 * e] = __uint_as_float(w[e] << 16);
-      r.v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    for (int i = 0; i < (BF16 ? 1 : 2); ++i) {
+      if constexpr (BF16)
+        r.w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_in *>(p + 16 * i));
+      else
+        r.w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_f32 *>(p + 16 * i));
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r.v[e] = e < nv ? bf16_to_f32(p[e]) : 0.0f;
-  }
-  return r;
-}
-__device__ __forceinline__ Eight load_f32(const void *base, int64_t at, int nv) {
-  Eight r;
-  const float *p = static_cast<const float *>(base) + at;
-  if (nv == 8) {
-    const f32x4_in a = *reinterpret_cast<const f32x4_in *>(p), b = *reinterpret_cast<const f32x4_in *>(p + 4);
+    for (int i = 0; i < (BF16 ? 1 : 2); ++i) r.w[i] = u32x4_in{0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      r.v[e] = a[e];
-      r.v[4 + e] = b[e];
+    for (int e = 0; e < 8; ++e) {
+      if (e >= nv) continue;
+      if constexpr (BF16)
+        r.w[0][e / 2] |= uint32_t(static_cast<const uint16_t *>(base)[at + e]) << (16 * (e % 2));
+      else
+        r.w[e / 4][e % 4] = static_cast<const uint32_t *>(base)[at + e];
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r.v[e] = e < nv ? p[e] : 0.0f;
   }
   return r;
 }
-// Eight columns from `col` of row `row`, restored.
-template <int KIND>
-__device__ __forceinline__ Eight load_saved(const SavedRef &s, int64_t row, int64_t col, int nv) {
+template <bool BF16>
+__device__ __forceinline__ Eight unpack(const RawEight<BF16> &r) {
+  Eight x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (BF16) {
+      x.v[2 * e] = __uint_as_float(r.w[0][e] << 16);
+      x.v[2 * e + 1] = __uint_as_float(r.w[0][e] & 0xffff0000u);
+    } else {
+      x.v[e] = __uint_as_float(r.w[0][e]);
+      x.v[4 + e] = __uint_as_float(r.w[1][e]);
+    }
+  }
+  return x;
+}
+template <int KIND, bool FULL>
+__device__ __forceinline__ RawSaved<KIND> load_saved(const SavedRef &s, int64_t row, int64_t col, int nv) {
+  RawSaved<KIND> r;
   if constexpr (KIND == kSavedBF16) {
-    return load_bf16(s.data, row * s.ld + col, nv);
+    r.v = load_raw<true, FULL>(s.data, row * s.ld + col, nv);
   } else {
     const uint8_t *p = static_cast<const uint8_t *>(s.data) + row * s.ld + col;
-    u32x2_out w = {0u, 0u};
-    uint32_t byte = 0u;
-    if (nv == 8) {
-      w = *reinterpret_cast<const u32x2_out *>(p);
+    r.byte = FULL || nv > 0 ? s.exps[row * s.ld_exps + col / kSaveGroup] : 0u;
+    if (FULL || nv == 8) {
+      r.w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_out *>(p));
     } else {
+      r.w = u32x2_out{0u, 0u};
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (e < nv) w[e / 4] |= uint32_t(p[e]) << (8 * (e % 4));
+        if (e < nv) r.w[e / 4] |= uint32_t(p[e]) << (8 * (e % 4));
     }
-    if (nv > 0) byte = s.exps[row * s.ld_exps + col / kSaveGroup];
-    const f32x4 a = restore4(w[0], byte), b = restore4(w[1], byte);
+  }
+  return r;
+}
+template <int KIND>
+__device__ __forceinline__ Eight restore(const RawSaved<KIND> &r) {
+  if constexpr (KIND == kSavedBF16) {
+    return unpack(r.v);
+  } else {
+    const f32x4 a = restore4(r.w[0], r.byte), b = restore4(r.w[1], r.byte);
     return Eight{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
   }
 }
@@ -90,7 +123,6 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(ActGradParams p, int
   constexpr int STEPS = ROWS / 16;
   constexpr int RPL = ROWS / 8;  // rows per lane when transposing
   __shared__ __attribute__((aligned(16))) uint8_t tile[OUTS][ROWS * kTile];
-  __shared__ uint32_t red[kThreads / 64];
   static_assert(sizeof(tile) >= 16 * kTile * sizeof(float), "the column sums' staging fits in the tile");
   const int tid = threadIdx.x;
   const int64_t rt = int64_t(blockIdx.x) / tiles_c;
@@ -101,140 +133,173 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(ActGradParams p, int
   const bool codes = p.scale != nullptr;
   const float scale = codes ? *p.scale : 0.0f;
   if (blockIdx.x == 0 && tid == 0 && codes && p.snapshot != nullptr) *p.snapshot = *p.scale_inv;
-  uint32_t amax = 0;
+  float amax = 0.0f;
   float sums[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
-#pragma unroll 2
-  for (int st = 0; st < STEPS; ++st) {
-    const int row_l = st * 16 + rl;
-    const int64_t row = r0 + row_l;
-    const int nv = row < p.rows ? nc : 0;
-    Eight dd, z, u;
-    dd = BF16 ? load_bf16(p.dd, row * p.ld_dd + col, nv) : load_f32(p.dd, row * p.ld_dd + col, nv);
-    z = load_saved<KIND>(p.z, row, col, nv);
-    if constexpr (GATED) u = load_saved<KIND>(p.u, row, col, nv);
-    Eight d[OUTS];
-    act_switch(p.act, [&](auto act) {
+  // Steps go in groups whose loads are all in flight together; FULL: every
+  // element of the tile exists.
+  auto run = [&](auto act, auto full) {
+    constexpr bool FULL = decltype(full)::value;
+    constexpr int G = FULL ? (STEPS < 4 ? STEPS : 4) : 2;
+#pragma unroll 1
+    for (int s0 = 0; s0 < STEPS; s0 += G) {
+      RawEight<BF16> dd_raw[G];
+      RawSaved<KIND> z_raw[G], u_raw[GATED ? G : 1];
+      int nvs[G];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float v, slope;
-        act_both<decltype(act)::value>(z.v[e], v, slope);
-        if constexpr (GATED) {
-          d[0].v[e] = dd.v[e] * u.v[e] * slope;
-          d[1].v[e] = dd.v[e] * v;
-        } else {
-          d[0].v[e] = dd.v[e] * slope;
+      for (int q = 0; q < G; ++q) {
+        const int64_t row = r0 + (s0 + q) * 16 + rl;
+        nvs[q] = FULL ? 8 : (row < p.rows ? nc : 0);
+        dd_raw[q] = load_raw<BF16, FULL>(p.dd, row * p.ld_dd + col, nvs[q]);
+        z_raw[q] = load_saved<KIND, FULL>(p.z, row, col, nvs[q]);
+        if constexpr (GATED) u_raw[q] = load_saved<KIND, FULL>(p.u, row, col, nvs[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < G; ++q) {
+        const int row_l = (s0 + q) * 16 + rl;
+        const int64_t row = r0 + row_l;
+        const int nv = nvs[q];
+        const Eight dd = unpack(dd_raw[q]), z = restore(z_raw[q]);
+        Eight u, d[OUTS];
+        if constexpr (GATED) u = restore(u_raw[q]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float v, slope;
+          act_both<decltype(act)::value>(z.v[e], v, slope);
+          if constexpr (GATED) {
+            d[0].v[e] = dd.v[e] * u.v[e] * slope;
+            d[1].v[e] = dd.v[e] * v;
+          } else {
+            d[0].v[e] = dd.v[e] * slope;
+          }
+        }
+        if (!FULL && nv < 8) {  // a NaN in a group's exponent reaches the columns past the last one
+#pragma unroll
+          for (int o = 0; o < OUTS; ++o)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[o].v[e] = e < nv ? d[o].v[e] : 0.0f;
+        }
+#pragma unroll
+        for (int o = 0; o < OUTS; ++o) {
+          const int64_t oc = col + (o == 0 ? 0 : p.cols);
+          const float *v = d[o].v;
+          float most = nan_max(amax4(f32x4{v[0], v[1], v[2], v[3]}), amax4(f32x4{v[4], v[5], v[6], v[7]}));
+          amax = nan_max(amax, most);
+          if constexpr (!GATED) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sums[e] += v[e];
+          }
+          if (codes) {
+            uint32_t w0, w1;
+            if (__builtin_expect(most * scale <= (FMT == 0 ? 448.0f : 57344.0f), 1)) {
+              w0 = enc4_in_range<FMT>(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
+              w1 = enc4_in_range<FMT>(v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale);
+            } else {  // a value to saturate, or a NaN
+              w0 = enc4<FMT>(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
+              w1 = enc4<FMT>(v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                w0 = nan_fix(w0, e, v[e]);
+                w1 = nan_fix(w1, e, v[4 + e]);
+              }
+            }
+            *reinterpret_cast<uint2 *>(tile[o] + lds_chunk_offset<RPL>(row_l, cl >> 4) + (cl & 15)) = make_uint2(w0, w1);
+            if (p.q_row != nullptr) {
+              uint8_t *dst = p.q_row + row * p.ld_row + oc;
+              if (FULL || nv == 8) {
+                *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w0, w1};
+              } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  if (e < nv) dst[e] = uint8_t(byte_of(e < 4 ? w0 : w1, e % 4));
+              }
+            }
+          }
+          if (p.dz == nullptr) continue;
+          if (p.dz_bf16) {
+            uint16_t *dst = static_cast<uint16_t *>(p.dz) + row * p.ld_dz + oc;
+            u32x4_in w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = bf16x2_bits(d[o].v[2 * e], d[o].v[2 * e + 1]);
+            if (FULL || nv == 8) {
+              *reinterpret_cast<u32x4_in *>(dst) = w;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (e < nv) dst[e] = uint16_t(w[e / 2] >> (16 * (e % 2)));
+            }
+          } else {
+            float *dst = static_cast<float *>(p.dz) + row * p.ld_dz + oc;
+            if (FULL || nv == 8) {
+              *reinterpret_cast<f32x4_in *>(dst) = f32x4_in{d[o].v[0], d[o].v[1], d[o].v[2], d[o].v[3]};
+              *reinterpret_cast<f32x4_in *>(dst + 4) = f32x4_in{d[o].v[4], d[o].v[5], d[o].v[6], d[o].v[7]};
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (e < nv) dst[e] = d[o].v[e];
+            }
+          }
         }
       }
-    });
-    if (nv < 8) {  // a NaN in a group's exponent reaches the columns past the last one
-#pragma unroll
-      for (int o = 0; o < OUTS; ++o)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[o].v[e] = e < nv ? d[o].v[e] : 0.0f;
     }
+  };
+  const bool full = r0 + ROWS <= p.rows && c0 + kTile <= p.cols;
+  act_switch(p.act, [&](auto act) {
+    if (full)
+      run(act, std::true_type{});
+    else
+      run(act, std::false_type{});
+  });
+
+  const uint32_t wave_max = update_wave_max(abs_bits(amax));
+  if (codes && p.q_col != nullptr) {
+    __syncthreads();  // the tile's codes are in LDS
+    const int rb = tid & 7, cq = tid >> 3;
+    const int64_t n = p.rows - (r0 + rb * RPL);  // rows of this lane's block that exist (or more)
 #pragma unroll
     for (int o = 0; o < OUTS; ++o) {
-      const int64_t oc = col + (o == 0 ? 0 : p.cols);
-      uint32_t most = 0;
+      uint32_t w[4][RPL / 4];  // [column][four rows]
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t b = abs_bits(d[o].v[e]);
-        most = b > most ? b : most;
-        if (!GATED) sums[e] += d[o].v[e];
+      for (int q = 0; q < RPL / 4; ++q) {
+        uint32_t d[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          d[i] = *reinterpret_cast<const uint32_t *>(tile[o] + lds_chunk_offset<RPL>(rb * RPL + 4 * q + i, cq >> 2) + ((cq & 3) << 2));
+        // 4 x 4 bytes transposed: pairs of rows, then pairs of pairs
+        const uint32_t a = __builtin_amdgcn_perm(d[1], d[0], 0x05010400u), b = __builtin_amdgcn_perm(d[3], d[2], 0x05010400u);
+        const uint32_t c = __builtin_amdgcn_perm(d[1], d[0], 0x07030602u), f = __builtin_amdgcn_perm(d[3], d[2], 0x07030602u);
+        w[0][q] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+        w[1][q] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        w[2][q] = __builtin_amdgcn_perm(f, c, 0x05040100u);
+        w[3][q] = __builtin_amdgcn_perm(f, c, 0x07060302u);
       }
-      amax = most > amax ? most : amax;
-      if (codes) {
-        const float *v = d[o].v;
-        uint32_t w0 = enc4<FMT>(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
-        uint32_t w1 = enc4<FMT>(v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale);
-        if (__builtin_expect(most > 0x7f800000u, 0)) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            w0 = nan_fix(w0, e, v[e]);
-            w1 = nan_fix(w1, e, v[4 + e]);
-          }
-        }
-        *reinterpret_cast<uint2 *>(tile[o] + lds_chunk_offset<RPL>(row_l, cl >> 4) + (cl & 15)) = make_uint2(w0, w1);
-        if (p.q_row != nullptr) {
-          uint8_t *dst = p.q_row + row * p.ld_row + oc;
-          if (nv == 8) {
-            *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w0, w1};
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (e < nv) dst[e] = uint8_t(byte_of(e < 4 ? w0 : w1, e % 4));
-          }
-        }
-      }
-      if (p.dz != nullptr) {
-        if (p.dz_bf16) {
-          uint16_t *dst = static_cast<uint16_t *>(p.dz) + row * p.ld_dz + oc;
-          u32x4_in w;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = bf16x2_bits(d[o].v[2 * e], d[o].v[2 * e + 1]);
-          if (nv == 8) {
-            *reinterpret_cast<u32x4_in *>(dst) = w;
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (e < nv) dst[e] = uint16_t(w[e / 2] >> (16 * (e % 2)));
-          }
+      for (int j = 0; j < 4; ++j) {
+        const int64_t c = c0 + 4 * cq + j;
+        if (c >= p.cols || n <= 0) continue;
+        uint8_t *dst = p.q_col + (c + (o == 0 ? 0 : p.cols)) * p.ld_col + r0 + rb * RPL;
+        if (n >= RPL) {
+          if constexpr (RPL == 16)
+            *reinterpret_cast<u32x4_out *>(dst) = u32x4_out{w[j][0], w[j][1], w[j][2], w[j][3]};
+          else
+            *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w[j][0], w[j][1]};
         } else {
-          float *dst = static_cast<float *>(p.dz) + row * p.ld_dz + oc;
-          if (nv == 8) {
-            *reinterpret_cast<f32x4_in *>(dst) = f32x4_in{d[o].v[0], d[o].v[1], d[o].v[2], d[o].v[3]};
-            *reinterpret_cast<f32x4_in *>(dst + 4) = f32x4_in{d[o].v[4], d[o].v[5], d[o].v[6], d[o].v[7]};
-          } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (e < nv) dst[e] = d[o].v[e];
-          }
+          for (int e = 0; e < RPL; ++e)
+            if (e < n) dst[e] = uint8_t(byte_of(w[j][e / 4], e % 4));
         }
       }
     }
   }
-
   if (codes) {
-    amax = update_wave_max(amax);
-    if ((tid & 63) == 0) red[tid >> 6] = amax;
-    __syncthreads();  // also: the tile's codes are in LDS
+    __syncthreads();  // the tile has been read: its first words take the waves' maxima
+    uint32_t *red = reinterpret_cast<uint32_t *>(tile[0]);
+    if ((tid & 63) == 0) red[tid >> 6] = wave_max;
+    __syncthreads();
     if (tid == 0) {
       uint32_t a = red[0];
       for (int w = 1; w < kThreads / 64; ++w) a = red[w] > a ? red[w] : a;
       fold_amax(p.amax_accum, p.amax_slot, a);
-    }
-    if (p.q_col != nullptr) {
-      const int rb = tid & 7, cq = tid >> 3;
-      const int64_t n = p.rows - (r0 + rb * RPL);  // rows of this lane's block that exist (or more)
-#pragma unroll
-      for (int o = 0; o < OUTS; ++o) {
-        uint32_t d[RPL];
-#pragma unroll
-        for (int i = 0; i < RPL; ++i)
-          d[i] = *reinterpret_cast<const uint32_t *>(tile[o] + lds_chunk_offset<RPL>(rb * RPL + i, cq >> 2) + ((cq & 3) << 2));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int64_t c = c0 + 4 * cq + j;
-          if (c >= p.cols || n <= 0) continue;
-          uint32_t w[RPL / 4];
-#pragma unroll
-          for (int q = 0; q < RPL / 4; ++q)
-            w[q] = byte_of(d[4 * q], j) | (byte_of(d[4 * q + 1], j) << 8) | (byte_of(d[4 * q + 2], j) << 16) |
-                   (byte_of(d[4 * q + 3], j) << 24);
-          uint8_t *dst = p.q_col + (c + (o == 0 ? 0 : p.cols)) * p.ld_col + r0 + rb * RPL;
-          if (n >= RPL) {
-            if constexpr (RPL == 16)
-              *reinterpret_cast<u32x4_out *>(dst) = u32x4_out{w[0], w[1], w[2], w[3]};
-            else
-              *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w[0], w[1]};
-          } else {
-#pragma unroll
-            for (int e = 0; e < RPL; ++e)
-              if (e < n) dst[e] = uint8_t(byte_of(w[e / 4], e % 4));
-          }
-        }
-      }
     }
   }
 
@@ -253,14 +318,24 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(ActGradParams p, int
   }
 }
 
-// dbias[c] (=, or +=) the sum over row tiles of partials[t][c], in order.
+// dbias[c] (=, or +=) the sum over row tiles of partials[t][c]: 64 columns a
+// workgroup, four lanes a column, each every fourth tile, then those four; always
+// in that order.
 __global__ __launch_bounds__(kThreads) void bias_grad_kernel(const float *partials, float *dbias, int64_t tiles, int64_t cols,
                                                              int accumulate) {
-  const int64_t c = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  if (c >= cols) return;
+  __shared__ float part[kThreads];
+  const int64_t c = int64_t(blockIdx.x) * 64 + (threadIdx.x & 63);
   float a = 0.0f;
-  for (int64_t t = 0; t < tiles; ++t) a += partials[t * cols + c];
-  dbias[c] = accumulate ? dbias[c] + a : a;
+  if (c < cols) {
+#pragma unroll 4
+    for (int64_t t = threadIdx.x >> 6; t < tiles; t += 4) a += partials[t * cols + c];
+  }
+  part[threadIdx.x] = a;
+  __syncthreads();
+  if (threadIdx.x < 64 && c < cols) {
+    a = (part[threadIdx.x] + part[64 + threadIdx.x]) + (part[128 + threadIdx.x] + part[192 + threadIdx.x]);
+    dbias[c] = accumulate ? dbias[c] + a : a;
+  }
 }
 
 template <bool GATED, bool BF16, int KIND, int FMT>
@@ -295,7 +370,7 @@ hipError_t launch_act_grad(const ActGradParams &p, float *dbias, bool accumulate
     if (e != hipSuccess) return e;
   }
   if (dbias == nullptr || p.cols <= 0) return hipSuccess;
-  const int64_t tiles = (p.rows + rows - 1) / rows, blocks = (p.cols + kThreads - 1) / kThreads;
+  const int64_t tiles = (p.rows + rows - 1) / rows, blocks = (p.cols + 63) / 64;
   if (blocks >= int64_t(1) << 31) return hipErrorInvalidValue;
   return klaunch(bias_grad_kernel, dim3(unsigned(blocks)), dim3(kThreads), 0, s, p.partials, dbias, tiles, p.cols,
                  accumulate ? 1 : 0);

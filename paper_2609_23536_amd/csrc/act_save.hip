@@ -48,8 +48,7 @@ __global__ __launch_bounds__(kThreads) void act_save_kernel(SaveParams p, int64_
           if (e < nv) (e < 4 ? a : b)[e % 4] = src[e];
       }
     }
-    const uint32_t ma = amax4(a), mb = amax4(b);
-    const uint32_t byte = save_exponent(max_lanes4(ma > mb ? ma : mb));
+    const uint32_t byte = save_exponent(max_lanes4(nan_max(amax4(a), amax4(b))));
     const uint32_t w0 = save_codes(a, byte), w1 = save_codes(b, byte);
     uint8_t *dst = static_cast<uint8_t *>(p.saved.data) + row * p.saved.ld + col;
     if (nv == 8) {

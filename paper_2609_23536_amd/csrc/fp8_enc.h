@@ -39,6 +39,20 @@ __device__ __forceinline__ uint32_t enc4(float a, float b, float c, float d) {
   return uint32_t(r);
 }
 
+// The same for values that are known to be within +-fmax.
+template <int FMT>
+__device__ __forceinline__ uint32_t enc4_in_range(float a, float b, float c, float d) {
+  int r;
+  if constexpr (FMT == 0) {
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+  } else {
+    r = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, 0, false);
+    r = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, r, true);
+  }
+  return uint32_t(r);
+}
+
 // NaN -> 0x7F with the input's sign bit, for the rare thread that saw one.
 __device__ __forceinline__ uint32_t nan_fix(uint32_t u, int byte, float v) {
   if (v != v) {

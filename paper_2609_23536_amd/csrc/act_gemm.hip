@@ -33,7 +33,8 @@ typedef unsigned int u32x4_at16 __attribute__((ext_vector_type(4)));
 typedef float f32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned int u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
 
-// Four values from row-major storage of either type; nv of them exist.
+// Four values from row-major storage of either type; nv of them exist.  (Where
+// some do not, the last one is read again: no load waits for another.)
 __device__ __forceinline__ v4f load_quad(const void *base, bool bf16, int64_t at, int nv) {
   v4f r = {0.f, 0.f, 0.f, 0.f};
   if (bf16) {
@@ -42,20 +43,15 @@ __device__ __forceinline__ v4f load_quad(const void *base, bool bf16, int64_t at
       const u32x2_at2 w = *reinterpret_cast<const u32x2_at2 *>(p);
       r = v4f{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
               __uint_as_float(w.y & 0xffff0000u)};
-    } else {
-#pragma unroll
-      for (int e = 0; e < 3; ++e)
-        if (e < nv) r[e] = bf16_to_f32(p[e]);
+    } else if (nv > 0) {
+      r = v4f{bf16_to_f32(p[0]), bf16_to_f32(p[nv > 1 ? 1 : 0]), bf16_to_f32(p[nv - 1]), 0.f};
     }
   } else {
     const float *p = static_cast<const float *>(base) + at;
-    if (nv == 4) {
+    if (nv == 4)
       r = *reinterpret_cast<const f32x4_at4 *>(p);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 3; ++e)
-        if (e < nv) r[e] = p[e];
-    }
+    else if (nv > 0)
+      r = v4f{p[0], p[nv > 1 ? 1 : 0], p[nv - 1], 0.f};
   }
   return r;
 }

@@ -62,13 +62,21 @@ __device__ __forceinline__ RawEight<BF16> load_raw(const void *base, int64_t at,
   } else {
 #pragma unroll
     for (int i = 0; i < (BF16 ? 1 : 2); ++i) r.w[i] = u32x4_in{0u, 0u, 0u, 0u};
+    if (nv > 0) {  // single elements, the last one again past it: no load waits for another
+      uint32_t x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (e >= nv) continue;
-      if constexpr (BF16)
-        r.w[0][e / 2] |= uint32_t(static_cast<const uint16_t *>(base)[at + e]) << (16 * (e % 2));
-      else
-        r.w[e / 4][e % 4] = static_cast<const uint32_t *>(base)[at + e];
+      for (int e = 0; e < 8; ++e) {
+        const int64_t i = at + (e < nv ? e : nv - 1);
+        x[e] = BF16 ? uint32_t(static_cast<const uint16_t *>(base)[i]) : static_cast<const uint32_t *>(base)[i];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t v = e < nv ? x[e] : 0u;
+        if constexpr (BF16)
+          r.w[0][e / 2] |= v << (16 * (e % 2));
+        else
+          r.w[e / 4][e % 4] = v;
+      }
     }
   }
   return r;
@@ -100,9 +108,13 @@ __device__ __forceinline__ RawSaved<KIND> load_saved(const SavedRef &s, int64_t 
       r.w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_out *>(p));
     } else {
       r.w = u32x2_out{0u, 0u};
+      if (nv > 0) {
+        uint32_t x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < nv) r.w[e / 4] |= uint32_t(p[e]) << (8 * (e % 4));
+        for (int e = 0; e < 8; ++e) x[e] = p[e < nv ? e : nv - 1];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.w[e / 4] |= (e < nv ? x[e] : 0u) << (8 * (e % 4));
+      }
     }
   }
   return r;
@@ -117,21 +129,35 @@ __device__ __forceinline__ Eight restore(const RawSaved<KIND> &r) {
   }
 }
 
-template <bool GATED, bool BF16, int KIND, int FMT, int ROWS>
-__global__ __launch_bounds__(kThreads) void act_grad_kernel(ActGradParams p, int64_t tiles_c) {
+// Row tiles whose columns the workgroups in flight share: rows and transposed
+// rows are usually a multiple of 4 KB apart, so that tiles side by side in one
+// row tile write all their transposed codes to a few memory channels.  8192 x
+// 28672 gated, MI355X: 1 446 us, 8 451, 16 453, 32 397, 64 408; 2048 x 14336 (16
+// row tiles) 55 with 1, 53 with all.
+constexpr int kGroupRows = 32;
+
+template <bool GATED, bool BF16, int KIND, int ROWS, int THREADS>
+__global__ __launch_bounds__(THREADS) void act_grad_kernel(ActGradParams p, int tiles_r, int tiles_c, int nt) {
   constexpr int OUTS = GATED ? 2 : 1;
-  constexpr int STEPS = ROWS / 16;
-  constexpr int RPL = ROWS / 8;  // rows per lane when transposing
+  constexpr int RS = THREADS / 16;          // rows per step
+  constexpr int STEPS = ROWS / RS;
+  constexpr int RPL = ROWS / 8;             // rows and columns per lane when transposing
+  constexpr int CPL = kTile * 8 / THREADS;
   __shared__ __attribute__((aligned(16))) uint8_t tile[OUTS][ROWS * kTile];
-  static_assert(sizeof(tile) >= 16 * kTile * sizeof(float), "the column sums' staging fits in the tile");
+  static_assert(sizeof(tile) >= RS / 2 * kTile * sizeof(float), "the column sums' staging fits in the tile");
   const int tid = threadIdx.x;
-  const int64_t rt = int64_t(blockIdx.x) / tiles_c;
-  const int64_t r0 = rt * ROWS, c0 = int64_t(blockIdx.x) % tiles_c * kTile;
+  // Tiles go down groups of kGroupRows row tiles, column after column.
+  const int in_group = kGroupRows * tiles_c, group = int(blockIdx.x) / in_group, first = group * kGroupRows;
+  const int height = min(tiles_r - first, kGroupRows), at = int(blockIdx.x) - group * in_group;
+  const int rt = first + at % height;
+  const int64_t r0 = int64_t(rt) * ROWS, c0 = int64_t(at / height) * kTile;
   const int rl = tid >> 4, cl = (tid & 15) * 8;
   const int64_t col = c0 + cl;
   const int nc = int(p.cols - col < 0 ? 0 : (p.cols - col > 8 ? 8 : p.cols - col));
   const bool codes = p.scale != nullptr;
   const float scale = codes ? *p.scale : 0.0f;
+  const bool e4m3 = p.fmt == 0;  // uniform
+  const float fmax = e4m3 ? 448.0f : 57344.0f;
   if (blockIdx.x == 0 && tid == 0 && codes && p.snapshot != nullptr) *p.snapshot = *p.scale_inv;
   float amax = 0.0f;
   float sums[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -148,7 +174,7 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(ActGradParams p, int
       int nvs[G];
 #pragma unroll
       for (int q = 0; q < G; ++q) {
-        const int64_t row = r0 + (s0 + q) * 16 + rl;
+        const int64_t row = r0 + (s0 + q) * RS + rl;
         nvs[q] = FULL ? 8 : (row < p.rows ? nc : 0);
         dd_raw[q] = load_raw<BF16, FULL>(p.dd, row * p.ld_dd + col, nvs[q]);
         z_raw[q] = load_saved<KIND, FULL>(p.z, row, col, nvs[q]);
@@ -156,7 +182,7 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(ActGradParams p, int
       }
 #pragma unroll
       for (int q = 0; q < G; ++q) {
-        const int row_l = (s0 + q) * 16 + rl;
+        const int row_l = (s0 + q) * RS + rl;
         const int64_t row = r0 + row_l;
         const int nv = nvs[q];
         const Eight dd = unpack(dd_raw[q]), z = restore(z_raw[q]);
@@ -190,13 +216,15 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(ActGradParams p, int
             for (int e = 0; e < 8; ++e) sums[e] += v[e];
           }
           if (codes) {
+            const float s8[8] = {v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale,
+                                 v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale};
             uint32_t w0, w1;
-            if (__builtin_expect(most * scale <= (FMT == 0 ? 448.0f : 57344.0f), 1)) {
-              w0 = enc4_in_range<FMT>(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
-              w1 = enc4_in_range<FMT>(v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale);
+            if (__builtin_expect(most * scale <= fmax, 1)) {
+              w0 = e4m3 ? enc4_in_range<0>(s8[0], s8[1], s8[2], s8[3]) : enc4_in_range<1>(s8[0], s8[1], s8[2], s8[3]);
+              w1 = e4m3 ? enc4_in_range<0>(s8[4], s8[5], s8[6], s8[7]) : enc4_in_range<1>(s8[4], s8[5], s8[6], s8[7]);
             } else {  // a value to saturate, or a NaN
-              w0 = enc4<FMT>(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
-              w1 = enc4<FMT>(v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale);
+              w0 = e4m3 ? enc4<0>(s8[0], s8[1], s8[2], s8[3]) : enc4<1>(s8[0], s8[1], s8[2], s8[3]);
+              w1 = e4m3 ? enc4<0>(s8[4], s8[5], s8[6], s8[7]) : enc4<1>(s8[4], s8[5], s8[6], s8[7]);
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 w0 = nan_fix(w0, e, v[e]);
@@ -207,7 +235,10 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(ActGradParams p, int
             if (p.q_row != nullptr) {
               uint8_t *dst = p.q_row + row * p.ld_row + oc;
               if (FULL || nv == 8) {
-                *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w0, w1};
+                if (nt)
+                  __builtin_nontemporal_store(u32x2_out{w0, w1}, reinterpret_cast<u32x2_out *>(dst));
+                else
+                  *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w0, w1};
               } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -258,31 +289,42 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(ActGradParams p, int
     const int64_t n = p.rows - (r0 + rb * RPL);  // rows of this lane's block that exist (or more)
 #pragma unroll
     for (int o = 0; o < OUTS; ++o) {
-      uint32_t w[4][RPL / 4];  // [column][four rows]
+      uint32_t w[CPL][RPL / 4];  // [column][four rows]
 #pragma unroll
       for (int q = 0; q < RPL / 4; ++q) {
         uint32_t d[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          d[i] = *reinterpret_cast<const uint32_t *>(tile[o] + lds_chunk_offset<RPL>(rb * RPL + 4 * q + i, cq >> 2) + ((cq & 3) << 2));
-        // 4 x 4 bytes transposed: pairs of rows, then pairs of pairs
+        for (int i = 0; i < 4; ++i) {
+          const uint8_t *at = tile[o] + lds_chunk_offset<RPL>(rb * RPL + 4 * q + i, cq * CPL >> 4) + (cq * CPL & 15);
+          if constexpr (CPL == 4)
+            d[i] = *reinterpret_cast<const uint32_t *>(at);
+          else
+            d[i] = *reinterpret_cast<const uint16_t *>(at);
+        }
+        // 4 x 4 (4 x 2) bytes transposed: pairs of rows, then pairs of pairs
         const uint32_t a = __builtin_amdgcn_perm(d[1], d[0], 0x05010400u), b = __builtin_amdgcn_perm(d[3], d[2], 0x05010400u);
-        const uint32_t c = __builtin_amdgcn_perm(d[1], d[0], 0x07030602u), f = __builtin_amdgcn_perm(d[3], d[2], 0x07030602u);
         w[0][q] = __builtin_amdgcn_perm(b, a, 0x05040100u);
         w[1][q] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-        w[2][q] = __builtin_amdgcn_perm(f, c, 0x05040100u);
-        w[3][q] = __builtin_amdgcn_perm(f, c, 0x07060302u);
+        if constexpr (CPL == 4) {
+          const uint32_t c = __builtin_amdgcn_perm(d[1], d[0], 0x07030602u), f = __builtin_amdgcn_perm(d[3], d[2], 0x07030602u);
+          w[2][q] = __builtin_amdgcn_perm(f, c, 0x05040100u);
+          w[3][q] = __builtin_amdgcn_perm(f, c, 0x07060302u);
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t c = c0 + 4 * cq + j;
+      for (int j = 0; j < CPL; ++j) {
+        const int64_t c = c0 + CPL * cq + j;
         if (c >= p.cols || n <= 0) continue;
         uint8_t *dst = p.q_col + (c + (o == 0 ? 0 : p.cols)) * p.ld_col + r0 + rb * RPL;
         if (n >= RPL) {
-          if constexpr (RPL == 16)
-            *reinterpret_cast<u32x4_out *>(dst) = u32x4_out{w[j][0], w[j][1], w[j][2], w[j][3]};
-          else
+          if constexpr (RPL == 16) {
+            if (nt)
+              __builtin_nontemporal_store(u32x4_out{w[j][0], w[j][1], w[j][2], w[j][3]}, reinterpret_cast<u32x4_out *>(dst));
+            else
+              *reinterpret_cast<u32x4_out *>(dst) = u32x4_out{w[j][0], w[j][1], w[j][2], w[j][3]};
+          } else {
             *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w[j][0], w[j][1]};
+          }
         } else {
 #pragma unroll
           for (int e = 0; e < RPL; ++e)
@@ -298,22 +340,29 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(ActGradParams p, int
     __syncthreads();
     if (tid == 0) {
       uint32_t a = red[0];
-      for (int w = 1; w < kThreads / 64; ++w) a = red[w] > a ? red[w] : a;
+      for (int w = 1; w < THREADS / 64; ++w) a = red[w] > a ? red[w] : a;
       fold_amax(p.amax_accum, p.amax_slot, a);
     }
   }
 
   if (!GATED && p.partials != nullptr && p.rows > 0) {
     __syncthreads();  // the tile has been read
-    float *col_sums = reinterpret_cast<float *>(tile[0]);  // [16 row lanes][128 columns]
+    float *col_sums = reinterpret_cast<float *>(tile[0]);  // [half the row lanes][128 columns]
+    if (rl < RS / 2) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) col_sums[rl * kTile + cl + e] = sums[e];
+      for (int e = 0; e < 8; ++e) col_sums[rl * kTile + cl + e] = sums[e];
+    }
+    __syncthreads();
+    if (rl >= RS / 2) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) col_sums[(rl - RS / 2) * kTile + cl + e] += sums[e];
+    }
     __syncthreads();
     if (tid < kTile && c0 + tid < p.cols) {
       float a = 0.0f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) a += col_sums[r * kTile + tid];
-      p.partials[rt * p.cols + c0 + tid] = a;
+      for (int r = 0; r < RS / 2; ++r) a += col_sums[r * kTile + tid];
+      p.partials[int64_t(rt) * p.cols + c0 + tid] = a;
     }
   }
 }
@@ -338,27 +387,25 @@ __global__ __launch_bounds__(kThreads) void bias_grad_kernel(const float *partia
   }
 }
 
-template <bool GATED, bool BF16, int KIND, int FMT>
+template <bool GATED, bool BF16, int KIND>
 hipError_t launch_rows(int rows_per_tile, const ActGradParams &p, hipStream_t s) {
   const bool empty = p.rows == 0 || p.cols == 0;  // one workgroup then writes the snapshot
+  const int64_t tiles_r = empty ? 1 : (p.rows + rows_per_tile - 1) / rows_per_tile;
   const int64_t tiles_c = empty ? 1 : (p.cols + kTile - 1) / kTile;
-  const int64_t tiles = empty ? 1 : (p.rows + rows_per_tile - 1) / rows_per_tile * tiles_c;
-  if (tiles >= int64_t(1) << 31) return hipErrorInvalidValue;
-  const dim3 grid{unsigned(tiles)}, block(kThreads);
-  return rows_per_tile == 64 ? klaunch(act_grad_kernel<GATED, BF16, KIND, FMT, 64>, grid, block, 0, s, p, tiles_c)
-                             : klaunch(act_grad_kernel<GATED, BF16, KIND, FMT, 128>, grid, block, 0, s, p, tiles_c);
-}
-
-template <bool GATED, bool BF16, int KIND>
-hipError_t launch_fmt(int rows, const ActGradParams &p, hipStream_t s) {
-  return p.fmt == 0 ? launch_rows<GATED, BF16, KIND, 0>(rows, p, s) : launch_rows<GATED, BF16, KIND, 1>(rows, p, s);
+  if (tiles_r * tiles_c >= int64_t(1) << 31) return hipErrorInvalidValue;
+  // Codes that the 256 MB memory-side cache cannot keep until they are read are
+  // stored non-temporally (8192 x 28672 gated, MI355X: 397 us without, 385 so).
+  const int nt = p.rows * p.cols * (GATED ? 4 : 2) > (int64_t(256) << 20);
+  const dim3 grid{unsigned(tiles_r * tiles_c)};
+  return rows_per_tile == 64 ? klaunch(act_grad_kernel<GATED, BF16, KIND, 64, 512>, grid, dim3(512), 0, s, p, int(tiles_r), int(tiles_c), nt)
+                             : klaunch(act_grad_kernel<GATED, BF16, KIND, 128, 256>, grid, dim3(256), 0, s, p, int(tiles_r), int(tiles_c), nt);
 }
 
 template <bool GATED>
 hipError_t launch_kind(int rows, const ActGradParams &p, hipStream_t s) {
   if (p.z.kind == kSavedBF16)
-    return p.dd_bf16 ? launch_fmt<GATED, true, kSavedBF16>(rows, p, s) : launch_fmt<GATED, false, kSavedBF16>(rows, p, s);
-  return p.dd_bf16 ? launch_fmt<GATED, true, kSavedI8>(rows, p, s) : launch_fmt<GATED, false, kSavedI8>(rows, p, s);
+    return p.dd_bf16 ? launch_rows<GATED, true, kSavedBF16>(rows, p, s) : launch_rows<GATED, false, kSavedBF16>(rows, p, s);
+  return p.dd_bf16 ? launch_rows<GATED, true, kSavedI8>(rows, p, s) : launch_rows<GATED, false, kSavedI8>(rows, p, s);
 }
 
 }  // namespace

@@ -32,20 +32,24 @@ __global__ __launch_bounds__(kThreads) void act_save_kernel(SaveParams p, int64_
                   __uint_as_float(w[1] & 0xffff0000u)};
         b = f32x4{__uint_as_float(w[2] << 16), __uint_as_float(w[2] & 0xffff0000u), __uint_as_float(w[3] << 16),
                   __uint_as_float(w[3] & 0xffff0000u)};
-      } else {
+      } else if (nv > 0) {  // single elements, the last one again past it: no load waits for another
+        uint32_t x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < nv) (e < 4 ? a : b)[e % 4] = bf16_to_f32(src[e]);
+        for (int e = 0; e < 8; ++e) x[e] = src[e < nv ? e : nv - 1];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) (e < 4 ? a : b)[e % 4] = e < nv ? bf16_to_f32(x[e]) : 0.0f;
       }
     } else {
       const float *src = static_cast<const float *>(p.x) + row * p.ld + col;
       if (nv == 8) {
         a = *reinterpret_cast<const f32x4_in *>(src);
         b = *reinterpret_cast<const f32x4_in *>(src + 4);
-      } else {
+      } else if (nv > 0) {
+        float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < nv) (e < 4 ? a : b)[e % 4] = src[e];
+        for (int e = 0; e < 8; ++e) x[e] = src[e < nv ? e : nv - 1];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) (e < 4 ? a : b)[e % 4] = e < nv ? x[e] : 0.0f;
       }
     }
     const uint32_t byte = save_exponent(max_lanes4(nan_max(amax4(a), amax4(b))));
@@ -78,9 +82,11 @@ __global__ __launch_bounds__(kThreads) void act_restore_kernel(SaveParams p, int
     if (nv == 8) {
       w = *reinterpret_cast<const u32x2_out *>(src);
     } else {
+      uint32_t x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < nv) w[e / 4] |= uint32_t(src[e]) << (8 * (e % 4));
+      for (int e = 0; e < 8; ++e) x[e] = src[e < nv ? e : nv - 1];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e / 4] |= (e < nv ? x[e] : 0u) << (8 * (e % 4));
     }
     const uint32_t byte = p.saved.exps[row * p.saved.ld_exps + col / kSaveGroup];
     const f32x4 a = restore4(w[0], byte), b = restore4(w[1], byte);

@@ -114,7 +114,8 @@ __device__ __forceinline__ void finish_some(const ActGemmParams &g, const float 
   constexpr int RS = LANES / LPR;          // rows per step
   constexpr int STEPS = ROWS / RS;
   constexpr int Q = STEPS < 8 ? STEPS : 8;  // steps whose loads are in flight together
-  static_assert(OW % 32 == 0 && LANES % LPR == 0 && ROWS % RS == 0 && STEPS % Q == 0, "whole steps");
+  // (OW = 16, half a saved group, only where nothing is saved in 8 bits)
+  static_assert(OW % 16 == 0 && LANES % LPR == 0 && ROWS % RS == 0 && STEPS % Q == 0, "whole steps");
   const int rl = t / LPR, cl = (t % LPR) * 4;
   const int64_t col = col0 + cl;
   const int nv = FULL ? 4 : int(g.n - col < 0 ? 0 : (g.n - col > 4 ? 4 : g.n - col));
@@ -415,8 +416,123 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void act_r
   }
 }
 
+// Up to 16 rows (a token or a few being served): every operand row of B is read once
+// and by one workgroup, so the product is bound by streaming B from memory, and
+// what a tile kernel does for reuse (LDS stages, barriers) only costs latency.
+// A workgroup takes 16 OB outputs; its W waves split the reduction, K tile t to
+// wave t % W.  A wave loads its fragments straight into registers, U K tiles
+// in flight (lane l: row l % 16, bytes 16 (l / 16) of either half of the 128,
+// the same for both operands), and the waves' sums meet in LDS, added in order.
+template <bool GATED, int FA, int FB, int OB, int W>
+__global__ __launch_bounds__(64 * W) void act_rows_kernel(ActGemmParams g) {
+  constexpr int NB = GATED ? 2 * OB : OB;  // 16-row blocks of B
+  constexpr int U = 4;                     // K tiles in flight
+  constexpr int EP = 16 * NB + 4;
+  __shared__ __attribute__((aligned(16))) float sums[W][16 * EP];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int fr = lane & 15, fq = lane >> 4;
+  const int64_t n0 = int64_t(blockIdx.x) * (16 * OB);
+  const int T = int((g.k + BK - 1) / BK), ktail = int(g.k % BK);
+
+  const uint8_t *pa = g.a + min(int64_t(fr), g.m - 1) * g.lda, *pb[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {  // gated: gates and ups in alternating blocks
+    const int64_t row = min(n0 + 16 * (GATED ? j / 2 : j) + fr, g.n - 1);
+    pb[j] = (GATED && j % 2 == 1 ? g.b2 : g.b) + row * g.ldb;
+  }
+  v4f acc[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) acc[j] = v4f{0.f, 0.f, 0.f, 0.f};
+
+  // The lane's 32 bytes of K tile t.
+  auto load = [&](const uint8_t *p, int t) -> v8i {
+    int c0 = fq, c1 = 4 + fq;
+    if (ktail != 0 && t == T - 1) {  // chunks past the row's last 16 bytes re-read it; masked below
+      const int last = (ktail - 1) >> 4;
+      c0 = min(c0, last);
+      c1 = min(c1, last);
+    }
+    const uint4 lo = *reinterpret_cast<const uint4 *>(p + int64_t(t) * BK + 16 * c0);
+    const uint4 hi = *reinterpret_cast<const uint4 *>(p + int64_t(t) * BK + 16 * c1);
+    return v8i{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
+  };
+  auto masked = [&](v8i f) -> v8i {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int nb = ktail - (q < 4 ? 16 * fq : 64 + 16 * fq) - 4 * (q % 4);  // bytes of this word to keep
+      f[q] &= int(uint32_t((uint64_t(1) << (8 * (nb <= 0 ? 0 : (nb >= 4 ? 4 : nb)))) - 1u));
+    }
+    return f;
+  };
+  for (int t0 = wave; t0 < T; t0 += U * W) {
+    v8i fa[U], fb[U][NB];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = min(t0 + u * W, T - 1);  // past the end: the last tile again, not used
+#pragma unroll
+      for (int j = 0; j < NB; ++j) fb[u][j] = load(pb[j], t);
+      fa[u] = load(pa, t);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * W;
+      if (t >= T) break;
+      if (ktail != 0 && t == T - 1) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) fb[u][j] = masked(fb[u][j]);
+        fa[u] = masked(fa[u]);
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+        acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u][j], fa[u], acc[j], FB, FA, 0, 0, 0, 0);
+    }
+  }
+  const int e0 = pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b_scale_inv);
+  const int e1 = GATED ? pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b2_scale_inv) : e0;
+#pragma unroll
+  for (int j = 0; j < NB; ++j) *reinterpret_cast<v4f *>(sums[wave] + fr * EP + 16 * j + 4 * fq) = acc[j];
+  __syncthreads();
+  // sums of the waves, scaled, into the first one's place
+  for (int q = threadIdx.x; q < 16 * 4 * NB; q += 64 * W) {
+    const int row = q / (4 * NB), col = q % (4 * NB) * 4;
+    v4f s = *reinterpret_cast<const v4f *>(sums[0] + row * EP + col);
+#pragma unroll
+    for (int w = 1; w < W; ++w) s += *reinterpret_cast<const v4f *>(sums[w] + row * EP + col);
+    const int e = (col / 16) % 2 == 0 ? e0 : e1;
+    *reinterpret_cast<v4f *>(sums[0] + row * EP + col) =
+        v4f{__builtin_ldexpf(s[0], e), __builtin_ldexpf(s[1], e), __builtin_ldexpf(s[2], e), __builtin_ldexpf(s[3], e)};
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) finish_rows<GATED, 16, 16 * OB, 64, EP>(g, sums[0], lane, 0, n0);
+}
+
+constexpr int64_t kFewRows = 16;
+constexpr int kFewRowsTile = 0;  // in place of a GemmTile
+
+// One workgroup for 16 outputs (32 where they are saved in 8 bits, whose groups
+// have 32 columns).  Eight waves keep the most bytes in flight, but up to 16 K
+// tiles four waves have them all in flight in one go and start sooner.  MI355X,
+// one row, us with 4 / 8 waves: 7936 x 739 (6 K tiles, 7 rows) 4.8 / 5.7, gated
+// 2730 x 1365 (11) 4.1 / 5.2, 4096 x 4096 (32) 7.7 / 6.0, gated 14336 x 4096 28.5 /
+// 24.9, 8192 x 28672 45.1 / 41.9.
+// With the small tiles (64 x 64 and 64 x 128) these take, us: 4096 x 14336 21.8 ->
+// 13.6, gated 14336 x 4096 30.5 -> 24.6, 8192 x 28672 66 -> 42 (5.6 TB/s), gated
+// 28672 x 8192 87 -> 79 (5.9 TB/s); with 16 rows 21.3 -> 17.7 and 30.8 -> 28.4; with 32
+// rows in two row blocks a wave 21.8 -> 23.6 and 30.8 -> 38.0, so not there.
+template <bool GATED, int FA, int FB>
+hipError_t launch_few_rows(const ActGemmParams &p, hipStream_t s) {
+  const bool wide = p.z.kind == kSavedI8, few = p.k <= 16 * BK;
+  const dim3 grid(unsigned((p.n + (wide ? 31 : 15)) / (wide ? 32 : 16)));
+  if (wide)
+    return few ? klaunch(act_rows_kernel<GATED, FA, FB, 2, 4>, grid, dim3(256), 0, s, p)
+               : klaunch(act_rows_kernel<GATED, FA, FB, 2, 8>, grid, dim3(512), 0, s, p);
+  return few ? klaunch(act_rows_kernel<GATED, FA, FB, 1, 4>, grid, dim3(256), 0, s, p)
+             : klaunch(act_rows_kernel<GATED, FA, FB, 1, 8>, grid, dim3(512), 0, s, p);
+}
+
 template <bool GATED, int FA, int FB>
 hipError_t launch_tile(int tile, const ActGemmParams &p, hipStream_t s) {
+  if (tile == kFewRowsTile) return launch_few_rows<GATED, FA, FB>(p, s);
   const dim3 block(256);
   int tm = 0, tn = 0;
   auto grid = [&](int bm, int bn) {
@@ -469,6 +585,8 @@ hipError_t launch_act_gemm(const ActGemmParams &p, hipStream_t s) {
                                1u << kTile128x64Deep | 1u << kTile64x128 | 1u << kTile64x128Deep | 1u << kTile128x128 |
                                1u << kTile128x128Deep;
   const int force = gemm_tile_override();
+  if (force == kTileAuto && p.m <= kFewRows)
+    return gated ? launch_fmts<true>(kFewRowsTile, p, s) : launch_fmts<false>(kFewRowsTile, p, s);
   const int tile = force == kTileAuto ? choose_gemm_tile(g, kShapes) : (force == kTile192x256 ? kTile192x256 : kTile256x256);
   return gated ? launch_fmts<true>(tile, p, s) : launch_fmts<false>(tile, p, s);
 }

@@ -180,10 +180,22 @@ def ptr(x) -> int:
     return int(x.data_ptr())
 
 
+_current_stream = None  # () -> handle of torch's current stream
+
+
+def _bind_current_stream():
+    """The first use initialises CUDA and binds torch's raw accessors: 0.3 us a call instead of 7 for a Stream object."""
+    global _current_stream
+    import torch
+    torch.cuda.current_stream()
+    raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    _current_stream = lambda: raw(device())  # noqa: E731
+    return _current_stream()
+
+
 def stream_handle(s) -> int:
     if s is None:
-        import torch
-        return int(torch.cuda.current_stream().cuda_stream)
+        return _current_stream() if _current_stream is not None else _bind_current_stream()
     if isinstance(s, int):
         return s
     return int(s.cuda_stream)

@@ -17,10 +17,11 @@
 // nor the outputs have a size limit past a tile's: a row stride below 2^23
 // bytes (256 rows of it are 2^31).
 //
-// Epilogue: accumulators go through LDS (as in the plain GEMM) and come back row
-// by row, four columns a lane; the eight lanes of a 32-column group share its
-// maximum by lane permutes.  Large tiles do this per wave (32 rows at a time),
-// small ones per workgroup (64 rows at a time).
+// Epilogue.  Large tiles finish in the accumulators' own layout, one wave's block
+// of rows at a time (see act_large_kernel).  Small tiles' accumulators go through
+// LDS, 64 rows of the workgroup at a time, and come back row by row, four
+// columns a lane, the eight lanes of a 32-column group sharing its maximum by
+// lane permutes.
 #include "act.h"
 #include "gemm_loops.h"
 
@@ -182,59 +183,125 @@ __device__ __forceinline__ void static_for(F &&f) {
   }
 }
 
-// Stores a wave's [32, 4 OWQ] BF16 block, of which the lane holds quad q of row
-// 16 h + (lane & 15), columns 16 q' + 4 (lane >> 4) .., through `ls`: the lanes
-// then write whole row runs, 16 bytes each.  LDS operations of one wave
-// complete in order.
-template <int QUADS>
-__device__ __forceinline__ void store_block_bf16(uint8_t *ls, int lane, uint16_t *dst, int64_t ld, const v4f (&v)[2][QUADS]) {
-  constexpr int RUN = 32 * QUADS, PITCH = RUN + 16, LPR = RUN / 16, RS = 64 / LPR;  // bytes of a row, lanes a row, rows a step
+// A wave's block of 16 NR rows x 16 QUADS columns, of which the lane holds quad q
+// of rows 16 h + (lane & 15): columns 16 q + 4 (lane >> 4) ..  It goes through
+// LDS, so that the lanes then write whole row runs, 16 bytes each (LDS operations
+// of one wave complete in order).  Rows of RUN bytes, PITCH apart in LDS.
+template <int QUADS, int ES>
+struct Rows {
+  static constexpr int RUN = 16 * QUADS * ES, PITCH = RUN + 16, LPR = RUN / 16, RS = 64 / LPR;  // lanes a row, rows a step
+};
+
+template <int QUADS, int NR, bool BF16>
+__device__ __forceinline__ void stage_block(uint8_t *ls, int lane, const v4f (&v)[NR][QUADS]) {
+  using L = Rows<QUADS, BF16 ? 2 : 4>;
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < NR; ++h)
 #pragma unroll
-    for (int q = 0; q < QUADS; ++q)
-      *reinterpret_cast<uint2 *>(ls + (16 * h + (lane & 15)) * PITCH + 32 * q + 8 * (lane >> 4)) =
-          make_uint2(bf16x2_bits(v[h][q][0], v[h][q][1]), bf16x2_bits(v[h][q][2], v[h][q][3]));
-  uint16_t *out = dst + (lane / LPR) * ld + (lane % LPR) * 8;
-#pragma unroll
-  for (int s = 0; s < 32 / RS; ++s)
-    __builtin_nontemporal_store(*reinterpret_cast<const u32x4_at16 *>(ls + (s * RS + lane / LPR) * PITCH + (lane % LPR) * 16),
-                                reinterpret_cast<u32x4_in *>(out + s * RS * ld));
+    for (int q = 0; q < QUADS; ++q) {
+      uint8_t *at = ls + (16 * h + (lane & 15)) * L::PITCH + (16 * q + 4 * (lane >> 4)) * (BF16 ? 2 : 4);
+      if constexpr (BF16)
+        *reinterpret_cast<uint2 *>(at) = make_uint2(bf16x2_bits(v[h][q][0], v[h][q][1]), bf16x2_bits(v[h][q][2], v[h][q][3]));
+      else
+        *reinterpret_cast<v4f *>(at) = v[h][q];
+    }
 }
 
-// The same for an 8-bit checkpoint: codes of whole 32-column groups (two quads
-// of four lanes), and their exponent bytes.
-template <int QUADS>
-__device__ __forceinline__ void save_block_i8(uint8_t *ls, int lane, uint8_t *dst, int64_t ld, uint8_t *exps, int64_t ld_exps,
-                                              const v4f (&v)[2][QUADS]) {
-  constexpr int RUN = 16 * QUADS, PITCH = RUN + 16, LPR = RUN / 16, RS = 64 / LPR;
-  static_assert(QUADS % 2 == 0 && QUADS <= 8, "whole groups, their bytes in a word");
-  uint32_t bytes[2][(QUADS + 7) / 8] = {};
+// Codes of an 8-bit checkpoint (a group is two quads of four lanes), and the exponent
+// bytes straight to memory, from lanes 0 .. 15 of each block row.
+template <bool EDGE, int QUADS, int NR>
+__device__ __forceinline__ void stage_codes(uint8_t *ls, int lane, uint8_t *exps, int64_t ld_exps, int rows, int cols,
+                                            const v4f (&v)[NR][QUADS]) {
+  using L = Rows<QUADS, 1>;
+  static_assert(QUADS == 4 || QUADS == 8, "whole groups, their bytes in a word");
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < NR; ++h) {
+    uint32_t bytes = 0u;
 #pragma unroll
     for (int q = 0; q < QUADS; q += 2) {
       const uint32_t byte = save_exponent(max_lanes_by16(nan_max(amax4(v[h][q]), amax4(v[h][q + 1]))));
-      bytes[h][0] |= byte << (4 * q);
-      uint8_t *at = ls + (16 * h + (lane & 15)) * PITCH + 16 * q + 4 * (lane >> 4);
+      bytes |= byte << (4 * q);
+      uint8_t *at = ls + (16 * h + (lane & 15)) * L::PITCH + 16 * q + 4 * (lane >> 4);
       *reinterpret_cast<uint32_t *>(at) = save_codes(v[h][q], byte);
       *reinterpret_cast<uint32_t *>(at + 16) = save_codes(v[h][q + 1], byte);
     }
-  uint8_t *out = dst + (lane / LPR) * ld + (lane % LPR) * 16;
+    if (lane < 16 && (!EDGE || 16 * h + lane < rows)) {
+      uint8_t *at = exps + (16 * h + lane) * ld_exps;
+      if (EDGE && cols < 16 * QUADS) {
 #pragma unroll
-  for (int s = 0; s < 32 / RS; ++s)
-    __builtin_nontemporal_store(*reinterpret_cast<const u32x4_at16 *>(ls + (s * RS + lane / LPR) * PITCH + (lane % LPR) * 16),
-                                reinterpret_cast<u32x4_out *>(out + s * RS * ld));
-  if (lane < 32) {  // lanes 0 .. 15 the first block row's bytes, 16 .. 31 the second's
-    uint8_t *e = exps + lane * ld_exps;
-    const uint32_t w = lane < 16 ? bytes[0][0] : bytes[1][0];
-    if constexpr (QUADS == 8)
-      *reinterpret_cast<u32_out *>(e) = w;
-    else if constexpr (QUADS == 4)
-      *reinterpret_cast<u16_at1 *>(e) = uint16_t(w);
-    else
-      *e = uint8_t(w);
+        for (int q = 0; q < QUADS / 2; ++q)
+          if (q * kSaveGroup < cols) at[q] = uint8_t(bytes >> (8 * q));
+      } else if constexpr (QUADS == 8) {
+        *reinterpret_cast<u32_out *>(at) = bytes;
+      } else {
+        *reinterpret_cast<u16_at1 *>(at) = uint16_t(bytes);
+      }
+    }
   }
+}
+
+// The staged block to memory: `base` is its first element, `pitch` in bytes.
+// EDGE: rows x cols of it exist.
+template <bool EDGE, int QUADS, int NR, int ES>
+__device__ __forceinline__ void store_staged(const uint8_t *ls, int lane, void *base, int64_t pitch, int rows, int cols) {
+  using L = Rows<QUADS, ES>;
+  char *out = static_cast<char *>(base) + (lane / L::LPR) * pitch + (lane % L::LPR) * 16;
+  const uint8_t *in = ls + (lane / L::LPR) * L::PITCH + (lane % L::LPR) * 16;
+#pragma unroll
+  for (int s = 0; s < 16 * NR / L::RS; ++s) {
+    const u32x4_at16 v = *reinterpret_cast<const u32x4_at16 *>(in + s * (L::RS * L::PITCH));
+    char *dst = out + s * L::RS * pitch;
+    if constexpr (EDGE) {
+      const int n = (cols - lane % L::LPR * (16 / ES)) * ES;  // bytes of the lane's sixteen that exist
+      if (s * L::RS + lane / L::LPR >= rows || n <= 0) continue;
+      if (n < 16) {
+#pragma unroll
+        for (int b = 0; b < 16; b += ES) {
+          if (b >= n) break;
+          if constexpr (ES == 1) dst[b] = char(v[b / 4] >> (8 * (b % 4)));
+          if constexpr (ES == 2) *reinterpret_cast<uint16_t *>(dst + b) = uint16_t(v[b / 4] >> (8 * (b % 4)));
+          if constexpr (ES == 4) *reinterpret_cast<uint32_t *>(dst + b) = v[b / 4];
+        }
+        continue;
+      }
+    }
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4_out *>(dst));
+  }
+}
+
+// A lane's residual quads of a block row, as stored: from element `at`, `cols`
+// of which exist.
+template <bool EDGE, int QUADS>
+struct Quads {
+  v4f raw[QUADS];  // BF16: the first two words
+  __device__ __forceinline__ void load(const void *base, bool bf16, int64_t at, int cols) {
+#pragma unroll
+    for (int j = 0; j < QUADS; ++j) {
+      if (EDGE && cols < 16 * j + 4) {  // not the whole quad
+        const v4f r = load_quad(base, bf16, at + 16 * j, max(cols - 16 * j, 0));
+        raw[j] = r;
+        if (bf16) {
+          raw[j][0] = __uint_as_float(bf16x2_bits(r[0], r[1]));
+          raw[j][1] = __uint_as_float(bf16x2_bits(r[2], r[3]));
+        }
+      } else if (bf16) {
+        const u32x2_at2 w = *reinterpret_cast<const u32x2_at2 *>(static_cast<const uint16_t *>(base) + at + 16 * j);
+        raw[j][0] = __uint_as_float(w.x);
+        raw[j][1] = __uint_as_float(w.y);
+      } else {
+        raw[j] = *reinterpret_cast<const f32x4_at4 *>(static_cast<const float *>(base) + at + 16 * j);
+      }
+    }
+  }
+  __device__ __forceinline__ v4f get(bool bf16, int j) const {
+    if (!bf16) return raw[j];
+    const uint32_t a = __float_as_uint(raw[j][0]), b = __float_as_uint(raw[j][1]);
+    return v4f{__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)};
+  }
+};
+
+__device__ __forceinline__ v4f ldexp4(v4f a, int e) {
+  return v4f{__builtin_ldexpf(a[0], e), __builtin_ldexpf(a[1], e), __builtin_ldexpf(a[2], e), __builtin_ldexpf(a[3], e)};
 }
 
 struct TilePlace {
@@ -275,11 +342,9 @@ __global__ __launch_bounds__(256) void act_large_kernel(ActGemmParams g, int til
   constexpr int I = TM / 16, J = TN / 16;
   constexpr int CHA = BM / 32, CHB = BN / 32;
   constexpr int STAGE = (BM + BN) * BK;
-  constexpr int EP = TN + 4;
-  static_assert(J % 2 == 0 && NW * 32 * EP * 4 <= 2 * STAGE, "block columns in pairs, staging within the stages");
+  static_assert(J % 2 == 0 && I % 2 == 0, "block columns and rows in pairs");
   __shared__ __attribute__((aligned(16))) uint8_t smem[2 * STAGE + NW * 1024];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = wave >> 1, wn = wave & 1;
   const TilePlace at = place(tiles_m, tiles_n, BM, BNO);
   uint32_t oa[CHA], ob[CHB];
 #pragma unroll
@@ -296,73 +361,120 @@ __global__ __launch_bounds__(256) void act_large_kernel(ActGemmParams g, int til
   large_k_loop<FA, FB, BM, BN>(uniform(g.a + at.m0 * g.lda), b_base<GATED>(g, at.n0), oa, ob, g.k, smem, acc);
 
   __syncthreads();  // every wave is done reading the last stage
-  float *ep = reinterpret_cast<float *>(smem) + wave * 32 * EP;
   const int fr = lane & 15, fq = lane >> 4;
   const int e0 = pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b_scale_inv);
   const int e1 = GATED ? pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b2_scale_inv) : e0;
-  const bool whole = at.m0 + BM <= g.m && at.n0 + BNO <= g.n;
-  static_for<TM / 32>([&](auto block) {
-    constexpr int i = decltype(block)::value;
-    if constexpr (GATED) {
-      // Whole tiles finish in the accumulators' own layout, where a lane holds
-      // the gates and the ups of the same outputs, and only what is stored goes
-      // through LDS, in its own few bytes.
-      if (whole) {
-        const int64_t row = at.m0 + wm * TM + i * 32, col = at.n0 + wn * (TN / 2);
-        uint8_t *ls = reinterpret_cast<uint8_t *>(ep);
-        v4f gate[2][J / 2], up[2][J / 2];
+  // A tile finishes in the accumulators' own layout, where a lane holds four
+  // neighbouring outputs of one row (and their gates beside their ups), a block
+  // of rows at a time; only what is stored goes through LDS.  The residual is
+  // read in that layout too (32-byte pieces of BF16 rows, four of which share a
+  // line while it is in the L1), before the block above it is stored: read row by
+  // row when due it cost 37 us a round of tiles on MI355X, against 16 in all
+  // without it.  (Bringing its lines into the L2 before the K loop: slower.)
+  // Gated tiles take two block rows at a time, one is 5% slower; plain ones one,
+  // two spill.
+  constexpr int QV = GATED ? J / 2 : J;  // quads a lane holds of an output row
+  constexpr int NR = GATED ? 2 : 1;      // block rows at a time
+  const int wu = __builtin_amdgcn_readfirstlane(wave);
+  const int64_t wrow = at.m0 + (wu >> 1) * TM, wcol = at.n0 + (wu & 1) * (16 * QV);
+  const int rows_left = int(min(int64_t(BM), g.m - wrow)), cols = int(min(int64_t(BN), g.n - wcol));  // of the wave's block, or more
+  if (rows_left <= 0 || cols <= 0) return;
+  uint8_t *ls = smem + wave * (STAGE / 2), *ls_u = ls + 16 * NR * Rows<QV, 2>::PITCH;
+  uint8_t *ls_c = GATED ? ls_u + 16 * NR * Rows<QV, 2>::PITCH : ls_u;  // D last: at most FP32
+  static_assert(16 * NR * ((GATED ? 2 : 1) * Rows<QV, 2>::PITCH + Rows<QV, 4>::PITCH) <= STAGE / 2, "the blocks staged fit");
+  const bool has_res = !GATED && g.residual != nullptr, res_bf16 = g.residual_bf16 != 0;
+  const bool i8 = g.z.kind == kSavedI8, kept = g.z.kind == kSavedBF16;
+  auto finish = [&](auto edge) {
+    constexpr bool EDGE = decltype(edge)::value;  // part of the wave's block does not exist
+    v4f bias[QV];
+    Quads<EDGE, QV> res;
+    auto load_res = [&](int i) {
+      const int64_t r = EDGE ? min(wrow + 16 * i + fr, g.m - 1) : wrow + 16 * i + fr;
+      res.load(g.residual, res_bf16, r * g.ld_residual + wcol + 4 * fq, cols - 4 * fq);
+    };
+    if (has_res) load_res(0);
+    if constexpr (!GATED) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int j = 0; j < J / 2; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              gate[h][j][e] = __builtin_ldexpf(acc[2 * i + h][2 * j][e], e0);
-              up[h][j][e] = __builtin_ldexpf(acc[2 * i + h][2 * j + 1][e], e1);
-            }
-        if (g.z.kind == kSavedI8) {
-          save_block_i8<J / 2>(ls, lane, static_cast<uint8_t *>(g.z.data) + row * g.z.ld + col, g.z.ld,
-                               g.z.exps + row * g.z.ld_exps + col / kSaveGroup, g.z.ld_exps, gate);
-          save_block_i8<J / 2>(ls, lane, static_cast<uint8_t *>(g.u.data) + row * g.u.ld + col, g.u.ld,
-                               g.u.exps + row * g.u.ld_exps + col / kSaveGroup, g.u.ld_exps, up);
-        } else if (g.z.kind == kSavedBF16) {
-          store_block_bf16<J / 2>(ls, lane, static_cast<uint16_t *>(g.z.data) + row * g.z.ld + col, g.z.ld, gate);
-          store_block_bf16<J / 2>(ls, lane, static_cast<uint16_t *>(g.u.data) + row * g.u.ld + col, g.u.ld, up);
-        }
-        act_switch(g.act, [&](auto act) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < J / 2; ++j)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) gate[h][j][e] = act_value<decltype(act)::value>(gate[h][j][e]) * up[h][j][e];
-        });
-        if (g.c_bf16) {
-          store_block_bf16<J / 2>(ls, lane, static_cast<uint16_t *>(g.c) + row * g.ldc + col, g.ldc, gate);
-        } else {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < J / 2; ++j)
-              *reinterpret_cast<f32x4_at4 *>(static_cast<float *>(g.c) + (row + 16 * h + fr) * g.ldc + col + 16 * j + 4 * fq) =
-                  gate[h][j];
-        }
-        return;
+      for (int j = 0; j < QV; ++j) {
+        bias[j] = v4f{0.f, 0.f, 0.f, 0.f};
+        const int nv = EDGE ? max(0, min(4, cols - 16 * j - 4 * fq)) : 4;
+        if (g.bias != nullptr) bias[j] = load_quad(g.bias, g.bias_bf16 != 0, wcol + 16 * j + 4 * fq, nv);
       }
     }
+    static_for<I / NR>([&](auto block) {
+      constexpr int i = decltype(block)::value * NR;
+      const int64_t row = wrow + i * 16;
+      const int rows = rows_left - i * 16;
+      if (EDGE && rows <= 0) return;
+      v4f z[NR][QV], up[NR][QV];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < NR; ++h)
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const v4f a = acc[2 * i + h][j];
-        const int e = j % 2 == 0 ? e0 : e1;
-        *reinterpret_cast<v4f *>(ep + (h * 16 + fr) * EP + j * 16 + 4 * fq) =
-            v4f{__builtin_ldexpf(a[0], e), __builtin_ldexpf(a[1], e), __builtin_ldexpf(a[2], e), __builtin_ldexpf(a[3], e)};
+        for (int j = 0; j < QV; ++j) {
+          if constexpr (GATED) {
+            z[h][j] = ldexp4(acc[i + h][2 * j], e0);
+            up[h][j] = ldexp4(acc[i + h][2 * j + 1], e1);
+          } else {
+            z[h][j] = ldexp4(acc[i + h][j], e0) + bias[j];
+          }
+          if constexpr (EDGE) {  // columns past the last one count as zero in their group
+            const int nv = cols - 16 * j - 4 * fq;
+            z[h][j] = v4f{nv > 0 ? z[h][j][0] : 0.f, nv > 1 ? z[h][j][1] : 0.f, nv > 2 ? z[h][j][2] : 0.f, nv > 3 ? z[h][j][3] : 0.f};
+            if constexpr (GATED)
+              up[h][j] = v4f{nv > 0 ? up[h][j][0] : 0.f, nv > 1 ? up[h][j][1] : 0.f, nv > 2 ? up[h][j][2] : 0.f, nv > 3 ? up[h][j][3] : 0.f};
+          }
+        }
+      if (i8) {
+        stage_codes<EDGE, QV, NR>(ls, lane, g.z.exps + row * g.z.ld_exps + wcol / kSaveGroup, g.z.ld_exps, rows, cols, z);
+        if constexpr (GATED)
+          stage_codes<EDGE, QV, NR>(ls_u, lane, g.u.exps + row * g.u.ld_exps + wcol / kSaveGroup, g.u.ld_exps, rows, cols, up);
+      } else if (kept) {
+        stage_block<QV, NR, true>(ls, lane, z);
+        if constexpr (GATED) stage_block<QV, NR, true>(ls_u, lane, up);
       }
-    // same wave writes then reads its own LDS rows: LDS operations of one wave complete in order
-    finish_rows<GATED, 32, GATED ? TN / 2 : TN, 64, EP>(g, ep, lane, at.m0 + wm * TM + i * 32,
-                                                        at.n0 + wn * (GATED ? TN / 2 : TN));
-  });
+      act_switch(g.act, [&](auto act) {
+#pragma unroll
+        for (int h = 0; h < NR; ++h)
+#pragma unroll
+          for (int j = 0; j < QV; ++j) {
+            v4f d = z[h][j];
+            if constexpr (GATED)
+              d = v4f{act_value<decltype(act)::value>(d[0]) * up[h][j][0], act_value<decltype(act)::value>(d[1]) * up[h][j][1],
+                      act_value<decltype(act)::value>(d[2]) * up[h][j][2], act_value<decltype(act)::value>(d[3]) * up[h][j][3]};
+            else
+              d = v4f{act_value<decltype(act)::value>(d[0]), act_value<decltype(act)::value>(d[1]),
+                      act_value<decltype(act)::value>(d[2]), act_value<decltype(act)::value>(d[3])};
+            z[h][j] = d;
+          }
+      });
+      if (has_res) {
+#pragma unroll
+        for (int j = 0; j < QV; ++j) z[0][j] += res.get(res_bf16, j);
+        if (i + 1 < I) load_res(i + 1);
+      }
+      // what was staged first has long been written when it is read back
+      if (i8) {
+        store_staged<EDGE, QV, NR, 1>(ls, lane, static_cast<uint8_t *>(g.z.data) + row * g.z.ld + wcol, g.z.ld, rows, cols);
+        if constexpr (GATED)
+          store_staged<EDGE, QV, NR, 1>(ls_u, lane, static_cast<uint8_t *>(g.u.data) + row * g.u.ld + wcol, g.u.ld, rows, cols);
+      } else if (kept) {
+        store_staged<EDGE, QV, NR, 2>(ls, lane, static_cast<uint16_t *>(g.z.data) + row * g.z.ld + wcol, g.z.ld * 2, rows, cols);
+        if constexpr (GATED)
+          store_staged<EDGE, QV, NR, 2>(ls_u, lane, static_cast<uint16_t *>(g.u.data) + row * g.u.ld + wcol, g.u.ld * 2, rows, cols);
+      }
+      if (g.c_bf16) {
+        stage_block<QV, NR, true>(ls_c, lane, z);
+        store_staged<EDGE, QV, NR, 2>(ls_c, lane, static_cast<uint16_t *>(g.c) + row * g.ldc + wcol, g.ldc * 2, rows, cols);
+      } else {
+        stage_block<QV, NR, false>(ls_c, lane, z);
+        store_staged<EDGE, QV, NR, 4>(ls_c, lane, static_cast<float *>(g.c) + row * g.ldc + wcol, g.ldc * 4, rows, cols);
+      }
+    });
+  };
+  if (rows_left >= TM && cols >= 16 * QV)
+    finish(std::false_type{});
+  else
+    finish(std::true_type{});
 }
 
 template <bool GATED, int FA, int FB, int BM, int BN, int S>

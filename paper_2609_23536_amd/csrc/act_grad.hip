@@ -129,6 +129,27 @@ __device__ __forceinline__ Eight restore(const RawSaved<KIND> &r) {
   }
 }
 
+// Code stores, non-temporal or not; between empty asm, or the compiler would merge
+// the two into one ordinary store.
+__device__ __forceinline__ void store_codes2(uint8_t *dst, u32x2_out v, int nt) {
+  if (nt) {
+    asm volatile("");
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x2_out *>(dst));
+    asm volatile("");
+  } else {
+    *reinterpret_cast<u32x2_out *>(dst) = v;
+  }
+}
+__device__ __forceinline__ void store_codes4(uint8_t *dst, u32x4_out v, int nt) {
+  if (nt) {
+    asm volatile("");
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4_out *>(dst));
+    asm volatile("");
+  } else {
+    *reinterpret_cast<u32x4_out *>(dst) = v;
+  }
+}
+
 // Row tiles whose columns the workgroups in flight share: rows and transposed
 // rows are usually a multiple of 4 KB apart, so that tiles side by side in one
 // row tile write all their transposed codes to a few memory channels.  8192 x
@@ -235,10 +256,7 @@ __global__ __launch_bounds__(THREADS) void act_grad_kernel(ActGradParams p, int 
             if (p.q_row != nullptr) {
               uint8_t *dst = p.q_row + row * p.ld_row + oc;
               if (FULL || nv == 8) {
-                if (nt)
-                  __builtin_nontemporal_store(u32x2_out{w0, w1}, reinterpret_cast<u32x2_out *>(dst));
-                else
-                  *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w0, w1};
+                store_codes2(dst, u32x2_out{w0, w1}, nt);
               } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -317,14 +335,10 @@ __global__ __launch_bounds__(THREADS) void act_grad_kernel(ActGradParams p, int 
         if (c >= p.cols || n <= 0) continue;
         uint8_t *dst = p.q_col + (c + (o == 0 ? 0 : p.cols)) * p.ld_col + r0 + rb * RPL;
         if (n >= RPL) {
-          if constexpr (RPL == 16) {
-            if (nt)
-              __builtin_nontemporal_store(u32x4_out{w[j][0], w[j][1], w[j][2], w[j][3]}, reinterpret_cast<u32x4_out *>(dst));
-            else
-              *reinterpret_cast<u32x4_out *>(dst) = u32x4_out{w[j][0], w[j][1], w[j][2], w[j][3]};
-          } else {
-            *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w[j][0], w[j][1]};
-          }
+          if constexpr (RPL == 16)
+            store_codes4(dst, u32x4_out{w[j][0], w[j][1], w[j][2], w[j][3]}, nt);
+          else
+            store_codes2(dst, u32x2_out{w[j][0], w[j][1]}, nt);
         } else {
 #pragma unroll
           for (int e = 0; e < RPL; ++e)

@@ -3,59 +3,72 @@
 //
 // HBM-bound: a save reads 2 or 4 bytes per value and writes 33/32, a restore the
 // other way round.  A workgroup takes 64 rows x 128 columns, a lane eight
-// columns of every sixteenth row: a group is four neighbouring lanes, which
-// share its maximum by lane permutes.
+// columns of every sixteenth row, all four loads in flight: a group is four
+// neighbouring lanes, which share its maximum by lane permutes.
 #include "act.h"
 
 namespace qe {
 namespace {
 
 typedef float f32x4_in __attribute__((ext_vector_type(4), aligned(4)));
-constexpr int kRows = 64;
+constexpr int kRows = 64, kSteps = kRows / 16;
 
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void act_save_kernel(SaveParams p, int64_t tiles_c) {
-  const int tid = threadIdx.x;
-  const int64_t r0 = int64_t(blockIdx.x) / tiles_c * kRows;
-  const int64_t col = int64_t(blockIdx.x) % tiles_c * kTile + (tid & 15) * 8;
-  const int nc = int(p.cols - col < 0 ? 0 : (p.cols - col > 8 ? 8 : p.cols - col));
-#pragma unroll
-  for (int st = 0; st < kRows / 16; ++st) {
-    const int64_t row = r0 + st * 16 + (tid >> 4);
-    const int nv = row < p.rows ? nc : 0;
-    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-    if constexpr (BF16) {
-      const uint16_t *src = static_cast<const uint16_t *>(p.x) + row * p.ld + col;
-      if (nv == 8) {
-        const u32x4_in w = *reinterpret_cast<const u32x4_in *>(src);
-        a = f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16),
+struct Eight {
+  f32x4 a, b;
+};
+
+// Eight values of a row at `at`, of which nv exist (all, if FULL; the others
+// read as zero).  Where some do not exist the last one is read again in their
+// place, so that no load waits for another.
+template <bool BF16, bool FULL>
+__device__ __forceinline__ Eight load8(const void *base, int64_t at, int nv) {
+  Eight r = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  if constexpr (BF16) {
+    const uint16_t *p = static_cast<const uint16_t *>(base) + at;
+    if (FULL || nv == 8) {
+      const u32x4_in w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_in *>(p));
+      r.a = f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16),
                   __uint_as_float(w[1] & 0xffff0000u)};
-        b = f32x4{__uint_as_float(w[2] << 16), __uint_as_float(w[2] & 0xffff0000u), __uint_as_float(w[3] << 16),
+      r.b = f32x4{__uint_as_float(w[2] << 16), __uint_as_float(w[2] & 0xffff0000u), __uint_as_float(w[3] << 16),
                   __uint_as_float(w[3] & 0xffff0000u)};
-      } else if (nv > 0) {  // single elements, the last one again past it: no load waits for another
-        uint32_t x[8];
+    } else if (nv > 0) {
+      float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = src[e < nv ? e : nv - 1];
+      for (int e = 0; e < 8; ++e) x[e] = bf16_to_f32(p[e < nv ? e : nv - 1]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) (e < 4 ? a : b)[e % 4] = e < nv ? bf16_to_f32(x[e]) : 0.0f;
-      }
-    } else {
-      const float *src = static_cast<const float *>(p.x) + row * p.ld + col;
-      if (nv == 8) {
-        a = *reinterpret_cast<const f32x4_in *>(src);
-        b = *reinterpret_cast<const f32x4_in *>(src + 4);
-      } else if (nv > 0) {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = src[e < nv ? e : nv - 1];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) (e < 4 ? a : b)[e % 4] = e < nv ? x[e] : 0.0f;
-      }
+      for (int e = 0; e < 8; ++e) (e < 4 ? r.a : r.b)[e % 4] = e < nv ? x[e] : 0.0f;
     }
-    const uint32_t byte = save_exponent(max_lanes4(nan_max(amax4(a), amax4(b))));
-    const uint32_t w0 = save_codes(a, byte), w1 = save_codes(b, byte);
+  } else {
+    const float *p = static_cast<const float *>(base) + at;
+    if (FULL || nv == 8) {
+      r.a = __builtin_nontemporal_load(reinterpret_cast<const f32x4_in *>(p));
+      r.b = __builtin_nontemporal_load(reinterpret_cast<const f32x4_in *>(p + 4));
+    } else if (nv > 0) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = p[e < nv ? e : nv - 1];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) (e < 4 ? r.a : r.b)[e % 4] = e < nv ? x[e] : 0.0f;
+    }
+  }
+  return r;
+}
+
+template <bool BF16, bool FULL>
+__device__ __forceinline__ void save_tile(const SaveParams &p, int64_t row0, int64_t col) {
+  const int nc = FULL ? 8 : int(p.cols - col < 0 ? 0 : (p.cols - col > 8 ? 8 : p.cols - col));
+  Eight x[kSteps];
+#pragma unroll
+  for (int st = 0; st < kSteps; ++st)
+    x[st] = load8<BF16, FULL>(p.x, (row0 + st * 16) * p.ld + col, FULL || row0 + st * 16 < p.rows ? nc : 0);
+#pragma unroll
+  for (int st = 0; st < kSteps; ++st) {
+    const int64_t row = row0 + st * 16;
+    const int nv = FULL || row < p.rows ? nc : 0;
+    const uint32_t byte = save_exponent(max_lanes4(nan_max(amax4(x[st].a), amax4(x[st].b))));
+    const uint32_t w0 = save_codes(x[st].a, byte), w1 = save_codes(x[st].b, byte);
     uint8_t *dst = static_cast<uint8_t *>(p.saved.data) + row * p.saved.ld + col;
-    if (nv == 8) {
+    if (FULL || nv == 8) {
       *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w0, w1};
     } else {
 #pragma unroll
@@ -66,34 +79,39 @@ __global__ __launch_bounds__(kThreads) void act_save_kernel(SaveParams p, int64_
   }
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void act_restore_kernel(SaveParams p, int64_t tiles_c) {
-  const int tid = threadIdx.x;
-  const int64_t r0 = int64_t(blockIdx.x) / tiles_c * kRows;
-  const int64_t col = int64_t(blockIdx.x) % tiles_c * kTile + (tid & 15) * 8;
-  const int nc = int(p.cols - col < 0 ? 0 : (p.cols - col > 8 ? 8 : p.cols - col));
+template <bool BF16, bool FULL>
+__device__ __forceinline__ void restore_tile(const SaveParams &p, int64_t row0, int64_t col) {
+  const int nc = FULL ? 8 : int(p.cols - col < 0 ? 0 : (p.cols - col > 8 ? 8 : p.cols - col));
+  u32x2_out w[kSteps];
+  uint32_t byte[kSteps];
 #pragma unroll
-  for (int st = 0; st < kRows / 16; ++st) {
-    const int64_t row = r0 + st * 16 + (tid >> 4);
-    const int nv = row < p.rows ? nc : 0;
+  for (int st = 0; st < kSteps; ++st) {
+    const int64_t row = row0 + st * 16;
+    const int nv = FULL || row < p.rows ? nc : 0;
+    w[st] = u32x2_out{0u, 0u};
+    byte[st] = 0u;
     if (nv == 0) continue;
     const uint8_t *src = static_cast<const uint8_t *>(p.saved.data) + row * p.saved.ld + col;
-    u32x2_out w = {0u, 0u};
-    if (nv == 8) {
-      w = *reinterpret_cast<const u32x2_out *>(src);
+    if (FULL || nv == 8) {
+      w[st] = __builtin_nontemporal_load(reinterpret_cast<const u32x2_out *>(src));
     } else {
       uint32_t x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = src[e < nv ? e : nv - 1];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e / 4] |= (e < nv ? x[e] : 0u) << (8 * (e % 4));
+      for (int e = 0; e < 8; ++e) w[st][e / 4] |= (e < nv ? x[e] : 0u) << (8 * (e % 4));
     }
-    const uint32_t byte = p.saved.exps[row * p.saved.ld_exps + col / kSaveGroup];
-    const f32x4 a = restore4(w[0], byte), b = restore4(w[1], byte);
+    byte[st] = p.saved.exps[row * p.saved.ld_exps + col / kSaveGroup];
+  }
+#pragma unroll
+  for (int st = 0; st < kSteps; ++st) {
+    const int64_t row = row0 + st * 16;
+    const int nv = FULL || row < p.rows ? nc : 0;
+    const f32x4 a = restore4(w[st][0], byte[st]), b = restore4(w[st][1], byte[st]);
     if constexpr (BF16) {
       uint16_t *dst = static_cast<uint16_t *>(p.x) + row * p.ld + col;
       const u32x4_in v = {bf16x2_bits(a[0], a[1]), bf16x2_bits(a[2], a[3]), bf16x2_bits(b[0], b[1]), bf16x2_bits(b[2], b[3])};
-      if (nv == 8) {
+      if (FULL || nv == 8) {
         *reinterpret_cast<u32x4_in *>(dst) = v;
       } else {
 #pragma unroll
@@ -102,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void act_restore_kernel(SaveParams p, int
       }
     } else {
       float *dst = static_cast<float *>(p.x) + row * p.ld + col;
-      if (nv == 8) {
+      if (FULL || nv == 8) {
         *reinterpret_cast<f32x4_in *>(dst) = a;
         *reinterpret_cast<f32x4_in *>(dst + 4) = b;
       } else {
@@ -114,21 +132,37 @@ __global__ __launch_bounds__(kThreads) void act_restore_kernel(SaveParams p, int
   }
 }
 
-template <typename K>
-hipError_t launch_tiles(K bf16, K f32, const SaveParams &p, hipStream_t s) {
+template <bool SAVE, bool BF16>
+__global__ __launch_bounds__(kThreads) void act_checkpoint_kernel(SaveParams p, int64_t tiles_c) {
+  const int64_t r0 = int64_t(blockIdx.x) / tiles_c * kRows, c0 = int64_t(blockIdx.x) % tiles_c * kTile;
+  const int64_t row = r0 + (threadIdx.x >> 4), col = c0 + (threadIdx.x & 15) * 8;
+  const bool full = r0 + kRows <= p.rows && c0 + kTile <= p.cols;
+  if constexpr (SAVE) {
+    if (full)
+      save_tile<BF16, true>(p, row, col);
+    else
+      save_tile<BF16, false>(p, row, col);
+  } else {
+    if (full)
+      restore_tile<BF16, true>(p, row, col);
+    else
+      restore_tile<BF16, false>(p, row, col);
+  }
+}
+
+template <bool SAVE>
+hipError_t launch_tiles(const SaveParams &p, hipStream_t s) {
   if (p.rows <= 0 || p.cols <= 0) return hipSuccess;
   const int64_t tiles_c = (p.cols + kTile - 1) / kTile, tiles = (p.rows + kRows - 1) / kRows * tiles_c;
   if (tiles >= int64_t(1) << 31) return hipErrorInvalidValue;
-  return klaunch(p.x_bf16 ? bf16 : f32, dim3(unsigned(tiles)), dim3(kThreads), 0, s, p, tiles_c);
+  const dim3 grid{unsigned(tiles)}, block(kThreads);
+  return p.x_bf16 ? klaunch(act_checkpoint_kernel<SAVE, true>, grid, block, 0, s, p, tiles_c)
+                  : klaunch(act_checkpoint_kernel<SAVE, false>, grid, block, 0, s, p, tiles_c);
 }
 
 }  // namespace
 
-hipError_t launch_act_save(const SaveParams &p, hipStream_t s) {
-  return launch_tiles(act_save_kernel<true>, act_save_kernel<false>, p, s);
-}
-hipError_t launch_act_restore(const SaveParams &p, hipStream_t s) {
-  return launch_tiles(act_restore_kernel<true>, act_restore_kernel<false>, p, s);
-}
+hipError_t launch_act_save(const SaveParams &p, hipStream_t s) { return launch_tiles<true>(p, s); }
+hipError_t launch_act_restore(const SaveParams &p, hipStream_t s) { return launch_tiles<false>(p, s); }
 
 }  // namespace qe

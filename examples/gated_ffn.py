@@ -1,0 +1,183 @@
+"""A gated feed-forward block in FP8 on one MI355X: a training step and single-token serving.
+
+    python examples/gated_ffn.py [--tokens 4096 --hidden 4096 --ffn 14336]   # Llama-3-8B-shaped by default
+
+    h = silu(x Wg^T) * (x Wu^T)        qe_fp8_gemm_gated, which keeps both pre-activations in 8 bits
+    y = h Wd^T + x                     qe_fp8_gemm_act
+    dh = dy Wd                         qe_fp8_gemm_tn
+    dg, du from dh and the checkpoint  qe_act_grad, straight to the FP8 codes that the next products read
+    dx = [dg du] [Wg; Wu], dW = ..     qe_fp8_gemm_tn, the weight gradients into one flat FP32 buffer
+
+Scales are delayed: every tensor is cast with the scale that its earlier amaxes gave it.  Nothing is allocated in a
+step, so it can be captured into a graph.
+"""
+import argparse
+import os
+import sys
+import time
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2609_23536_amd import qe  # noqa: E402
+
+
+def _ok(status):
+    if status != "OK":
+        raise RuntimeError(status)
+
+
+def _ld(v):
+    return (v + 15) // 16 * 16 if v <= 256 else (v + 127) // 128 * 128  # whole lines for long rows
+
+
+class Role:
+    """One tensor's FP8 codes, row-wise and transposed, and its delayed-scaling state."""
+
+    def __init__(self, rows, cols, fmt, history=16):
+        self.rows, self.cols, self.fmt = rows, cols, fmt
+        self.row = torch.zeros((rows, _ld(cols)), dtype=torch.uint8, device="cuda")
+        self.col = torch.zeros((cols, _ld(rows)), dtype=torch.uint8, device="cuda")
+        self.hist = torch.zeros(history, dtype=torch.float32, device="cuda")
+        self.scales = torch.ones(3, dtype=torch.float32, device="cuda")  # scale, its inverse, the inverse of the codes' own
+        self.accum = torch.zeros(qe.AMAX_LINES * qe.AMAX_STRIDE, dtype=torch.float32, device="cuda")
+        self.meta = qe.make_meta(self.hist, self.scales[0:1], self.scales[1:2], fmt, 0, self.accum)
+
+    @property
+    def inv(self):
+        return self.scales[2:3]
+
+    def cast(self, x, rows=None, transposed=True):
+        dt = qe.BF16 if x.dtype == torch.bfloat16 else qe.F32
+        _ok(qe.qe_quantize_fp8(x, dt, rows or self.rows, self.cols, self.meta, self.row, self.row.shape[1],
+                               self.col if transposed else None, self.col.shape[1] if transposed else 0, self.inv))
+
+
+class GatedFFN:
+    """Weights of one block and the buffers of one microbatch of `tokens`."""
+
+    def __init__(self, wg_wu, wd, tokens, act=qe.ACT_SILU):
+        self.act, self.tokens = act, tokens
+        self.ffn, self.hidden = wd.shape[1], wd.shape[0]
+        t, f, d = tokens, self.ffn, self.hidden
+        self.wgu_master, self.wd_master = wg_wu, wd
+        self.wgu, self.wd = Role(2 * f, d, qe.E4M3), Role(d, f, qe.E4M3)
+        self.x, self.h_q = Role(t, d, qe.E4M3), Role(t, f, qe.E4M3)
+        self.dy, self.dgu = Role(t, d, qe.E5M2), Role(t, 2 * f, qe.E5M2)
+        bf = dict(dtype=torch.bfloat16, device="cuda")
+        self.h, self.y = torch.zeros((t, f), **bf), torch.zeros((t, d), **bf)
+        self.dh, self.dx = torch.zeros((t, f), **bf), torch.zeros((t, d), **bf)
+        self.grad = torch.zeros(3 * f * d, dtype=torch.float32, device="cuda")  # dWgu, then dWd
+        groups = (f + qe.SAVED_GROUP - 1) // qe.SAVED_GROUP
+        self.codes = torch.zeros((2, t, f), dtype=torch.int8, device="cuda")
+        self.exps = torch.zeros((2, t, groups), dtype=torch.uint8, device="cuda")
+        self.saved = [qe.make_saved(qe.SAVED_I8, self.codes[i], f, self.exps[i], groups) for i in range(2)]
+
+    def refresh(self):
+        """After an optimizer step: the weights' codes."""
+        self.wgu.cast(self.wgu_master)
+        self.wd.cast(self.wd_master)
+
+    def _up(self, rows, saved):
+        f, w = self.ffn, self.wgu
+        _ok(qe.qe_fp8_gemm_gated(self.x.row, self.x.fmt, self.x.row.shape[1], w.row, w.row[f:], w.fmt, w.row.shape[1], rows,
+                                 f, self.hidden, self.x.inv, w.inv, w.inv, self.act, self.h, qe.BF16, f, saved[0], saved[1]))
+
+    def _down(self, x, rows):
+        d, w = self.hidden, self.wd
+        _ok(qe.qe_fp8_gemm_act(self.h_q.row, self.h_q.fmt, self.h_q.row.shape[1], w.row, w.fmt, w.row.shape[1], rows, d,
+                               self.ffn, self.h_q.inv, w.inv,
+                               qe.make_epilogue(residual=x, residual_dtype=qe.BF16, ld_residual=d), self.y, qe.BF16, d))
+
+    def forward(self, x):
+        self.x.cast(x)
+        self._up(self.tokens, self.saved)
+        self.h_q.cast(self.h)
+        self._down(x, self.tokens)
+        _ok(qe.qe_amax_scale_update([self.x.meta, self.h_q.meta]))
+        return self.y
+
+    def serve(self, x):
+        """A few tokens, nothing kept for a backward pass and no scale moved."""
+        n = x.shape[0]
+        self.x.cast(x, n, transposed=False)
+        self._up(n, (None, None))
+        self.h_q.cast(self.h, n, transposed=False)
+        self._down(x, n)
+        return self.y[:n]
+
+    @staticmethod
+    def _product(a, a_t, b, b_t, m, n, k, inv, out, dtype, ld):
+        _ok(qe.qe_fp8_gemm_tn(a, a_t, a.shape[1], b, b_t, b.shape[1], m, n, k, inv[0], inv[1], out, dtype, ld))
+
+    def backward(self, dy):
+        t, f, d = self.tokens, self.ffn, self.hidden
+        self.dy.cast(dy)
+        self._product(self.dy.row, self.dy.fmt, self.wd.col, self.wd.fmt, t, f, d, (self.dy.inv, self.wd.inv), self.dh, qe.BF16, f)
+        _ok(qe.qe_act_grad(self.dh, qe.BF16, f, t, f, self.act, self.saved[0], self.saved[1], meta=self.dgu.meta,
+                           q_row=self.dgu.row, ld_row=self.dgu.row.shape[1], q_col=self.dgu.col,
+                           ld_col=self.dgu.col.shape[1], scale_inv_snapshot=self.dgu.inv))
+        self._product(self.dgu.row, self.dgu.fmt, self.wgu.col, self.wgu.fmt, t, d, 2 * f, (self.dgu.inv, self.wgu.inv), self.dx,
+                      qe.BF16, d)
+        self.dx += dy  # the residual's own gradient
+        dwgu, dwd = self.grad[:2 * f * d], self.grad[2 * f * d:]
+        self._product(self.dgu.col, self.dgu.fmt, self.x.col, self.x.fmt, 2 * f, d, t, (self.dgu.inv, self.x.inv), dwgu, qe.F32, d)
+        self._product(self.dy.col, self.dy.fmt, self.h_q.col, self.h_q.fmt, d, f, t, (self.dy.inv, self.h_q.inv), dwd, qe.F32, f)
+        _ok(qe.qe_amax_scale_update([self.dy.meta, self.dgu.meta]))
+        return self.dx, dwgu.view(2 * f, d), dwd.view(d, f)
+
+
+def make(tokens, hidden, ffn, seed=0):
+    """A block with random weights, its input and its output's gradient, after two steps that set the scales."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+
+    def normal(*shape, sigma):
+        return (torch.randn(shape, generator=g, device="cuda") * sigma).to(torch.bfloat16)
+    block = GatedFFN(normal(2 * ffn, hidden, sigma=0.02), normal(hidden, ffn, sigma=0.02), tokens)
+    x, dy = normal(tokens, hidden, sigma=1.0), normal(tokens, hidden, sigma=0.01)
+    for _ in range(2):
+        block.refresh()
+        _ok(qe.qe_amax_scale_update([block.wgu.meta, block.wd.meta]))
+        block.refresh()
+        block.forward(x)
+        block.backward(dy)
+    return block, x, dy
+
+
+def reference(block, x, dy):
+    """y, dx, dWgu, dWd of the same block in 32 bits, without FP8."""
+    wgu, wd, x, dy = (t.float() for t in (block.wgu_master, block.wd_master, x, dy))
+    g, u = (x @ wgu.t()).split(block.ffn, 1)
+    p = torch.sigmoid(g)
+    h, dh = g * p * u, dy @ wd
+    dgu = torch.cat((dh * u * p * (1 + g * (1 - p)), dh * g * p), 1)
+    return h @ wd.t() + x, dgu @ wgu + dy, dgu.t() @ x, dy.t() @ h
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--tokens", type=int, default=4096)
+    ap.add_argument("--hidden", type=int, default=4096)
+    ap.add_argument("--ffn", type=int, default=14336)
+    a = ap.parse_args()
+    block, x, dy = make(a.tokens, a.hidden, a.ffn)
+
+    def timed(name, fn, n=20):
+        fn()
+        torch.cuda.synchronize()
+        t = time.perf_counter()
+        for _ in range(n):
+            fn()
+        torch.cuda.synchronize()
+        print("%-34s %9.1f us" % (name, (time.perf_counter() - t) / n * 1e6))
+    got = (block.forward(x), *block.backward(dy))
+    for name, v, r in zip(("y", "dx", "dWg, dWu", "dWd"), got, reference(block, x, dy)):
+        print("%-9s relative difference to FP32 %.3f" % (name, float((v.float() - r).norm() / r.norm())))
+    timed("forward, %d tokens" % a.tokens, lambda: block.forward(x))
+    timed("backward", lambda: block.backward(dy))
+    timed("serve, 1 token", lambda: block.serve(x[:1]))
+
+
+if __name__ == "__main__":
+    main()

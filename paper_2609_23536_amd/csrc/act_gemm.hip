@@ -531,22 +531,23 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void act_r
 // Up to 16 rows (a token or a few being served): every operand row of B is read once
 // and by one workgroup, so the product is bound by streaming B from memory, and
 // what a tile kernel does for reuse (LDS stages, barriers) only costs latency.
-// A workgroup takes 16 OB outputs; its W waves split the reduction, K tile t to
+// (Also for more rows where few_blocks says so.)
+// A workgroup takes 16 rows and 16 OB outputs; its W waves split the reduction, K tile t to
 // wave t % W.  A wave loads its fragments straight into registers, U K tiles
 // in flight (lane l: row l % 16, bytes 16 (l / 16) of either half of the 128,
 // the same for both operands), and the waves' sums meet in LDS, added in order.
 template <bool GATED, int FA, int FB, int OB, int W>
-__global__ __launch_bounds__(64 * W) void act_rows_kernel(ActGemmParams g) {
+__global__ __launch_bounds__(64 * W) void act_rows_kernel(ActGemmParams g, int blocks_n) {
   constexpr int NB = GATED ? 2 * OB : OB;  // 16-row blocks of B
   constexpr int U = 4;                     // K tiles in flight
   constexpr int EP = 16 * NB + 4;
   __shared__ __attribute__((aligned(16))) float sums[W][16 * EP];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   const int fr = lane & 15, fq = lane >> 4;
-  const int64_t n0 = int64_t(blockIdx.x) * (16 * OB);
+  const int64_t m0 = int64_t(int(blockIdx.x) / blocks_n) * 16, n0 = int64_t(int(blockIdx.x) % blocks_n) * (16 * OB);
   const int T = int((g.k + BK - 1) / BK), ktail = int(g.k % BK);
 
-  const uint8_t *pa = g.a + min(int64_t(fr), g.m - 1) * g.lda, *pb[NB];
+  const uint8_t *pa = g.a + min(m0 + fr, g.m - 1) * g.lda, *pb[NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) {  // gated: gates and ups in alternating blocks
     const int64_t row = min(n0 + 16 * (GATED ? j / 2 : j) + fr, g.n - 1);
@@ -615,11 +616,28 @@ __global__ __launch_bounds__(64 * W) void act_rows_kernel(ActGemmParams g) {
         v4f{__builtin_ldexpf(s[0], e), __builtin_ldexpf(s[1], e), __builtin_ldexpf(s[2], e), __builtin_ldexpf(s[3], e)};
   }
   __syncthreads();
-  if (threadIdx.x < 64) finish_rows<GATED, 16, 16 * OB, 64, EP>(g, sums[0], lane, 0, n0);
+  if (threadIdx.x < 64) finish_rows<GATED, 16, 16 * OB, 64, EP>(g, sums[0], lane, m0, n0);
 }
 
 constexpr int64_t kFewRows = 16;
 constexpr int kFewRowsTile = 0;  // in place of a GemmTile
+
+// More rows, in blocks of 16, where the whole product has few blocks and a long
+// reduction: a tile kernel then runs a handful of workgroups, each through all of
+// K.  MI355X, us with the small tiles / so: 17 x 512 x 2048 6.3 / 4.6, 17 x 256 x 16092
+// 19.5 / 12.4, 112 x 128 x 16092 32.6 / 12.7, 200 x 256 x 6534 10.9 / 7.7, gated 369 x 128 x
+// 6534 17.2 / 10.1; at K = 512 both are level.  Past one workgroup per unit every
+// block's operands come from the caches once more: 369 x 256 x 16092 (384 blocks) 37.3 /
+// 22.7, but 200 x 512 x 6534 (416) 11.0 / 12.7 and 1340 columns of K = 2048 (588) 6.3 / 8.3.
+// Gated products saved in 8 bits take 32 outputs a workgroup and lose: 50 x 64 x
+// 6534 11.5 / 15.2.
+bool few_blocks(const ActGemmParams &p) {
+  if (p.m <= kFewRows) return true;
+  const bool gated = p.b2 != nullptr, wide = p.z.kind == kSavedI8;
+  const int64_t blocks = (p.m + 15) / 16 * ((p.n + (wide ? 31 : 15)) / (wide ? 32 : 16));
+  if (p.k <= 1024 || (gated && wide)) return false;
+  return blocks <= 256 || (blocks <= 512 && p.k > 12288 && !gated && !wide);
+}
 
 // One workgroup for 16 outputs (32 where they are saved in 8 bits, whose groups
 // have 32 columns).  Eight waves keep the most bytes in flight, but up to 16 K
@@ -634,12 +652,13 @@ constexpr int kFewRowsTile = 0;  // in place of a GemmTile
 template <bool GATED, int FA, int FB>
 hipError_t launch_few_rows(const ActGemmParams &p, hipStream_t s) {
   const bool wide = p.z.kind == kSavedI8, few = p.k <= 16 * BK;
-  const dim3 grid(unsigned((p.n + (wide ? 31 : 15)) / (wide ? 32 : 16)));
+  const int blocks_n = int((p.n + (wide ? 31 : 15)) / (wide ? 32 : 16));
+  const dim3 grid(unsigned((p.m + 15) / 16) * unsigned(blocks_n));
   if (wide)
-    return few ? klaunch(act_rows_kernel<GATED, FA, FB, 2, 4>, grid, dim3(256), 0, s, p)
-               : klaunch(act_rows_kernel<GATED, FA, FB, 2, 8>, grid, dim3(512), 0, s, p);
-  return few ? klaunch(act_rows_kernel<GATED, FA, FB, 1, 4>, grid, dim3(256), 0, s, p)
-             : klaunch(act_rows_kernel<GATED, FA, FB, 1, 8>, grid, dim3(512), 0, s, p);
+    return few ? klaunch(act_rows_kernel<GATED, FA, FB, 2, 4>, grid, dim3(256), 0, s, p, blocks_n)
+               : klaunch(act_rows_kernel<GATED, FA, FB, 2, 8>, grid, dim3(512), 0, s, p, blocks_n);
+  return few ? klaunch(act_rows_kernel<GATED, FA, FB, 1, 4>, grid, dim3(256), 0, s, p, blocks_n)
+             : klaunch(act_rows_kernel<GATED, FA, FB, 1, 8>, grid, dim3(512), 0, s, p, blocks_n);
 }
 
 template <bool GATED, int FA, int FB>
@@ -697,7 +716,7 @@ hipError_t launch_act_gemm(const ActGemmParams &p, hipStream_t s) {
                                1u << kTile128x64Deep | 1u << kTile64x128 | 1u << kTile64x128Deep | 1u << kTile128x128 |
                                1u << kTile128x128Deep;
   const int force = gemm_tile_override();
-  if (force == kTileAuto && p.m <= kFewRows)
+  if (force == kTileAuto && few_blocks(p))
     return gated ? launch_fmts<true>(kFewRowsTile, p, s) : launch_fmts<false>(kFewRowsTile, p, s);
   const int tile = force == kTileAuto ? choose_gemm_tile(g, kShapes) : (force == kTile192x256 ? kTile192x256 : kTile256x256);
   return gated ? launch_fmts<true>(tile, p, s) : launch_fmts<false>(tile, p, s);

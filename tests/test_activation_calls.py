@@ -28,6 +28,16 @@ def test_products_get_their_kernel():
         assert len(names) == 1 and t[0] in names[0], (t, names)
 
 
+# gated, m, n, k: up to 16 rows, or few blocks of 16 x 16 outputs and a long reduction; and what is just past that
+ROWS = [(False, 1, 4096, 14336), (True, 16, 14336, 4096), (False, 17, 256, 1025), (True, 256, 256, 1025), (False, 512, 256, 12289)]
+TILED = [(False, 17, 256, 1024), (True, 257, 256, 1025), (False, 257, 256, 12288), (False, 513, 256, 12289), (True, 512, 256, 12289)]
+
+
+def test_few_blocks_split_the_reduction():
+    assert all("act_rows_kernel" in n for n, in calls(product_launches, [list(c) for c in ROWS]))
+    assert all("act_rows_kernel" not in n for n, in calls(product_launches, [list(c) for c in TILED]))
+
+
 OK = dict(a=16, fmt_a=0, lda=32, b=16, fmt_b=0, ldb=32, m=4, n=40, k=20, sa=16, sb=16, c=16, c_dtype=1, ldc=40)
 
 
@@ -163,3 +173,18 @@ def test_struct_sizes():
         subprocess.run(["gcc", "-std=c99", "-I", os.path.join(ROOT, "include"), c, "-o", exe], check=True)
         got = subprocess.run([exe], check=True, capture_output=True, text=True).stdout.split()
     assert [int(v) for v in got] == [ctypes.sizeof(qe.Saved), ctypes.sizeof(qe.Epilogue)]
+
+
+# name part, workgroups a compute unit is to hold (of a SIMD's 512 registers, given in eights, and 160 KB of LDS)
+OCCUPANCY = [("act_grad_kernelILb1ELb1ELi2ELi128ELi256E", 3), ("act_grad_kernelILb0ELb1ELi2ELi64ELi512E", 3),
+             ("act_ring_kernelILb1ELi0ELi0ELi64ELi64ELi4E", 2), ("act_ring_kernelILb0ELi0ELi0ELi128ELi128ELi2E", 2),
+             ("act_rows_kernelILb1ELi0ELi0ELi1ELi8E", 2), ("act_large_kernelILb1ELi0ELi0ELi256ELi256E", 1)]
+
+
+@pytest.mark.parametrize("part,workgroups", OCCUPANCY, ids=lambda v: str(v))
+def test_workgroups_per_compute_unit(part, workgroups):
+    from tests.kernel_resources import kernels
+    k, = [k for n, k in kernels(need_lib().LIB_PATH).items() if part in n]
+    waves = k[".max_flat_workgroup_size"] // 256  # on each SIMD
+    assert 512 // ((k[".vgpr_count"] + 7) // 8 * 8) >= workgroups * max(1, waves)
+    assert k[".group_segment_fixed_size"] * workgroups <= 160 * 1024

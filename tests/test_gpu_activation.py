@@ -188,6 +188,16 @@ def test_every_small_tile(tile):
         check_product(qe, dev(), (m, n, k), 5, "silu", "f32", "bf16", "bf16", "none" if m * n > 2 ** 20 else "i8")
 
 
+@pytest.mark.parametrize("shape", [(17, 33, 1100), (50, 70, 2100), (33, 500, 4001), (112, 160, 12300), (369, 250, 12304)], ids=ids)
+def test_few_blocks_of_a_long_reduction(shape):
+    """Several row blocks through the kernel that splits the reduction over its waves."""
+    qe, d = need_lib(), dev()
+    check_product(qe, d, shape, 1, "gelu", "f32", "bf16", "bf16", "none", 0, 0, 3)
+    check_product(qe, d, shape, 2, "silu", "none", "none", "f32", "i8", 1, 0, 0)
+    check_gated(qe, d, shape, 3, "silu", "bf16", "none", 0, 0, 1)
+    check_gated(qe, d, shape, 4, "relu", "f32", "bf16", 0, 1, 0)
+
+
 @pytest.mark.parametrize("shape", [(1, 1, 1), (37, 53, 100), (256, 128, 128), (300, 520, 384), (513, 259, 1000)], ids=ids)
 @pytest.mark.parametrize("tile", ["TILE_256x256", "TILE_192x256"])
 def test_large_tiles(tile, shape):

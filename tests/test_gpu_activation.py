@@ -218,6 +218,17 @@ def test_residual_in_place(dtype):
         check_product(need_lib(), dev(), shape, 9, "silu", "none", dtype, dtype, "none", in_place=True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_residual_in_place_on_large_tiles(dtype):
+    qe, d = need_lib(), dev()
+    assert qe.qe_set_gemm_tile(qe.TILE_256x256) == "OK"
+    try:
+        for shape in ((256, 256, 128), (300, 333, 256)):
+            check_product(qe, d, shape, 9, "gelu", "f32", dtype, dtype, "none", in_place=True)
+    finally:
+        assert qe.qe_set_gemm_tile(qe.TILE_AUTO) == "OK"
+
+
 def test_an_empty_reduction_leaves_bias_and_residual():
     qe, d = need_lib(), dev()
     a, bias = torch.zeros(64, dtype=torch.uint8, device=d), torch.arange(40, dtype=torch.float32, device=d)
@@ -341,8 +352,14 @@ def test_bias_grad(shape):
 
 @pytest.mark.parametrize("gated", [False, True])
 def test_grad_of_large_tensors(gated):
-    """Past 512 tiles of 128 rows, where the tiles have 128 rows."""
+    """Hundreds of 64-row tiles, in more than one group of row tiles."""
     check_grad(need_lib(), dev(), 2900, 3001, 8, "gelu_tanh", gated, "bf16", "bf16", 1, bias=None if gated else need_lib().INIT)
+
+
+@pytest.mark.parametrize("gated,rows,cols", [(False, 4200, 4300), (True, 8300, 2100)])
+def test_grad_of_tall_tiles(gated, rows, cols):
+    """Past 1024 tiles of 128 rows, where the tiles have 128 rows."""
+    check_grad(need_lib(), dev(), rows, cols, 8, "silu", gated, "bf16", "bf16", 1, bias=None if gated else need_lib().INIT)
 
 
 def test_grad_of_infinities_and_nans():

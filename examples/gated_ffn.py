@@ -74,9 +74,10 @@ class GatedFFN:
         self.saved = [qe.make_saved(qe.SAVED_I8, self.codes[i], f, self.exps[i], groups) for i in range(2)]
 
     def refresh(self):
-        """After an optimizer step: the weights' codes."""
+        """After an optimizer step: the weights' codes, and the scales of the next ones."""
         self.wgu.cast(self.wgu_master)
         self.wd.cast(self.wd_master)
+        _ok(qe.qe_amax_scale_update([self.wgu.meta, self.wd.meta]))
 
     def _up(self, rows, saved):
         f, w = self.ffn, self.wgu
@@ -136,9 +137,8 @@ def make(tokens, hidden, ffn, seed=0):
         return (torch.randn(shape, generator=g, device="cuda") * sigma).to(torch.bfloat16)
     block = GatedFFN(normal(2 * ffn, hidden, sigma=0.02), normal(hidden, ffn, sigma=0.02), tokens)
     x, dy = normal(tokens, hidden, sigma=1.0), normal(tokens, hidden, sigma=0.01)
+    block.refresh()
     for _ in range(2):
-        block.refresh()
-        _ok(qe.qe_amax_scale_update([block.wgu.meta, block.wd.meta]))
         block.refresh()
         block.forward(x)
         block.backward(dy)

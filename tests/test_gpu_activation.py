@@ -237,6 +237,28 @@ def test_an_empty_reduction_leaves_bias_and_residual():
     assert torch.equal(c, bias.expand(3, 40))
 
 
+@pytest.mark.parametrize("shape", [(65, 62), (300, 520)], ids=ids)
+@pytest.mark.parametrize("tile", ["TILE_AUTO", "TILE_256x256", "TILE_192x256"])
+def test_an_empty_reduction_on_every_kind_of_tile(tile, shape):
+    """Sums of nothing are zero: the bias through the activation, plus the residual; a gated product is zero."""
+    qe, d = need_lib(), dev()
+    m, n = shape
+    codes, one = torch.full((max(m, n), 16), 0x3A, dtype=torch.uint8, device=d), torch.ones(1, device=d)
+    bias = (torch.arange(n, device=d) - n // 2).float()
+    res = torch.arange(m * n, device=d).reshape(m, n).float()
+    c, h = filled(m, n, torch.float32, d), filled(m, n, torch.float32, d)
+    assert qe.qe_set_gemm_tile(getattr(qe, tile)) == "OK"
+    try:
+        epi = qe.make_epilogue(qe.ACT_RELU, bias, qe.F32, res, qe.F32, n)
+        assert qe.qe_fp8_gemm_act(codes, 0, 16, codes, 0, 16, m, n, 0, one, one, epi, c, qe.F32, n) == "OK"
+        assert qe.qe_fp8_gemm_gated(codes, 0, 16, codes, codes, 0, 16, m, n, 0, one, one, one, qe.ACT_SILU, h, qe.F32, n) == "OK"
+        torch.cuda.synchronize()
+    finally:
+        assert qe.qe_set_gemm_tile(qe.TILE_AUTO) == "OK"
+    assert torch.equal(c[:m], bias.clamp(min=0) + res) and untouched(c, m, n)
+    assert bool((h[:m] == 0).all()) and untouched(h, m, n)
+
+
 def test_random_codes_against_float64():
     """Sums of ordinary values: the matrix instruction holds FP32 sums of 128 products, which it aligns to their
     largest before it adds (the plain GEMM's tests allow 1e-3 of the largest output)."""

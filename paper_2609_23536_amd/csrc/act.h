@@ -116,8 +116,8 @@ __device__ __forceinline__ void act_switch(int act, F &&f) {
 // error is at most half a step, amax / 127 at most.  The group's byte is
 // 127 - s, the step's exponent field: amax's own exponent field less 6, one
 // more where its mantissa is above 127/64 (the carry of the addition below).
-// An infinity or a NaN makes the byte 255, whose step is infinite: code * step
-// and the restoring fma below are then NaN for the whole group.
+// An infinity or a NaN makes the byte 255, whose step is infinite, with codes of
+// zero: code * step is then NaN for the whole group.
 // Steps that are powers of two keep the restored values exact in BF16 and FP32
 // (a code has seven bits), scaling exact, and the byte count at 33/32.
 constexpr int kSaveGroup = 32;
@@ -139,18 +139,16 @@ __device__ __forceinline__ uint32_t save_codes(f32x4 x, uint32_t byte) {
   return byte == 255u ? 0u : lo | hi;
 }
 
-// Code j of a word, restored: the code as an unsigned byte u = code + 128 has a
-// hardware conversion, and u step - 128 step is exact.  `word` has its sign
-// bits flipped (w ^ 0x80808080).
+// Code j of a word, restored: a signed byte has a hardware conversion, and the
+// product with the step is exact.  (Not as code + 128 with an addend of -128
+// steps: that addend overflows for the steps 2^121 and 2^122 of large groups.)
 template <int J>
-__device__ __forceinline__ float restore_code(uint32_t word, float step, float off) {
-  return __builtin_fmaf(float((word >> (8 * J)) & 0xffu), step, off);  // off = -128 step
+__device__ __forceinline__ float restore_code(uint32_t word, float step) {
+  return float(int8_t(word >> (8 * J))) * step;
 }
 __device__ __forceinline__ f32x4 restore4(uint32_t codes, uint32_t byte) {
-  const float step = __uint_as_float(byte << 23), off = -128.0f * step;
-  const uint32_t w = codes ^ 0x80808080u;
-  return f32x4{restore_code<0>(w, step, off), restore_code<1>(w, step, off), restore_code<2>(w, step, off),
-             restore_code<3>(w, step, off)};
+  const float step = __uint_as_float(byte << 23);
+  return f32x4{restore_code<0>(codes, step), restore_code<1>(codes, step), restore_code<2>(codes, step), restore_code<3>(codes, step)};
 }
 
 // Maxima that keep a NaN (one instruction for three operands on gfx950).

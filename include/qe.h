@@ -254,8 +254,10 @@ typedef enum { QE_ACT_NONE = 0, QE_ACT_RELU = 1, QE_ACT_GELU = 2, QE_ACT_GELU_TA
  * Of a group with a = max |x|, s = floor(log2(127 / a)) clamped to [-126, 126]
  * (126 for a = 0), code = x 2^s rounded to nearest even, byte = 127 - s and the
  * restored value code 2^-s, exact in BF16 and FP32: off by at most half a step
- * 2^-s, which lies between a / 127 and a / 63.5.  A group that holds a NaN or
- * an infinity restores as NaN (byte 255, codes 0). */
+ * 2^-s, which lies between a / 127 and a / 63.5.  (For s = -122 codes stop at 63
+ * in magnitude, because 64 * 2^122 is no finite number of either type: values
+ * from 63.5 * 2^122 on are off by less than a step.)  A group that holds a NaN
+ * or an infinity restores as NaN (byte 255, codes 0). */
 typedef enum { QE_SAVED_NONE = 0, QE_SAVED_BF16 = 1, QE_SAVED_I8 = 2 } qe_saved_kind;
 typedef struct {
   void *data;

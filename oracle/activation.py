@@ -69,7 +69,8 @@ def pack(x):
     """(codes int8 [rows, cols], exponent bytes [rows, ceil(cols / 32)]) of float32 values.
 
     A group's step is 2^-s, s the largest integer <= 126 with amax 2^s <= 127; codes are x 2^s to nearest even and the byte
-    is 127 - s.  A group with a NaN or an infinity: byte 255, codes 0.
+    is 127 - s.  The codes of the largest step (s = -122) stop at 63, so that they restore to finite float32 values.  A group
+    with a NaN or an infinity: byte 255, codes 0.
     """
     x = np.asarray(x, dtype=np.float64)
     rows, cols = x.shape
@@ -90,7 +91,8 @@ def pack(x):
                 while amax[r] * 2.0 ** s > 127.0:
                     s -= 1
             exps[r, g] = 127 - s
-            codes[r, g * GROUP:(g + 1) * GROUP] = np.rint(part[r] * 2.0 ** s).astype(np.int8)
+            most = 63 if s == -122 else 127  # 64 steps of 2^122 are 2^128
+            codes[r, g * GROUP:(g + 1) * GROUP] = np.clip(np.rint(part[r] * 2.0 ** s), -most, most).astype(np.int8)
     return codes, exps
 
 

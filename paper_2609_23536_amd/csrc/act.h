@@ -113,7 +113,8 @@ __device__ __forceinline__ void act_switch(int act, F &&f) {
 // ----------------------------------------------------------- 8-bit checkpoint
 // 32 columns of a row share a step 2^-s, s = floor(log2(127 / amax)) clamped to
 // [-126, 126]; a value is the int8 code rne(x 2^s), so |code| <= 127 and the
-// error is at most half a step, amax / 127 at most.  The group's byte is
+// error is at most half a step, amax / 127 at most (less than a step from 63.5 *
+// 2^122 on, see save_codes).  The group's byte is
 // 127 - s, the step's exponent field: amax's own exponent field less 6, one
 // more where its mantissa is above 127/64 (the carry of the addition below).
 // An infinity or a NaN makes the byte 255, whose step is infinite, with codes of
@@ -129,14 +130,25 @@ __device__ __forceinline__ uint32_t save_exponent(float group_max) {
 }
 
 // Four values -> four int8 codes.  x 2^s is exact; adding 1.5 * 2^23 rounds it
-// to nearest even and leaves the code in the sum's low byte.
+// to nearest even and leaves the code in the sum's low byte.  RARE: the byte
+// may be the largest step's, 2^122, whose codes stop at 63 because 64 steps are
+// 2^128, or 255.  Whether it may is asked once for all that a wave stores
+// together: a branch around every four values cost 4% of a gated training pass.
+constexpr uint32_t kSaveTopByte = 249u;
+__device__ __forceinline__ bool save_rare(uint32_t byte) { return __builtin_amdgcn_ballot_w64(byte >= kSaveTopByte) != 0; }
+template <bool RARE>
 __device__ __forceinline__ uint32_t save_codes(f32x4 x, uint32_t byte) {
+  if constexpr (RARE) {
+    const float top = byte == kSaveTopByte ? 0x1.f8p127f : __builtin_inff();  // 63 steps
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_fmed3f(x[e], -top, top);
+  }
   const float mult = __uint_as_float((254u - byte) << 23);  // 2^s
   constexpr float kRound = 12582912.0f;
   const uint32_t b0 = __float_as_uint(__builtin_fmaf(x[0], mult, kRound)), b1 = __float_as_uint(__builtin_fmaf(x[1], mult, kRound));
   const uint32_t b2 = __float_as_uint(__builtin_fmaf(x[2], mult, kRound)), b3 = __float_as_uint(__builtin_fmaf(x[3], mult, kRound));
   const uint32_t lo = __builtin_amdgcn_perm(b1, b0, 0x0c0c0400u), hi = __builtin_amdgcn_perm(b3, b2, 0x04000c0cu);
-  return byte == 255u ? 0u : lo | hi;
+  return RARE && byte == 255u ? 0u : lo | hi;
 }
 
 // Code j of a word, restored: a signed byte has a hardware conversion, and the

@@ -98,7 +98,7 @@ __device__ __forceinline__ void save_quad(const SavedRef &s, int64_t row, int64_
     for (int e = 0; e < 4; ++e) z[e] = e < nv ? z[e] : 0.0f;
   }
   const uint32_t byte = save_exponent(max_lanes8(amax4(z)));
-  const uint32_t codes = save_codes(z, byte);
+  const uint32_t codes = __builtin_expect(save_rare(byte), 0) ? save_codes<true>(z, byte) : save_codes<false>(z, byte);
   uint8_t *p = static_cast<uint8_t *>(s.data) + row * s.ld + col;
   if (nv == 4) {
     *reinterpret_cast<u32_at1 *>(p) = codes;
@@ -219,17 +219,32 @@ __device__ __forceinline__ void stage_codes(uint8_t *ls, int lane, uint8_t *exps
                                             const v4f (&v)[NR][QUADS]) {
   using L = Rows<QUADS, 1>;
   static_assert(QUADS == 4 || QUADS == 8, "whole groups, their bytes in a word");
+  uint32_t byte[NR][QUADS / 2], most = 0u;
+#pragma unroll
+  for (int h = 0; h < NR; ++h)
+#pragma unroll
+    for (int q = 0; q < QUADS / 2; ++q) {
+      byte[h][q] = save_exponent(max_lanes_by16(nan_max(amax4(v[h][2 * q]), amax4(v[h][2 * q + 1]))));
+      most = byte[h][q] > most ? byte[h][q] : most;
+    }
+  auto codes = [&](auto rare) {
+    constexpr bool RARE = decltype(rare)::value;
+#pragma unroll
+    for (int h = 0; h < NR; ++h)
+#pragma unroll
+      for (int q = 0; q < QUADS; ++q)
+        *reinterpret_cast<uint32_t *>(ls + (16 * h + (lane & 15)) * L::PITCH + 16 * q + 4 * (lane >> 4)) =
+            save_codes<RARE>(v[h][q], byte[h][q / 2]);
+  };
+  if (__builtin_expect(save_rare(most), 0))
+    codes(std::true_type{});
+  else
+    codes(std::false_type{});
 #pragma unroll
   for (int h = 0; h < NR; ++h) {
     uint32_t bytes = 0u;
 #pragma unroll
-    for (int q = 0; q < QUADS; q += 2) {
-      const uint32_t byte = save_exponent(max_lanes_by16(nan_max(amax4(v[h][q]), amax4(v[h][q + 1]))));
-      bytes |= byte << (4 * q);
-      uint8_t *at = ls + (16 * h + (lane & 15)) * L::PITCH + 16 * q + 4 * (lane >> 4);
-      *reinterpret_cast<uint32_t *>(at) = save_codes(v[h][q], byte);
-      *reinterpret_cast<uint32_t *>(at + 16) = save_codes(v[h][q + 1], byte);
-    }
+    for (int q = 0; q < QUADS / 2; ++q) bytes |= byte[h][q] << (8 * q);
     if (lane < 16 && (!EDGE || 16 * h + lane < rows)) {
       uint8_t *at = exps + (16 * h + lane) * ld_exps;
       if (EDGE && cols < 16 * QUADS) {

@@ -64,22 +64,34 @@ __device__ __forceinline__ void save_tile(const SaveParams &p, int64_t row0, int
 #pragma unroll
   for (int st = 0; st < kSteps; ++st)
     x[st] = load8<BF16, FULL, NT>(p.x, (row0 + st * 16) * p.ld + col, FULL || row0 + st * 16 < p.rows ? nc : 0);
+  uint32_t byte[kSteps], most = 0u;
 #pragma unroll
   for (int st = 0; st < kSteps; ++st) {
-    const int64_t row = row0 + st * 16;
-    const int nv = FULL || row < p.rows ? nc : 0;
-    const uint32_t byte = save_exponent(max_lanes4(nan_max(amax4(x[st].a), amax4(x[st].b))));
-    const uint32_t w0 = save_codes(x[st].a, byte), w1 = save_codes(x[st].b, byte);
-    uint8_t *dst = static_cast<uint8_t *>(p.saved.data) + row * p.saved.ld + col;
-    if (FULL || nv == 8) {
-      *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w0, w1};
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < nv) dst[e] = uint8_t(byte_of(e < 4 ? w0 : w1, e % 4));
-    }
-    if (nv > 0 && (col & (kSaveGroup - 1)) == 0) p.saved.exps[row * p.saved.ld_exps + col / kSaveGroup] = uint8_t(byte);
+    byte[st] = save_exponent(max_lanes4(nan_max(amax4(x[st].a), amax4(x[st].b))));
+    most = byte[st] > most ? byte[st] : most;
   }
+  auto store = [&](auto rare) {
+    constexpr bool RARE = decltype(rare)::value;
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) {
+      const int64_t row = row0 + st * 16;
+      const int nv = FULL || row < p.rows ? nc : 0;
+      const uint32_t w0 = save_codes<RARE>(x[st].a, byte[st]), w1 = save_codes<RARE>(x[st].b, byte[st]);
+      uint8_t *dst = static_cast<uint8_t *>(p.saved.data) + row * p.saved.ld + col;
+      if (FULL || nv == 8) {
+        *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{w0, w1};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < nv) dst[e] = uint8_t(byte_of(e < 4 ? w0 : w1, e % 4));
+      }
+      if (nv > 0 && (col & (kSaveGroup - 1)) == 0) p.saved.exps[row * p.saved.ld_exps + col / kSaveGroup] = uint8_t(byte[st]);
+    }
+  };
+  if (__builtin_expect(save_rare(most), 0))
+    store(std::true_type{});
+  else
+    store(std::false_type{});
 }
 
 template <bool BF16, bool FULL>

@@ -88,3 +88,62 @@ def test_gradient_far_out(act):
                               dz_dtype=qe.F32, ld_dz=cols) == "OK"
         want = np.where(codes > 0, 0.5, np.where(codes < 0, 0.0, 0.25))
         assert np.array_equal(dz.double().cpu().numpy(), want)
+
+
+TOP = 2.0 ** 122  # the largest step
+LARGEST = float(np.finfo(np.float32).max)
+TOPMOST = [63.5 * TOP, np.nextafter(np.float32(63.5 * TOP), np.float32(0)), -63.5 * TOP, LARGEST, -LARGEST, 63.0 * TOP, 62.5 * TOP,
+           -0.5 * TOP, 0.75 * TOP, 0.0, 255.0 * 2.0 ** 120]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [32, 45])
+def test_the_largest_finite_values_stay_finite(cols, dtype):
+    """Off by less than a step and never infinite; the rest of their group as ever, within half a step."""
+    qe, d = need_lib(), dev()
+    v = np.zeros((3, cols), dtype=np.float32)
+    v[0, :len(TOPMOST)], v[1, :len(TOPMOST)], v[2, cols - 1] = TOPMOST, np.negative(TOPMOST), 255.0 * 2.0 ** 120
+    t, q = {"bf16": (torch.bfloat16, qe.BF16), "f32": (torch.float32, qe.F32)}[dtype]
+    if dtype == "bf16":
+        v = np.where(np.abs(v) > 255.0 * 2.0 ** 120, np.sign(v) * 255.0 * 2.0 ** 120, v).astype(np.float32)
+    x = torch.from_numpy(v).to(d).to(t)
+    v = x.double().cpu().numpy()
+    assert np.isfinite(v).all()
+    groups = -(-cols // 32)
+    data = torch.zeros((3, cols), dtype=torch.int8, device=d)
+    exps = torch.zeros((3, groups), dtype=torch.uint8, device=d)
+    s = qe.make_saved(qe.SAVED_I8, data, cols, exps, groups)
+    assert qe.qe_act_save(x, q, cols, 3, cols, s) == "OK"
+    codes, bytes_ = oa.pack(v)
+    assert np.array_equal(data.cpu().numpy(), codes) and np.array_equal(exps.cpu().numpy(), bytes_)
+    assert bytes_[0, 0] == 249 and np.abs(codes[0]).max() == 63
+    back = torch.zeros_like(x)
+    assert qe.qe_act_restore(s, 3, cols, back, q, cols) == "OK"
+    off = np.abs(back.double().cpu().numpy() - v)
+    assert (off < TOP).all() and (off[np.abs(v) < 63.5 * TOP] <= TOP / 2).all()
+
+
+@pytest.mark.parametrize("shape", [(3, 40), (20, 130), (70, 300)], ids=str)
+@pytest.mark.parametrize("tile", ["TILE_AUTO", "TILE_256x256"])
+def test_products_save_the_largest_finite_values(tile, shape):
+    """Pre-activations of a product (sums of nothing plus a bias) through each of its epilogues' checkpoints."""
+    qe, d = need_lib(), dev()
+    m, n = shape
+    bias = np.zeros(n, dtype=np.float32)
+    bias[:len(TOPMOST)] = TOPMOST
+    bias[n - 1] = -LARGEST
+    codes, one = torch.full((max(m, n), 16), 0x38, dtype=torch.uint8, device=d), torch.ones(1, device=d)
+    groups = -(-n // 32)
+    data = torch.zeros((m, n), dtype=torch.int8, device=d)
+    exps = torch.zeros((m, groups), dtype=torch.uint8, device=d)
+    c, b = torch.zeros((m, n), device=d), torch.from_numpy(bias).to(d)
+    epi = qe.make_epilogue(bias=b, bias_dtype=qe.F32, saved=qe.make_saved(qe.SAVED_I8, data, n, exps, groups))
+    assert qe.qe_set_gemm_tile(getattr(qe, tile)) == "OK"
+    try:
+        assert qe.qe_fp8_gemm_act(codes, 0, 16, codes, 0, 16, m, n, 0, one, one, epi, c, qe.F32, n) == "OK"
+        torch.cuda.synchronize()
+    finally:
+        assert qe.qe_set_gemm_tile(qe.TILE_AUTO) == "OK"
+    want = oa.pack(np.broadcast_to(bias, (m, n)))
+    assert np.array_equal(data.cpu().numpy(), want[0]) and np.array_equal(exps.cpu().numpy(), want[1])
+    assert np.isfinite(oa.unpack(*want).astype(np.float32)).all()

@@ -197,7 +197,9 @@ qe_status qe_quantize_fp8_current_noalloc(const void *in, qe_dtype in_dtype, int
 /* FP8 GEMM in "TN" form (both operands contiguous along the reduction axis):
  *     D[i][j] = (a_scale_inv * b_scale_inv) * sum_r A[i][r] * B[j][r]
  * A: m x k codes of format fmt_a, row stride lda bytes.  B: n x k codes of
- * format fmt_b, stride ldb.  a_scale_inv / b_scale_inv: one device float each.
+ * format fmt_b, stride ldb.  a_scale_inv / b_scale_inv: one device float each,
+ * of any value; where both are powers of two (as the scale update makes them) the
+ * scaling is exact, else their product and the scaled sum are each rounded once.
  * FP32 accumulation.  mode QE_PLACE_INIT stores D into c (QE_F32 or QE_BF16);
  * QE_PLACE_ACCUM adds it in FP32 (c must be QE_F32): c = fl32(c + D).  Only
  * the m x n view c[i * ldc + j] is read or written.  F (Y = X W^T), dI

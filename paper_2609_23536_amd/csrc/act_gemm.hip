@@ -1,6 +1,7 @@
 // FP8 products whose epilogue goes on past the sum (gfx950):
-//     plain:  Z = 2^(ea + eb) A B^T + bias,  D = act(Z) + residual
-//     gated:  G = 2^(ea + eg) A Bg^T,  U = 2^(ea + eu) A Bu^T,  D = act(G) * U
+//     plain:  Z = s A B^T + bias,  D = act(Z) + residual
+//     gated:  G = sg A Bg^T,  U = su A Bu^T,  D = act(G) * U
+// (s, sg, su: the products of the operands' scale inverses, sum_scale)
 // and, for a backward pass, Z (or G and U) saved beside D in BF16 or 8 bits
 // (act.h).  Everything after the sums stays in registers and FP32; D is rounded
 // once.
@@ -320,9 +321,7 @@ struct Quads {
   }
 };
 
-__device__ __forceinline__ v4f ldexp4(v4f a, int e) {
-  return v4f{__builtin_ldexpf(a[0], e), __builtin_ldexpf(a[1], e), __builtin_ldexpf(a[2], e), __builtin_ldexpf(a[3], e)};
-}
+__device__ __forceinline__ v4f scaled(v4f a, SumScale s) { return v4f{s(a[0]), s(a[1]), s(a[2]), s(a[3])}; }
 
 struct TilePlace {
   int64_t m0, n0;  // first row, first output column
@@ -382,8 +381,7 @@ __global__ __launch_bounds__(256) void act_large_kernel(ActGemmParams g, int til
 
   __syncthreads();  // every wave is done reading the last stage
   const int fr = lane & 15, fq = lane >> 4;
-  const int e0 = pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b_scale_inv);
-  const int e1 = GATED ? pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b2_scale_inv) : e0;
+  const SumScale s0 = sum_scale(g.a_scale_inv, g.b_scale_inv), s1 = GATED ? sum_scale(g.a_scale_inv, g.b2_scale_inv) : s0;
   // A tile finishes in the accumulators' own layout, where a lane holds four
   // neighbouring outputs of one row (and their gates beside their ups), a block
   // of rows at a time; only what is stored goes through LDS.  The residual is
@@ -432,10 +430,10 @@ __global__ __launch_bounds__(256) void act_large_kernel(ActGemmParams g, int til
 #pragma unroll
         for (int j = 0; j < QV; ++j) {
           if constexpr (GATED) {
-            z[h][j] = ldexp4(acc[i + h][2 * j], e0);
-            up[h][j] = ldexp4(acc[i + h][2 * j + 1], e1);
+            z[h][j] = scaled(acc[i + h][2 * j], s0);
+            up[h][j] = scaled(acc[i + h][2 * j + 1], s1);
           } else {
-            z[h][j] = ldexp4(acc[i + h][j], e0) + bias[j];
+            z[h][j] = scaled(acc[i + h][j], s0) + bias[j];
           }
           if constexpr (EDGE) {  // columns past the last one count as zero in their group
             const int nv = cols - 16 * j - 4 * fq;
@@ -526,8 +524,7 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void act_r
 
   float *ep = reinterpret_cast<float *>(smem);
   const int fr = lane & 15, fq = lane >> 4;
-  const int e0 = pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b_scale_inv);
-  const int e1 = GATED ? pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b2_scale_inv) : e0;
+  const SumScale s0 = sum_scale(g.a_scale_inv, g.b_scale_inv), s1 = GATED ? sum_scale(g.a_scale_inv, g.b2_scale_inv) : s0;
   constexpr int RW = ER < TM ? ER : TM;  // rows a wave stages per pass
 #pragma unroll
   for (int p = 0; p < BM / ER; ++p) {
@@ -538,9 +535,8 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void act_r
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           const v4f a = acc[TM < ER ? i : (p * ER % TM) / 16 + i][j];
-          const int e = j % 2 == 0 ? e0 : e1;
           *reinterpret_cast<v4f *>(ep + ((TM < ER ? wm * TM : 0) + i * 16 + fr) * EP + wn * TN + j * 16 + 4 * fq) =
-              v4f{__builtin_ldexpf(a[0], e), __builtin_ldexpf(a[1], e), __builtin_ldexpf(a[2], e), __builtin_ldexpf(a[3], e)};
+              scaled(a, j % 2 == 0 ? s0 : s1);
         }
     }
     __syncthreads();
@@ -620,8 +616,7 @@ __global__ __launch_bounds__(64 * W) void act_rows_kernel(ActGemmParams g, int b
         acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u][j], fa[u], acc[j], FB, FA, 0, 0, 0, 0);
     }
   }
-  const int e0 = pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b_scale_inv);
-  const int e1 = GATED ? pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b2_scale_inv) : e0;
+  const SumScale s0 = sum_scale(g.a_scale_inv, g.b_scale_inv), s1 = GATED ? sum_scale(g.a_scale_inv, g.b2_scale_inv) : s0;
 #pragma unroll
   for (int j = 0; j < NB; ++j) *reinterpret_cast<v4f *>(sums[wave] + fr * EP + 16 * j + 4 * fq) = acc[j];
   __syncthreads();
@@ -631,9 +626,8 @@ __global__ __launch_bounds__(64 * W) void act_rows_kernel(ActGemmParams g, int b
     v4f s = *reinterpret_cast<const v4f *>(sums[0] + row * EP + col);
 #pragma unroll
     for (int w = 1; w < W; ++w) s += *reinterpret_cast<const v4f *>(sums[w] + row * EP + col);
-    const int e = (col / 16) % 2 == 0 ? e0 : e1;
-    *reinterpret_cast<v4f *>(sums[0] + row * EP + col) =
-        v4f{__builtin_ldexpf(s[0], e), __builtin_ldexpf(s[1], e), __builtin_ldexpf(s[2], e), __builtin_ldexpf(s[3], e)};
+    const bool second = (col / 16) % 2 != 0;
+    *reinterpret_cast<v4f *>(sums[0] + row * EP + col) = scaled(s, SumScale{second ? s1.a : s0.a, second ? s1.b : s0.b});
   }
   __syncthreads();
   if (threadIdx.x < 64) finish_rows<GATED, 16, 16 * OB, 64, EP>(g, sums[0], lane, m0, n0);

@@ -6,9 +6,10 @@
 // the same "TN" product with both operands contiguous along the reduction:
 //     D[i][j] = 2^(ea + eb) * sum_r A[i][r] B[j][r]
 // where 2^ea, 2^eb are the operands' scale inverses (powers of two, so the
-// rescale is one exact ldexp).  The epilogue stores D (FP32 or BF16), or adds
-// it to an FP32 destination in place: the direct placement of dW into its
-// slice of the flat main-gradient buffer (§3.4), with no staging copy.
+// rescale is exact; other values are multiplied in as they are).  The epilogue
+// stores D (FP32 or BF16), or adds it to an FP32 destination in place: the direct
+// placement of dW into its slice of the flat main-gradient buffer (§3.4), with no
+// staging copy.
 //
 // gemm_tn_w4_kernel serves the large tiles, 256 x 256 x 128 (and 256 x 224,
 // 256 x 192, 192 x 256); gemm_ring.hip the small ones.  Every shape uses
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(256) void gemm_tn_w4_kernel(GemmParams g, int tiles
   // 32 lanes x 16 B cover one 512-byte output row run per store instruction.
   __syncthreads();  // every wave is done reading the last stage
   float *ep = reinterpret_cast<float *>(smem) + wave * 32 * EP;
-  const int e = pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b_scale_inv);
+  const SumScale scale = sum_scale(g.a_scale_inv, g.b_scale_inv);
   const bool nfull = n0 + BN <= N;
   // Full tile with a vector-aligned destination (the common case): no bounds
   // checks, every store address is a uniform row base (scalar registers) plus
@@ -205,8 +206,7 @@ __global__ __launch_bounds__(256) void gemm_tn_w4_kernel(GemmParams g, int tiles
           for (int j = 0; j < J; ++j) {
             const v4f a = acc[2 * i + h][j];
             *reinterpret_cast<uint2 *>(ehw + h * 16 * EPH + j * 16) =
-                make_uint2(bf16x2_bits(__builtin_ldexpf(a[0], e), __builtin_ldexpf(a[1], e)),
-                           bf16x2_bits(__builtin_ldexpf(a[2], e), __builtin_ldexpf(a[3], e)));
+                make_uint2(bf16x2_bits(scale(a[0]), scale(a[1])), bf16x2_bits(scale(a[2]), scale(a[3])));
           }
         const uint16_t *ehr = eh + (lane >> 4) * EPH + (lane & 15) * 8;
         const uint32_t voffh = uint32_t((lane >> 4) * g.ldc + (lane & 15) * 8) * 2u;
@@ -226,8 +226,8 @@ __global__ __launch_bounds__(256) void gemm_tn_w4_kernel(GemmParams g, int tiles
 #pragma unroll
       for (int j = 0; j < J; ++j)
         *reinterpret_cast<float4 *>(ew + h * 16 * EP + j * 16) =
-            make_float4(__builtin_ldexpf(acc[2 * i + h][j][0], e), __builtin_ldexpf(acc[2 * i + h][j][1], e),
-                        __builtin_ldexpf(acc[2 * i + h][j][2], e), __builtin_ldexpf(acc[2 * i + h][j][3], e));
+            make_float4(scale(acc[2 * i + h][j][0]), scale(acc[2 * i + h][j][1]), scale(acc[2 * i + h][j][2]),
+                        scale(acc[2 * i + h][j][3]));
     // same wave writes then reads its own LDS rows: LDS operations of one wave
     // complete in order
     if (fast) {

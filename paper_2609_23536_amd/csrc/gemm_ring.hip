@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void gemm_
   // reads its destination before it stages its rows, all loads in flight.
   // Accesses are non-temporal, as in the large tiles, unless launch_ring says
   // otherwise.
-  const int e = pow2_exponent(g.a_scale_inv) + pow2_exponent(g.b_scale_inv);
+  const SumScale scale = sum_scale(g.a_scale_inv, g.b_scale_inv);
   float *ep = reinterpret_cast<float *>(smem);
   constexpr int RW = ER < TM ? ER : TM;  // rows a wave stages per pass
   constexpr int NQ = ER * BN / 4 / 256;  // column quads per lane and pass
@@ -126,8 +126,7 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void gemm_
         for (int j = 0; j < J; ++j) {
           const v4f a = acc[TM < ER ? i : (p * ER % TM) / 16 + i][j];
           *reinterpret_cast<float4 *>(ep + ((TM < ER ? wm * TM : 0) + i * 16 + fr) * EP + wn * TN + j * 16 + 4 * fq) =
-              make_float4(__builtin_ldexpf(a[0], e), __builtin_ldexpf(a[1], e), __builtin_ldexpf(a[2], e),
-                          __builtin_ldexpf(a[3], e));
+              make_float4(scale(a[0]), scale(a[1]), scale(a[2]), scale(a[3]));
         }
     }
     __syncthreads();

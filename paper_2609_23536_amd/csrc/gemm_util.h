@@ -69,7 +69,23 @@ __device__ __forceinline__ uint4 mask_tail(uint4 v, int64_t valid) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-__device__ __forceinline__ int pow2_exponent(const float *p) { return int((__float_as_uint(*p) >> 23) & 0xffu) - 127; }
+// The product of two operands' scale inverses, m 2^e, as two factors that a sum is
+// multiplied by in turn: m 2^f and 2^(e - f), f half of e, so that the first
+// product neither overflows nor loses bits where the result does not.  Where both
+// inverses are powers of two, which the scale update makes them, m = 1 and the
+// result is the sum's ldexp; otherwise m and the product with it are rounded once
+// each.  (Under a branch for m != 1 the large tiles' accumulators spill.  Against
+// one ldexp, MI355X: level on the stages' products, 4096 x 14336 x 256 37.3 -> 38.3 us.)
+struct SumScale {
+  float a, b;
+  __device__ __forceinline__ float operator()(float sum) const { return sum * a * b; }
+};
+__device__ __forceinline__ SumScale sum_scale(const float *a_inv, const float *b_inv) {
+  const float x = *a_inv, y = *b_inv;
+  const float m = 2.0f * __builtin_amdgcn_frexp_mantf(x) * (2.0f * __builtin_amdgcn_frexp_mantf(y));
+  const int e = __builtin_amdgcn_frexp_expf(x) + __builtin_amdgcn_frexp_expf(y) - 2;
+  return {__builtin_ldexpf(m, e >> 1), __builtin_ldexpf(1.0f, e - (e >> 1))};
+}
 
 // Workgroups are dealt to the 8 XCDs round-robin; renumber so that each XCD
 // gets a contiguous range of tiles (shared A rows / B columns stay in one L2).

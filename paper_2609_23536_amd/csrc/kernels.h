@@ -140,7 +140,7 @@ struct QuantParams {
   float *snapshot;
 };
 
-// D = 2^(ea+eb) * sum_r A[i][r] B[j][r];  out = D (INIT) or out + D (ACCUM).
+// D = a_inv b_inv * sum_r A[i][r] B[j][r];  out = D (INIT) or out + D (ACCUM).
 struct GemmParams {
   const uint8_t *a;
   const uint8_t *b;
@@ -170,8 +170,8 @@ struct SavedRef {
   int32_t pad;
 };
 
-// Product with an epilogue: Z = 2^(ea + eb) A B^T + bias, D = act(Z) + residual;
-// gated (b2 set): D = act(2^(ea + eb) A B^T) * 2^(ea + eb2) A B2^T.
+// Product with an epilogue: Z = a_inv b_inv A B^T + bias, D = act(Z) + residual;
+// gated (b2 set): D = act(a_inv b_inv A B^T) * (a_inv b2_inv A B2^T).
 struct ActGemmParams {
   const uint8_t *a, *b, *b2;
   int64_t lda, ldb;

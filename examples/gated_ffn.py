@@ -27,6 +27,13 @@ def _ok(status):
         raise RuntimeError(status)
 
 
+def _check(name, t, rows, cols, *dtypes):
+    """The library sees an address: a tensor of another size, type or stride would be misread, or read and written past."""
+    if tuple(t.shape) != (rows, cols) or t.dtype not in dtypes or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s: want a contiguous [%d, %d] tensor of %s on the GPU, got %s of %s" % (
+            name, rows, cols, " or ".join(str(d) for d in dtypes), list(t.shape), t.dtype))
+
+
 def _ld(v):
     return (v + 15) // 16 * 16 if v <= 256 else (v + 127) // 128 * 128  # whole lines for long rows
 
@@ -49,7 +56,8 @@ class Role:
 
     def cast(self, x, rows=None, transposed=True):
         dt = qe.BF16 if x.dtype == torch.bfloat16 else qe.F32
-        _ok(qe.qe_quantize_fp8(x, dt, rows or self.rows, self.cols, self.meta, self.row, self.row.shape[1],
+        rows = self.rows if rows is None else rows
+        _ok(qe.qe_quantize_fp8(x, dt, rows, self.cols, self.meta, self.row, self.row.shape[1],
                                self.col if transposed else None, self.col.shape[1] if transposed else 0, self.inv))
 
 
@@ -60,6 +68,8 @@ class GatedFFN:
         self.act, self.tokens = act, tokens
         self.ffn, self.hidden = wd.shape[1], wd.shape[0]
         t, f, d = tokens, self.ffn, self.hidden
+        _check("wg_wu", wg_wu, 2 * f, d, torch.bfloat16, torch.float32)
+        _check("wd", wd, d, f, torch.bfloat16, torch.float32)
         self.wgu_master, self.wd_master = wg_wu, wd
         self.wgu, self.wd = Role(2 * f, d, qe.E4M3), Role(d, f, qe.E4M3)
         self.x, self.h_q = Role(t, d, qe.E4M3), Role(t, f, qe.E4M3)
@@ -91,6 +101,7 @@ class GatedFFN:
                                qe.make_epilogue(residual=x, residual_dtype=qe.BF16, ld_residual=d), self.y, qe.BF16, d))
 
     def forward(self, x):
+        _check("x", x, self.tokens, self.hidden, torch.bfloat16)
         self.x.cast(x)
         self._up(self.tokens, self.saved)
         self.h_q.cast(self.h)
@@ -101,6 +112,9 @@ class GatedFFN:
     def serve(self, x):
         """A few tokens, nothing kept for a backward pass and no scale moved."""
         n = x.shape[0]
+        if n > self.tokens:
+            raise ValueError("%d tokens in buffers for %d" % (n, self.tokens))
+        _check("x", x, n, self.hidden, torch.bfloat16)
         self.x.cast(x, n, transposed=False)
         self._up(n, (None, None))
         self.h_q.cast(self.h, n, transposed=False)
@@ -113,6 +127,7 @@ class GatedFFN:
 
     def backward(self, dy):
         t, f, d = self.tokens, self.ffn, self.hidden
+        _check("dy", dy, t, d, torch.bfloat16)
         self.dy.cast(dy)
         self._product(self.dy.row, self.dy.fmt, self.wd.col, self.wd.fmt, t, f, d, (self.dy.inv, self.wd.inv), self.dh, qe.BF16, f)
         _ok(qe.qe_act_grad(self.dh, qe.BF16, f, t, f, self.act, self.saved[0], self.saved[1], meta=self.dgu.meta,

@@ -39,32 +39,37 @@ def _ld(v):
 
 
 class Role:
-    """One tensor's FP8 codes, row-wise and transposed, and its delayed-scaling state."""
+    """One tensor's FP8 codes, row-wise and transposed, and its delayed-scaling state.
 
-    def __init__(self, rows, cols, fmt, history=16):
+    With `reads`, another role: codes (row-wise only) and amaxes of its own, cast with that role's scale.
+    """
+
+    def __init__(self, rows, cols, fmt, history=16, reads=None):
         self.rows, self.cols, self.fmt = rows, cols, fmt
         self.row = torch.zeros((rows, _ld(cols)), dtype=torch.uint8, device="cuda")
-        self.col = torch.zeros((cols, _ld(rows)), dtype=torch.uint8, device="cuda")
+        self.col = torch.zeros((cols, _ld(rows)), dtype=torch.uint8, device="cuda") if reads is None else None
         self.hist = torch.zeros(history, dtype=torch.float32, device="cuda")
         self.scales = torch.ones(3, dtype=torch.float32, device="cuda")  # scale, its inverse, the inverse of the codes' own
         self.accum = torch.zeros(qe.AMAX_LINES * qe.AMAX_STRIDE, dtype=torch.float32, device="cuda")
-        self.meta = qe.make_meta(self.hist, self.scales[0:1], self.scales[1:2], fmt, 0, self.accum)
+        scales = self.scales if reads is None else reads.scales
+        self.meta = qe.make_meta(self.hist, scales[0:1], scales[1:2], fmt, 0, self.accum)
 
     @property
     def inv(self):
         return self.scales[2:3]
 
-    def cast(self, x, rows=None, transposed=True):
+    def cast(self, x, rows=None):
         dt = qe.BF16 if x.dtype == torch.bfloat16 else qe.F32
         rows = self.rows if rows is None else rows
-        _ok(qe.qe_quantize_fp8(x, dt, rows, self.cols, self.meta, self.row, self.row.shape[1],
-                               self.col if transposed else None, self.col.shape[1] if transposed else 0, self.inv))
+        _ok(qe.qe_quantize_fp8(x, dt, rows, self.cols, self.meta, self.row, self.row.shape[1], self.col,
+                               0 if self.col is None else self.col.shape[1], self.inv))
 
 
 class GatedFFN:
-    """Weights of one block and the buffers of one microbatch of `tokens`."""
+    """Weights of one block, the buffers of one microbatch of `tokens` and, apart from those, of up to `serve_tokens` served
+    together (`tokens` if not given)."""
 
-    def __init__(self, wg_wu, wd, tokens, act=qe.ACT_SILU):
+    def __init__(self, wg_wu, wd, tokens, act=qe.ACT_SILU, serve_tokens=None):
         self.act, self.tokens = act, tokens
         self.ffn, self.hidden = wd.shape[1], wd.shape[0]
         t, f, d = tokens, self.ffn, self.hidden
@@ -82,6 +87,10 @@ class GatedFFN:
         self.codes = torch.zeros((2, t, f), dtype=torch.int8, device="cuda")
         self.exps = torch.zeros((2, t, groups), dtype=torch.uint8, device="cuda")
         self.saved = [qe.make_saved(qe.SAVED_I8, self.codes[i], f, self.exps[i], groups) for i in range(2)]
+        # served tokens leave no trace in a training step: codes, outputs and amaxes of their own
+        self.serve_tokens = n = t if serve_tokens is None else serve_tokens
+        self.serve_x, self.serve_h_q = Role(n, d, qe.E4M3, reads=self.x), Role(n, f, qe.E4M3, reads=self.h_q)
+        self.serve_h, self.serve_y = torch.zeros((n, f), **bf), torch.zeros((n, d), **bf)
 
     def refresh(self):
         """After an optimizer step: the weights' codes, and the scales of the next ones."""
@@ -89,37 +98,38 @@ class GatedFFN:
         self.wd.cast(self.wd_master)
         _ok(qe.qe_amax_scale_update([self.wgu.meta, self.wd.meta]))
 
-    def _up(self, rows, saved):
+    def _up(self, x, h, rows, saved):
         f, w = self.ffn, self.wgu
-        _ok(qe.qe_fp8_gemm_gated(self.x.row, self.x.fmt, self.x.row.shape[1], w.row, w.row[f:], w.fmt, w.row.shape[1], rows,
-                                 f, self.hidden, self.x.inv, w.inv, w.inv, self.act, self.h, qe.BF16, f, saved[0], saved[1]))
+        _ok(qe.qe_fp8_gemm_gated(x.row, x.fmt, x.row.shape[1], w.row, w.row[f:], w.fmt, w.row.shape[1], rows, f, self.hidden,
+                                 x.inv, w.inv, w.inv, self.act, h, qe.BF16, f, saved[0], saved[1]))
 
-    def _down(self, x, rows):
+    def _down(self, h_q, residual, y, rows):
         d, w = self.hidden, self.wd
-        _ok(qe.qe_fp8_gemm_act(self.h_q.row, self.h_q.fmt, self.h_q.row.shape[1], w.row, w.fmt, w.row.shape[1], rows, d,
-                               self.ffn, self.h_q.inv, w.inv,
-                               qe.make_epilogue(residual=x, residual_dtype=qe.BF16, ld_residual=d), self.y, qe.BF16, d))
+        _ok(qe.qe_fp8_gemm_act(h_q.row, h_q.fmt, h_q.row.shape[1], w.row, w.fmt, w.row.shape[1], rows, d, self.ffn, h_q.inv,
+                               w.inv, qe.make_epilogue(residual=residual, residual_dtype=qe.BF16, ld_residual=d), y, qe.BF16,
+                               d))
 
     def forward(self, x):
         _check("x", x, self.tokens, self.hidden, torch.bfloat16)
         self.x.cast(x)
-        self._up(self.tokens, self.saved)
+        self._up(self.x, self.h, self.tokens, self.saved)
         self.h_q.cast(self.h)
-        self._down(x, self.tokens)
+        self._down(self.h_q, x, self.y, self.tokens)
         _ok(qe.qe_amax_scale_update([self.x.meta, self.h_q.meta]))
         return self.y
 
     def serve(self, x):
-        """A few tokens, nothing kept for a backward pass and no scale moved."""
+        """A few tokens, nothing kept for a backward pass and no scale moved: with the scales of the last training step, and
+        between a forward and its backward as well as anywhere else."""
         n = x.shape[0]
-        if n > self.tokens:
-            raise ValueError("%d tokens in buffers for %d" % (n, self.tokens))
+        if n > self.serve_tokens:
+            raise ValueError("%d tokens in buffers for %d" % (n, self.serve_tokens))
         _check("x", x, n, self.hidden, torch.bfloat16)
-        self.x.cast(x, n, transposed=False)
-        self._up(n, (None, None))
-        self.h_q.cast(self.h, n, transposed=False)
-        self._down(x, n)
-        return self.y[:n]
+        self.serve_x.cast(x, n)
+        self._up(self.serve_x, self.serve_h, n, (None, None))
+        self.serve_h_q.cast(self.serve_h, n)
+        self._down(self.serve_h_q, x, self.serve_y, n)
+        return self.serve_y[:n]
 
     @staticmethod
     def _product(a, a_t, b, b_t, m, n, k, inv, out, dtype, ld):

@@ -650,7 +650,8 @@ bool few_blocks(const ActGemmParams &p) {
   const bool gated = p.b2 != nullptr, wide = p.z.kind == kSavedI8;
   const int64_t blocks = (p.m + 15) / 16 * ((p.n + (wide ? 31 : 15)) / (wide ? 32 : 16));
   if (p.k <= 1024 || (gated && wide)) return false;
-  return blocks <= 256 || (blocks <= 512 && p.k > 12288 && !gated && !wide);
+  const int64_t cus = compute_units();
+  return blocks <= cus || (blocks <= 2 * cus && p.k > 12288 && !gated && !wide);
 }
 
 // One workgroup for 16 outputs (32 where they are saved in 8 bits, whose groups

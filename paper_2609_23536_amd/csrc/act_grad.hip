@@ -427,13 +427,13 @@ hipError_t launch_kind(int rows, const ActGradParams &p, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_act_grad(const ActGradParams &p, float *dbias, bool accumulate, hipStream_t s) {
-  // Up to 1024 tiles of 128 rows (four a unit, what its registers hold) the tiles
-  // take 64 rows and twice the lanes: shorter chains, more waves to overlap them.
+  // Up to four tiles of 128 rows a unit (what its registers hold) the tiles take 64
+  // rows and twice the lanes: shorter chains, more waves to overlap them.
   // MI355X, us with 128 / 64 rows: gated 1024 x 14336 (896 tiles) 31.3 / 29.2, 4096 x 4096
   // (1024) 34.8 / 33.1, 1000 x 9000 FP32 with dense values and bias (568) 38.0 / 30.4;
   // beyond, the shorter runs of transposed codes cost more: 2048 x 10240 (1280) 59.2 /
   // 63.3, 2048 x 14336 (1792) 54.5 / 59.8.
-  const int rows = ((p.rows + 127) / 128) * ((p.cols + kTile - 1) / kTile) <= 1024 ? 64 : 128;
+  const int rows = ((p.rows + 127) / 128) * ((p.cols + kTile - 1) / kTile) <= 4 * compute_units() ? 64 : 128;
   if ((p.rows > 0 && p.cols > 0) || p.snapshot != nullptr) {
     const hipError_t e = p.u.kind != kSavedNone ? launch_kind<true>(rows, p, s) : launch_kind<false>(rows, p, s);
     if (e != hipSuccess) return e;

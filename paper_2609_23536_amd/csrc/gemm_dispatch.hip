@@ -91,7 +91,7 @@ constexpr ManyRounds kManyRounds[] = {
 static std::atomic<int> g_tile_override{0};
 
 // Compute units of the current device, read once per device from its properties; 256 on MI355X.
-static int cu_count() {
+int compute_units() {
   constexpr int kMaxDevices = 64;
   static std::atomic<int> cache[kMaxDevices];
   int dev = 0;
@@ -105,7 +105,7 @@ static int cu_count() {
 
 int choose_gemm_tile(const GemmParams &g, unsigned allowed) {
   const int64_t cbytes = g.out == 1 ? 2 : 4;
-  const int64_t cus = cu_count();
+  const int64_t cus = compute_units();
   const double T = double((g.k + 127) / 128);
   auto tiles = [&](int64_t bm, int64_t bn) { return ((g.m + bm - 1) / bm) * ((g.n + bn - 1) / bn); };
   const bool scalar = !gemm_vec_ok(g);

@@ -292,6 +292,7 @@ enum GemmTile {
 // as in launch_gemm.
 hipError_t launch_gemm_large(int tile, const GemmParams &g, hipStream_t s, const UpdateParams &u);
 hipError_t launch_gemm_ring(int tile, const GemmParams &g, hipStream_t s, const UpdateParams &u);
+int compute_units();  // of the current device
 // The tile shape the cost model expects to be fastest among those whose bit
 // (1 << GemmTile) is set in `allowed`.
 int choose_gemm_tile(const GemmParams &g, unsigned allowed);

@@ -8,6 +8,7 @@
 // call is in a text log.  Device addresses are numbers, never memory.
 #include <hip/hip_runtime_api.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <map>
@@ -133,15 +134,19 @@ void __hipUnregisterFatBinary(void **) {}
 hipError_t __hipPopCallConfiguration(dim3 *, dim3 *, size_t *, hipStream_t *) { return hipErrorUnknown; }
 
 // ---- device, memory
+static int units() {  // compute units: 256, as on MI355X, unless the test says otherwise
+  const char *s = getenv("FAKE_HIP_UNITS");
+  return s != nullptr ? atoi(s) : 256;
+}
 hipError_t hipGetDevice(int *d) { return *d = 0, hipSuccess; }
 hipError_t hipSetDevice(int) { return hipSuccess; }
 hipError_t hipGetDevicePropertiesR0600(hipDeviceProp_tR0600 *p, int) {
   memset(p, 0, sizeof(*p));
   strcpy(p->gcnArchName, "gfx950:sramecc+:xnack-");
-  p->multiProcessorCount = 256;
+  p->multiProcessorCount = units();
   return hipSuccess;
 }
-hipError_t hipDeviceGetAttribute(int *v, hipDeviceAttribute_t, int) { return *v = 256, hipSuccess; }
+hipError_t hipDeviceGetAttribute(int *v, hipDeviceAttribute_t, int) { return *v = units(), hipSuccess; }
 hipError_t hipMalloc(void **p, size_t bytes) {
   *p = reinterpret_cast<void *>(g_next);
   g_next += (bytes + 511) / 256 * 256;

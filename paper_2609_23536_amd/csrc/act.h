@@ -27,12 +27,13 @@ constexpr float kGeluB = 0.044715f;
 constexpr float kGeluFar = 256.0f;  // z^2 from which P is 0 or 1 in 32 bits; keeps z P (1 - P) z^2 off 0 * inf
 
 // Phi(z) and e = exp(-z^2 / 2), without a branch.  |z| < 1.5: Taylor's series of
-// Phi(z) - 1/2 to z^21 (the next term is below 2e-10).  Beyond, on the negative
-// side, where nothing may cancel: Phi(-a) = t P(t) e with t = 1 / (1 + 0.45 a), P of
-// degree 6 fitted to Phi(-a) / (t e) over a >= 1.5, relative error below 2.5e-7
-// there.  Off by at most 7.1e-8 over all FP32 z in -9 .. 9, as erf in FP32 is (6.1e-8;
-// the shorter form of Abramowitz and Stegun 7.1.26, off by 7.5e-8 before rounding,
-// moved ten times as many FP8 codes of a gradient as erf did).
+// Phi(z) - 1/2 to z^21 (the next term is below 2.4e-9; with coefficients of FP32 the
+// sum is off by 1.0e-8).  Beyond, on the negative side, where nothing may cancel:
+// Phi(-a) = t P(t) e with t = 1 / (1 + 0.45 a), P of degree 6 fitted to Phi(-a) / (t e)
+// over a >= 1.5, relative error below 2.6e-7 there.  With its roundings off by at
+// most 7.1e-8 over z in -9 .. 9, as erf in FP32 is (6.1e-8; the shorter form of
+// Abramowitz and Stegun 7.1.26, off by 7.5e-8 before rounding, moved ten times as
+// many FP8 codes of a gradient as erf did).
 __device__ __forceinline__ float normal_cdf(float z, float &e) {
   const float q = z * z, a = __builtin_fabsf(z);
   float c = 5.112434781e-12f;

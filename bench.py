@@ -87,15 +87,18 @@ def parse():
 
 CSRC = os.path.join(ROOT, "paper_2609_23536_amd", "csrc")
 GEMM_SOURCES = ("gemm_fp8.hip", "gemm_ring.hip", "gemm_loops.h", "gemm_dispatch.hip", "gemm_util.h")
+GEMM_SHARED = ("bf16.h",)  # code of the GEMM kernels that other kernels include too
 
 
 def gemm_source_sha256(csrc=CSRC):
-    """Of the GEMM's source files without comments and blank space: what was measured on other comments holds."""
+    """Of the GEMM's source files without comments and blank space: what was measured on other comments holds.  A shared
+    header that `csrc` does not hold is read from the package."""
     import hashlib
     import re
     h = hashlib.sha256()
-    for name in GEMM_SOURCES:
-        text = open(os.path.join(csrc, name)).read()
+    for name in GEMM_SOURCES + GEMM_SHARED:
+        path = os.path.join(csrc, name)
+        text = open(path if os.path.exists(path) or name in GEMM_SOURCES else os.path.join(CSRC, name)).read()
         code = re.sub(r'"(?:\\.|[^"\\])*"|//[^\n]*|/\*.*?\*/', lambda m: m[0] if m[0][0] == '"' else " ", text, flags=re.S)
         h.update("".join(code.split()).encode() + b"\n")
     return h.hexdigest()

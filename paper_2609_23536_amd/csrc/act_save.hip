@@ -5,7 +5,13 @@
 // other way round.  A workgroup takes 64 rows x 128 columns, a lane eight
 // columns of every sixteenth row, all four loads in flight: a group is four
 // neighbouring lanes, which share its maximum by lane permutes.  MI355X, BF16 4096 x
-// 14336: saved in 35 us (5.0 TB/s), restored in 29 (6.1).
+// 14336: saved in 36 us (5.0 TB/s), restored in 29 (6.1).
+//
+// All accesses are ordinary: what is saved was written by the kernel before and
+// is read again by the one after.  With non-temporal loads, MI355X, us from one to
+// the other, ordinary / so: BF16 save 4096 x 14336 35.8 / 34.7, with the cast
+// of the same tensor after it 74.1 / 79.9; 8192 x 28672 134 / 127 and 299 / 301; FP32
+// 4096 x 14336 60.9 / 69.5 and 115 / 133.
 #include "act.h"
 
 namespace qe {
@@ -21,14 +27,13 @@ struct Eight {
 // Eight values of a row at `at`, of which nv exist (all, if FULL; the others
 // read as zero).  Where some do not exist the last one is read again in their
 // place, so that no load waits for another.
-template <bool BF16, bool FULL, bool NT>
+template <bool BF16, bool FULL>
 __device__ __forceinline__ Eight load8(const void *base, int64_t at, int nv) {
   Eight r = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
   if constexpr (BF16) {
     const uint16_t *p = static_cast<const uint16_t *>(base) + at;
     if (FULL || nv == 8) {
-      const u32x4_in *v = reinterpret_cast<const u32x4_in *>(p);
-      const u32x4_in w = NT ? __builtin_nontemporal_load(v) : *v;
+      const u32x4_in w = *reinterpret_cast<const u32x4_in *>(p);
       r.a = f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16),
                   __uint_as_float(w[1] & 0xffff0000u)};
       r.b = f32x4{__uint_as_float(w[2] << 16), __uint_as_float(w[2] & 0xffff0000u), __uint_as_float(w[3] << 16),
@@ -43,9 +48,8 @@ __device__ __forceinline__ Eight load8(const void *base, int64_t at, int nv) {
   } else {
     const float *p = static_cast<const float *>(base) + at;
     if (FULL || nv == 8) {
-      const f32x4_in *v = reinterpret_cast<const f32x4_in *>(p), *w = reinterpret_cast<const f32x4_in *>(p + 4);
-      r.a = NT ? __builtin_nontemporal_load(v) : *v;
-      r.b = NT ? __builtin_nontemporal_load(w) : *w;
+      r.a = *reinterpret_cast<const f32x4_in *>(p);
+      r.b = *reinterpret_cast<const f32x4_in *>(p + 4);
     } else if (nv > 0) {
       float x[8];
 #pragma unroll
@@ -57,13 +61,13 @@ __device__ __forceinline__ Eight load8(const void *base, int64_t at, int nv) {
   return r;
 }
 
-template <bool BF16, bool FULL, bool NT>
+template <bool BF16, bool FULL>
 __device__ __forceinline__ void save_tile(const SaveParams &p, int64_t row0, int64_t col) {
   const int nc = FULL ? 8 : int(p.cols - col < 0 ? 0 : (p.cols - col > 8 ? 8 : p.cols - col));
   Eight x[kSteps];
 #pragma unroll
   for (int st = 0; st < kSteps; ++st)
-    x[st] = load8<BF16, FULL, NT>(p.x, (row0 + st * 16) * p.ld + col, FULL || row0 + st * 16 < p.rows ? nc : 0);
+    x[st] = load8<BF16, FULL>(p.x, (row0 + st * 16) * p.ld + col, FULL || row0 + st * 16 < p.rows ? nc : 0);
   uint32_t byte[kSteps], most = 0u;
 #pragma unroll
   for (int st = 0; st < kSteps; ++st) {
@@ -147,16 +151,16 @@ __device__ __forceinline__ void restore_tile(const SaveParams &p, int64_t row0, 
   }
 }
 
-template <bool SAVE, bool BF16, bool NT>
+template <bool SAVE, bool BF16>
 __global__ __launch_bounds__(kThreads) void act_checkpoint_kernel(SaveParams p, int64_t tiles_c) {
   const int64_t r0 = int64_t(blockIdx.x) / tiles_c * kRows, c0 = int64_t(blockIdx.x) % tiles_c * kTile;
   const int64_t row = r0 + (threadIdx.x >> 4), col = c0 + (threadIdx.x & 15) * 8;
   const bool full = r0 + kRows <= p.rows && c0 + kTile <= p.cols;
   if constexpr (SAVE) {
     if (full)
-      save_tile<BF16, true, NT>(p, row, col);
+      save_tile<BF16, true>(p, row, col);
     else
-      save_tile<BF16, false, NT>(p, row, col);
+      save_tile<BF16, false>(p, row, col);
   } else {
     if (full)
       restore_tile<BF16, true>(p, row, col);
@@ -171,16 +175,8 @@ hipError_t launch_tiles(const SaveParams &p, hipStream_t s) {
   const int64_t tiles_c = (p.cols + kTile - 1) / kTile, tiles = (p.rows + kRows - 1) / kRows * tiles_c;
   if (tiles >= int64_t(1) << 31) return hipErrorInvalidValue;
   const dim3 grid{unsigned(tiles)}, block(kThreads);
-  // A save reads non-temporally what the 256 MB memory-side cache will hardly
-  // hold, with its codes, from the pass before.  MI355X, us non-temporal /
-  // ordinary: FP32 1500 x 4099 (31 MB) 11.9 / 9.4, 2048 x 14336 (148 MB) 33.1 / 31.1,
-  // BF16 4096 x 14336 (178 MB) 35.8 / 41.9, 8192 x 28672 132 / 150.  Restores: ordinary
-  // is as fast or faster (8192 x 28672 139 / 126).
-  if (SAVE && p.rows * p.cols * (p.x_bf16 ? 3 : 5) > (int64_t(160) << 20))
-    return p.x_bf16 ? klaunch(act_checkpoint_kernel<SAVE, true, SAVE>, grid, block, 0, s, p, tiles_c)
-                    : klaunch(act_checkpoint_kernel<SAVE, false, SAVE>, grid, block, 0, s, p, tiles_c);
-  return p.x_bf16 ? klaunch(act_checkpoint_kernel<SAVE, true, false>, grid, block, 0, s, p, tiles_c)
-                  : klaunch(act_checkpoint_kernel<SAVE, false, false>, grid, block, 0, s, p, tiles_c);
+  return p.x_bf16 ? klaunch(act_checkpoint_kernel<SAVE, true>, grid, block, 0, s, p, tiles_c)
+                  : klaunch(act_checkpoint_kernel<SAVE, false>, grid, block, 0, s, p, tiles_c);
 }
 
 }  // namespace

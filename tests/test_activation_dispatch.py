@@ -40,3 +40,19 @@ def test_limits_follow_the_compute_units(units, monkeypatch):
                                                                                                         True, False, False]
     assert calls(product, [[False, 16, 64 * units, 1025], [True, 1, 4096, 128]]) == [True, True]  # up to 16 rows: always
     assert calls(gradient, [[512, 128 * units], [513, 128 * units]]) == [True, False]
+
+
+def saves(qe, hip, cases):
+    got = []
+    for rows, cols, dtype in cases:
+        hip.clear()
+        s = qe.make_saved(qe.SAVED_I8, ADDR, cols, ADDR, (cols + 31) // 32)
+        assert qe.qe_act_save(ADDR, dtype, cols, rows, cols, s, stream=0) == "OK"
+        got.append(hip.log("launch")[0][2])
+    return got
+
+
+def test_saves_of_every_size_take_one_kernel_a_type():
+    """A saved tensor is read again: no size has loads that keep it out of the caches."""
+    for dtype in (0, 1):
+        assert len(set(calls(saves, [[1, 32, dtype], [1500, 4099, dtype], [4096, 14336, dtype], [8192, 28672, dtype]]))) == 1

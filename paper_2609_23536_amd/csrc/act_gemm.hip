@@ -638,13 +638,18 @@ constexpr int kFewRowsTile = 0;  // in place of a GemmTile
 
 // More rows, in blocks of 16, where the whole product has few blocks and a long
 // reduction: a tile kernel then runs a handful of workgroups, each through all of
-// K.  MI355X, us with the small tiles / so: 17 x 512 x 2048 6.3 / 4.6, 17 x 256 x 16092
-// 19.5 / 12.4, 112 x 128 x 16092 32.6 / 12.7, 200 x 256 x 6534 10.9 / 7.7, gated 369 x 128 x
-// 6534 17.2 / 10.1; at K = 512 both are level.  Past one workgroup per unit every
-// block's operands come from the caches once more: 369 x 256 x 16092 (384 blocks) 37.3 /
-// 22.7, but 200 x 512 x 6534 (416) 11.0 / 12.7 and 1340 columns of K = 2048 (588) 6.3 / 8.3.
-// Gated products saved in 8 bits take 32 outputs a workgroup and lose: 50 x 64 x
-// 6534 11.5 / 15.2.
+// K.  MI355X, us with the small tiles / so, every call on other weights (1 GB of
+// them in turn, as a program of many layers has): 17 x 512 x 2048 8.1 / 8.1, x 4096
+// 11.9 / 8.1, x 14336 30.6 / 17.2; 200 x 256 x 6534 18.0 / 8.5; 32 x 2048 x 20480 45 / 22;
+// gated 112 x 128 x 8192 19.7 / 13.9; saved in 8 bits 200 x 256 x 14336 30.0 / 24.3.
+// Past one workgroup per unit every block's operands come from the caches once
+// more, and only long reductions win: 32 x 4096 x 13000 40.1 / 27.4, x 14336 33.5 /
+// 32.6, x 28672 62.9 / 54.9; 369 x 256 x 4096 9.5 / 10.2, x 12300 42.5 / 19.7.
+// (The same weights again and again, out of the caches: level up to K = 2048 and
+// 1.03 to 2 times faster so beyond, but strides of whole lines lose past one
+// workgroup per unit, 32 x 4096 x 14336 22.3 / 30.6, and gated or 8-bit saved, 17 x 512 x
+// 14336 18.2 / 23.3.)  Gated products saved in 8 bits take 32 outputs a workgroup
+// and lose: 50 x 64 x 6534 11.5 / 15.2.
 bool few_blocks(const ActGemmParams &p) {
   if (p.m <= kFewRows) return true;
   const bool gated = p.b2 != nullptr, wide = p.z.kind == kSavedI8;
@@ -660,10 +665,11 @@ bool few_blocks(const ActGemmParams &p) {
 // one row, us with 4 / 8 waves: 7936 x 739 (6 K tiles, 7 rows) 4.8 / 5.7, gated
 // 2730 x 1365 (11) 4.1 / 5.2, 4096 x 4096 (32) 7.7 / 6.0, gated 14336 x 4096 28.5 /
 // 24.9, 8192 x 28672 45.1 / 41.9.
-// With the small tiles (64 x 64 and 64 x 128) these take, us: 4096 x 14336 21.8 ->
-// 13.6, gated 14336 x 4096 30.5 -> 24.6, 8192 x 28672 66 -> 42 (5.6 TB/s), gated
-// 28672 x 8192 87 -> 79 (5.9 TB/s); with 16 rows 21.3 -> 17.7 and 30.8 -> 28.4; with 32
-// rows in two row blocks a wave 21.8 -> 23.6 and 30.8 -> 38.0, so not there.
+// Against the small tiles, MI355X, us small tile / so, other weights every call:
+// one row 512 x 14336 30.1 / 12.8, 8192 x 4096 13.4 / 9.9, 14336 x 8192 27.7 / 24.5, gated
+// 14336 x 4096 28.5 / 25.0, gated 14336 x 8192 46.4 / 44.7, but 14336 x 14336 39.3 / 42.7;
+// sixteen 512 x 14336 30.5 / 17.1, gated 14336 x 4096 28.1 / 27.8, but 14336 x 8192 28.0 /
+// 33.8.  Two row blocks a wave for 32 rows: 21.8 -> 23.6 and gated 30.8 -> 38.0, so not there.
 template <bool GATED, int FA, int FB>
 hipError_t launch_few_rows(const ActGemmParams &p, hipStream_t s) {
   const bool wide = p.z.kind == kSavedI8, few = p.k <= 16 * BK;

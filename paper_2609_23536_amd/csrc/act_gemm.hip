@@ -26,7 +26,7 @@
 //
 // MI355X: 8192 x 8192 x 28672 with a BF16 residual 1290-1340 us (2.9 PFLOP/s, as the
 // plain product), gated 4096 x 14336 x 4096 with both projections saved in 8 bits
-// 391-436 us, where the plain product of 28672 columns takes 379.  Bound by the MFMAs
+// 400-446 us, where the plain product of 28672 columns takes 379.  Bound by the MFMAs
 // and, over short K, by the epilogue's bursts of output.
 #include "act.h"
 #include "gemm_loops.h"

@@ -9,8 +9,9 @@
 // HBM-bound: per element it reads dD (2 or 4 bytes) and the saved values (33/32
 // or 2 bytes each) and writes two code bytes per output (and the dense value),
 // where separate passes would write and read dZ in 16 bits once more.  MI355X, a
-// gated pair in 8 bits, BF16 gradients: 8192 x 28672 to codes 388 us (4.9 TB/s),
-// 2048 x 14336 54 us (4.4), 4096 x 14336 to dense BF16 87 us (5.4).
+// gated pair in 8 bits, BF16 gradients: 8192 x 28672 to codes 395 us (4.8 TB/s),
+// 2048 x 14336 55 us (4.3), 4096 x 14336 to dense BF16 88 us (5.4); kept in BF16
+// instead, 8192 x 28672 465 us (5.0).
 //
 // Layout as in the cast (quantize.hip): a workgroup takes a tile of ROWS rows x
 // 128 columns, a lane eight columns of every sixteenth row, so a saved group of

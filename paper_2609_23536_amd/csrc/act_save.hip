@@ -5,7 +5,8 @@
 // other way round.  A workgroup takes 64 rows x 128 columns, a lane eight
 // columns of every sixteenth row, all four loads in flight: a group is four
 // neighbouring lanes, which share its maximum by lane permutes.  MI355X, BF16 4096 x
-// 14336: saved in 36 us (5.0 TB/s), restored in 29 (6.1).
+// 14336: saved in 36 us (5.0 TB/s) after the kernel that wrote it, in 42 from memory;
+// restored in 29 (6.1).
 //
 // All accesses are ordinary: what is saved was written by the kernel before and
 // is read again by the one after.  With non-temporal loads, MI355X, us from one to

@@ -188,8 +188,9 @@ def _bind_current_stream():
     are not part of torch's documented interface: where they are missing or answer otherwise, the Stream object serves."""
     global _current_stream
     import torch
-    handle = _current_stream = lambda: int(torch.cuda.current_stream().cuda_stream)  # noqa: E731
-    now = handle()
+    handle = lambda: int(torch.cuda.current_stream().cuda_stream)  # noqa: E731
+    now = handle()  # raises where there is no GPU: nothing is bound then
+    _current_stream = handle
     try:
         raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         if raw(device()) == now:

@@ -47,3 +47,18 @@ def test_current_stream(private, monkeypatch):
         assert qe.stream_handle(None) == handle
     assert (fake.objects == 1) == (private is as_known)  # no Stream object a call where the raw accessors serve
     assert qe.stream_handle(5) == 5 and qe.stream_handle(SimpleNamespace(cuda_stream=9)) == 9
+
+
+def test_a_failed_first_use_binds_nothing(monkeypatch):
+    qe = need_lib()
+    fake = Torch(as_known)
+    monkeypatch.setitem(sys.modules, "torch", fake)
+    monkeypatch.setattr(qe, "_current_stream", None)
+
+    def none():
+        raise RuntimeError("no GPU")
+    monkeypatch.setattr(fake.cuda, "current_stream", none)
+    with pytest.raises(RuntimeError):
+        qe.stream_handle(None)
+    monkeypatch.setattr(fake.cuda, "current_stream", fake._stream)
+    assert qe.stream_handle(None) == 0x70 and qe.stream_handle(None) == 0x70 and fake.objects == 1

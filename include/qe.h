@@ -349,6 +349,120 @@ qe_status qe_act_restore(const qe_saved *saved_host, int64_t rows, int64_t cols,
                          qe_stream stream);
 
 /* ------------------------------------------------------------------------
+ * FP8 with a scale for each block of 128, and the norms and the residual sum
+ * between two blocks (stateless, stream-ordered, allocation-free; they can be
+ * captured into a graph by the caller)
+ * ------------------------------------------------------------------------ */
+
+/* FP8 codes with a scale for each block of 128 columns of one row (block_rows 1:
+ * activations and gradients) or of 128 rows (block_rows 128: weights).  The code at
+ * (r, c), data[r * ld + c], stands for
+ *     code * 2^(exps[(r / block_rows) * ld_exps + c / 128] - 127);
+ * a byte of 255 stands for NaN. */
+typedef struct {
+  uint8_t *data;
+  int64_t ld; /* bytes */
+  uint8_t *exps;
+  int64_t ld_exps;
+  int32_t fmt; /* qe_fp8_fmt */
+  int32_t block_rows; /* 1 or 128 */
+} qe_blocked;
+
+/* A matrix of QE_F32 or QE_BF16 values, aligned to its element, row stride ld. */
+typedef struct {
+  void *data;
+  int64_t ld;
+  int32_t dtype; /* qe_dtype */
+  int32_t reserved;
+} qe_matrix;
+
+/* Cast of in, [rows, cols], with a scale for each block.  row_host receives the codes
+ * as [rows, cols], col_host the transposed ones as [cols, rows] with blocks of its own
+ * (128 rows of `in`); either may be NULL.  Both have one format and one block_rows;
+ * with block_rows 128 both hold the same codes and scales.
+ * Of a block with a = max |x|, e = floor(log2(fmax / a)) clamped to [-126, 126] (126
+ * for a = 0), code = x 2^e rounded to nearest even and byte = 127 - e: the largest
+ * value's code is in (fmax / 2, fmax], none saturates.  A block that holds a NaN or an
+ * infinity gets byte 255 and NaN codes.  A last block may be shorter than 128.
+ * Layout rules: ld >= the codes' columns, ld_exps >= ceil(columns / 128), any
+ * alignment.  (The products below want more.)  rows, cols below 2^31, 128 x 128 blocks
+ * below 2^24; rows or cols may be 0.
+ * Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
+qe_status qe_quantize_fp8_block(const qe_matrix *in_host, int64_t rows, int64_t cols, const qe_blocked *row_host,
+                                const qe_blocked *col_host, qe_stream stream);
+
+/* FP8 product in "TN" form with a scale for each block of 128 along the reduction:
+ *   Z = sum_b 2^(ea[i][b] + eb[j][b] - 254) sum_{r in block b} A[i][r] B[j][r] + bias[j]
+ *   c[i][j] = act(Z) + residual[i][j]
+ * a_host: [m, k], b_host: [n, k].  F (Y = X W^T) and dI (dX = dY W) read a weight with
+ * block_rows 128 (its codes, or its transposed codes), dW (dW = dY^T X) two operands
+ * with block_rows 1; any combination is accepted.  The scales are applied in the matrix
+ * instruction, exactly; the sums are otherwise as described for qe_fp8_gemm_act, and so
+ * is epi_host (may be NULL).  With residual = c (FP32) the product is accumulated in
+ * place, as QE_PLACE_ACCUM does.
+ * Layout rules: data 16-byte aligned, ld a multiple of 16, >= k rounded up to 16 and
+ * below 2^23; exps 4-byte aligned, ld_exps a multiple of 4, >= ceil(k / 128) rounded up
+ * to 4 and below 2^23 (the bytes past ceil(k / 128) are read and not used); ldc >= n; c
+ * aligned to its element; m, n below 2^31, ceil(m / 64) ceil(n / 32) below 2^24.
+ * Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
+qe_status qe_fp8_gemm_block(const qe_blocked *a_host, const qe_blocked *b_host, int64_t m, int64_t n, int64_t k,
+                            const qe_epilogue *epi_host, void *c, qe_dtype c_dtype, int64_t ldc, qe_stream stream);
+
+/* What happens between two blocks of a residual stream x, the first of which gave y:
+ *   p = y / sqrt(mean(y^2) + post_eps) * (weight_offset + post_weight)   (post_norm 0: y)
+ *   r = x_scale x + y_scale gate p
+ *   h = r / sqrt(mean(r^2) + pre_eps) * (weight_offset + pre_weight)     (pre_norm 0: none)
+ * with the means over a row.  Weights: cols values each (NULL: a factor of 1).  gate:
+ * row g of [ceil(rows / gate_rows), cols] applies to rows g gate_rows .. of y
+ * (gate_rows >= rows: one row of gates for all; NULL: 1). */
+typedef struct {
+  const void *post_weight, *pre_weight, *gate;
+  int64_t ld_gate, gate_rows;
+  int32_t post_norm, pre_norm;        /* 0 or 1 */
+  int32_t weight_dtype, gate_dtype;   /* qe_dtype */
+  float weight_offset, post_eps, pre_eps, x_scale, y_scale; /* eps > 0 where its norm is taken */
+  int32_t reserved;
+} qe_residual;
+
+/* The sum and the norms in one pass.  x_host or y_host may be NULL (no such term), not
+ * both.  r_host (may be NULL) receives r; h is computed from r as it is stored there,
+ * rounded to its type (not stored: from FP32), and goes to h_host as values, to row_host
+ * (block_rows 1) as FP8 codes and to col_host as transposed ones, as
+ * qe_quantize_fp8_block would cast the FP32 h; each may be NULL.  col_host needs
+ * pre_rstd and r_host (without y and with x_scale 1 it reads x instead where r_host is
+ * NULL).  post_rstd and pre_rstd (may be NULL) receive rows values 1 / sqrt(..), which
+ * the gradient reads.  All arithmetic is FP32: a row whose squares overflow has an
+ * infinite mean.  r or h may be x or y itself (same type and stride); outputs may not
+ * overlap otherwise (with col_host h may not be x either where it is read again).
+ * cols <= 16384 (QE_ERR_INVALID_ARG beyond), rows below 2^31, with col_host 128 x 128
+ * blocks below 2^24; rows or cols may be 0.  Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
+qe_status qe_residual_norm(const qe_matrix *x_host, const qe_matrix *y_host, int64_t rows, int64_t cols,
+                           const qe_residual *desc_host, const qe_matrix *r_host, const qe_matrix *h_host,
+                           const qe_blocked *row_host, const qe_blocked *col_host, float *post_rstd, float *pre_rstd,
+                           qe_stream stream);
+
+/* Its gradient.  dr_host: the gradient of r from what else reads it, dh_host: that of h
+ * (either may be NULL, not both); r_host, y_host: as the forward stored and read them (r
+ * is read with dh only, y_host NULL: there was none); post_rstd, pre_rstd: from the
+ * forward, read where their norm was taken.  dx_host receives x's gradient, dy_host y's
+ * (either may be NULL; each may be dr or dh itself, of the same type and stride, and not
+ * both the same).  dpost_weight, dpre_weight (cols floats) and dgate
+ * ([ceil(rows / gate_rows), cols], row stride ld_dgate), each of which may be NULL,
+ * receive those gradients (QE_PLACE_INIT) or are increased by them (QE_PLACE_ACCUM), in
+ * FP32 and in an order that does not change from call to call; workspace then holds
+ * 2 * cols * G * ceil(min(gate_rows, rows) / 16) floats, G the rows of gates (without
+ * gates 2 * cols * ceil(rows / 16)), whose contents do not matter before or after.
+ * dpre_weight without dh, dpost_weight without y or its norm, and dgate without y or a
+ * gate are refused.  Sizes as above, the workspace below 2^23 rows of cols floats (rows
+ * 0: INIT clears the weights' gradients).
+ * Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
+qe_status qe_residual_norm_grad(const qe_matrix *dr_host, const qe_matrix *dh_host, const qe_matrix *r_host,
+                                const qe_matrix *y_host, int64_t rows, int64_t cols, const qe_residual *desc_host,
+                                const float *post_rstd, const float *pre_rstd, const qe_matrix *dx_host,
+                                const qe_matrix *dy_host, float *dpost_weight, float *dpre_weight, float *dgate,
+                                int64_t ld_dgate, qe_place_mode mode, float *workspace, qe_stream stream);
+
+/* ------------------------------------------------------------------------
  * Stage context: layers, tape slots, versions, arena, executor
  * ------------------------------------------------------------------------ */
 

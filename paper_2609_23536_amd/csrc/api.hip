@@ -821,6 +821,87 @@ bool act_gemm_ok(const qe::ActGemmParams &p) {
   return p.m < kMaxDim && p.n < kMaxDim && ((p.m + 63) / 64) * ((p.n + 31) / 32) < kMaxDim;
 }
 
+// The epilogue of a product of n columns into p; false if it is refused.
+bool epilogue_ok(const qe_epilogue &e, int64_t m, int64_t n, qe::ActGemmParams *p) {
+  if (!valid_act(e.act)) return false;
+  if (e.bias != nullptr && (!valid_dtype(e.bias_dtype) || !elem_aligned(e.bias, e.bias_dtype))) return false;
+  if (e.residual != nullptr &&
+      (!valid_dtype(e.residual_dtype) || !elem_aligned(e.residual, e.residual_dtype) || e.ld_residual < n))
+    return false;
+  if (e.saved.kind != QE_SAVED_NONE && m > 0 && n > 0 && !saved_ok(e.saved, n)) return false;
+  p->act = e.act;
+  p->bias = e.bias;
+  p->bias_bf16 = e.bias_dtype == QE_BF16;
+  p->residual = e.residual;
+  p->residual_bf16 = e.residual_dtype == QE_BF16;
+  p->ld_residual = e.ld_residual;
+  p->z = saved_ref(&e.saved);
+  return true;
+}
+
+// ------------------------------------------------------------------ blocks of 128
+constexpr int64_t kMaxRows = int64_t(1) << 31;
+constexpr int64_t kMaxGroups = int64_t(1) << 24;  // workgroups of 256 lanes: a launch has less than 2^32 lanes
+
+bool cast_grid_ok(int64_t rows, int64_t cols) { return ((rows + 127) / 128) * ((cols + 127) / 128) < kMaxGroups; }
+
+// Codes and scales to be written, `cols` codes a row.
+bool blocked_out_ok(const qe_blocked &b, int64_t cols) {
+  return b.data != nullptr && b.exps != nullptr && valid_fmt(b.fmt) && (b.block_rows == 1 || b.block_rows == 128) &&
+         b.ld >= cols && b.ld_exps >= (cols + 127) / 128;
+}
+
+// An operand of a product over k.
+bool blocked_in_ok(const qe_blocked &b, int64_t k) {
+  constexpr int64_t kMaxLd = int64_t(1) << 23;
+  if (b.data == nullptr || b.exps == nullptr || !valid_fmt(b.fmt) || (b.block_rows != 1 && b.block_rows != 128)) return false;
+  if (uintptr_t(b.data) % 16 || b.ld % 16 || b.ld < rup16(k) || b.ld >= kMaxLd) return false;
+  return uintptr_t(b.exps) % 4 == 0 && b.ld_exps % 4 == 0 && b.ld_exps >= (k + 511) / 512 * 4 && b.ld_exps < kMaxLd;
+}
+
+qe::BlockedRef blocked_ref(const qe_blocked *b) {
+  qe::BlockedRef r;
+  memset(&r, 0, sizeof(r));
+  if (b != nullptr) {
+    r.data = b->data;
+    r.ld = b->ld;
+    r.exps = b->exps;
+    r.ld_exps = b->ld_exps;
+    r.fmt = b->fmt;
+    r.row_shift = b->block_rows == 128 ? 7 : 0;
+  }
+  return r;
+}
+
+// NULL, or a matrix whose rows of `cols` values can be read or written.
+bool matrix_ok(const qe_matrix *m, int64_t cols) {
+  return m == nullptr || (m->data != nullptr && valid_dtype(m->dtype) && elem_aligned(m->data, m->dtype) && m->ld >= cols);
+}
+
+qe::MatrixRef matrix_ref(const qe_matrix *m) {
+  qe::MatrixRef r;
+  memset(&r, 0, sizeof(r));
+  if (m != nullptr) {
+    r.data = m->data;
+    r.ld = m->ld;
+    r.bf16 = m->dtype == QE_BF16;
+  }
+  return r;
+}
+
+constexpr int64_t kMaxNormCols = 16384;  // a row stays in one workgroup's registers
+
+bool residual_ok(const qe_residual *d, int64_t rows, int64_t cols) {
+  if (d == nullptr || rows < 0 || rows >= kMaxRows || cols < 0 || cols > kMaxNormCols) return false;
+  if ((d->post_norm != 0 && d->post_norm != 1) || (d->pre_norm != 0 && d->pre_norm != 1)) return false;
+  if ((d->post_norm && !(d->post_eps > 0.0f)) || (d->pre_norm && !(d->pre_eps > 0.0f))) return false;
+  if ((d->post_weight != nullptr || d->pre_weight != nullptr) && !valid_dtype(d->weight_dtype)) return false;
+  if (d->post_weight != nullptr && !elem_aligned(d->post_weight, d->weight_dtype)) return false;
+  if (d->pre_weight != nullptr && !elem_aligned(d->pre_weight, d->weight_dtype)) return false;
+  return d->gate == nullptr ||
+         (valid_dtype(d->gate_dtype) && elem_aligned(d->gate, d->gate_dtype) && d->ld_gate >= cols && d->gate_rows >= 1);
+}
+
 }  // namespace
 
 extern "C" {
@@ -979,20 +1060,7 @@ qe_status qe_fp8_gemm_act(const uint8_t *a, qe_fp8_fmt fmt_a, int64_t lda, const
   qe::ActGemmParams p;
   memset(&p, 0, sizeof(p));  // padding too: recorded launches are compared bytewise
   if (epi_host != nullptr) {
-    const qe_epilogue &e = *epi_host;
-    if (!valid_act(e.act)) return QE_ERR_INVALID_ARG;
-    if (e.bias != nullptr && (!valid_dtype(e.bias_dtype) || !elem_aligned(e.bias, e.bias_dtype))) return QE_ERR_INVALID_ARG;
-    if (e.residual != nullptr && (!valid_dtype(e.residual_dtype) || !elem_aligned(e.residual, e.residual_dtype) ||
-                                  e.ld_residual < n))
-      return QE_ERR_INVALID_ARG;
-    if (e.saved.kind != QE_SAVED_NONE && m > 0 && n > 0 && !saved_ok(e.saved, n)) return QE_ERR_INVALID_ARG;
-    p.act = e.act;
-    p.bias = e.bias;
-    p.bias_bf16 = e.bias_dtype == QE_BF16;
-    p.residual = e.residual;
-    p.residual_bf16 = e.residual_dtype == QE_BF16;
-    p.ld_residual = e.ld_residual;
-    p.z = saved_ref(&e.saved);
+    if (!epilogue_ok(*epi_host, m, n, &p)) return QE_ERR_INVALID_ARG;
   }
   if (m == 0 || n == 0) return QE_OK;
   p.a = a;
@@ -1135,6 +1203,185 @@ qe_status qe_act_restore(const qe_saved *saved_host, int64_t rows, int64_t cols,
   const qe_status st = save_params(x, x_dtype, ld, rows, cols, saved_host, &p);
   if (st != QE_OK) return st;
   return qe::launch_act_restore(p, static_cast<hipStream_t>(stream)) == hipSuccess ? QE_OK : QE_ERR_HIP;
+}
+
+// ------------------------------------------------------------------ blocks of 128, norms around a residual sum
+qe_status qe_quantize_fp8_block(const qe_matrix *in_host, int64_t rows, int64_t cols, const qe_blocked *row_host,
+                                const qe_blocked *col_host, qe_stream stream) {
+  if (rows < 0 || cols < 0 || rows >= kMaxRows || cols >= kMaxRows) return QE_ERR_INVALID_ARG;
+  if (row_host != nullptr && col_host != nullptr &&
+      (row_host->fmt != col_host->fmt || row_host->block_rows != col_host->block_rows))
+    return QE_ERR_INVALID_ARG;
+  if (rows == 0 || cols == 0) return QE_OK;
+  if (in_host == nullptr || !matrix_ok(in_host, cols)) return QE_ERR_INVALID_ARG;
+  if ((row_host != nullptr && !blocked_out_ok(*row_host, cols)) || (col_host != nullptr && !blocked_out_ok(*col_host, rows)))
+    return QE_ERR_INVALID_ARG;
+  if (!cast_grid_ok(rows, cols)) return QE_ERR_INVALID_ARG;
+  qe::BlockCastParams p;
+  memset(&p, 0, sizeof(p));
+  p.in = matrix_ref(in_host);
+  p.rows = rows;
+  p.cols = cols;
+  p.row = blocked_ref(row_host);
+  p.col = blocked_ref(col_host);
+  return qe::launch_block_cast(p, static_cast<hipStream_t>(stream)) == hipSuccess ? QE_OK : QE_ERR_HIP;
+}
+
+qe_status qe_fp8_gemm_block(const qe_blocked *a_host, const qe_blocked *b_host, int64_t m, int64_t n, int64_t k,
+                            const qe_epilogue *epi_host, void *c, qe_dtype c_dtype, int64_t ldc, qe_stream stream) {
+  if (!valid_dtype(c_dtype) || m < 0 || n < 0 || k < 0 || ldc < n) return QE_ERR_INVALID_ARG;
+  qe::BlockGemmParams p;
+  memset(static_cast<void *>(&p), 0, sizeof(p));
+  if (epi_host != nullptr && !epilogue_ok(*epi_host, m, n, &p)) return QE_ERR_INVALID_ARG;
+  if (m == 0 || n == 0) return QE_OK;
+  if (a_host == nullptr || b_host == nullptr || !blocked_in_ok(*a_host, k) || !blocked_in_ok(*b_host, k)) return QE_ERR_INVALID_ARG;
+  if (c == nullptr || !elem_aligned(c, c_dtype) || m >= kMaxRows || n >= kMaxRows) return QE_ERR_INVALID_ARG;
+  if (((m + 63) / 64) * ((n + 31) / 32) >= kMaxGroups) return QE_ERR_INVALID_ARG;
+  p.a = a_host->data;
+  p.b = b_host->data;
+  p.lda = a_host->ld;
+  p.ldb = b_host->ld;
+  p.m = m;
+  p.n = n;
+  p.k = k;
+  p.c = c;
+  p.ldc = ldc;
+  p.c_bf16 = c_dtype == QE_BF16;
+  p.fmt_a = a_host->fmt;
+  p.fmt_b = b_host->fmt;
+  p.a_exps = a_host->exps;
+  p.b_exps = b_host->exps;
+  p.ld_a_exps = a_host->ld_exps;
+  p.ld_b_exps = b_host->ld_exps;
+  p.a_shift = a_host->block_rows == 128 ? 7 : 0;
+  p.b_shift = b_host->block_rows == 128 ? 7 : 0;
+  return qe::launch_block_gemm(p, static_cast<hipStream_t>(stream)) == hipSuccess ? QE_OK : QE_ERR_HIP;
+}
+
+qe_status qe_residual_norm(const qe_matrix *x_host, const qe_matrix *y_host, int64_t rows, int64_t cols,
+                           const qe_residual *desc_host, const qe_matrix *r_host, const qe_matrix *h_host,
+                           const qe_blocked *row_host, const qe_blocked *col_host, float *post_rstd, float *pre_rstd,
+                           qe_stream stream) {
+  if (!residual_ok(desc_host, rows, cols) || (x_host == nullptr && y_host == nullptr)) return QE_ERR_INVALID_ARG;
+  const qe_residual &d = *desc_host;
+  if (!d.pre_norm && (h_host != nullptr || row_host != nullptr || col_host != nullptr || pre_rstd != nullptr))
+    return QE_ERR_INVALID_ARG;
+  if (post_rstd != nullptr && (!d.post_norm || y_host == nullptr)) return QE_ERR_INVALID_ARG;
+  if (uintptr_t(post_rstd) % 4 || uintptr_t(pre_rstd) % 4) return QE_ERR_INVALID_ARG;
+  if ((row_host != nullptr && row_host->block_rows != 1) || (col_host != nullptr && col_host->block_rows != 1) ||
+      (row_host != nullptr && col_host != nullptr && row_host->fmt != col_host->fmt))
+    return QE_ERR_INVALID_ARG;
+  const bool stream_is_x = y_host == nullptr && d.x_scale == 1.0f;  // r is x
+  if (col_host != nullptr && (pre_rstd == nullptr || (r_host == nullptr && !stream_is_x))) return QE_ERR_INVALID_ARG;
+  // the transposed codes are made after h is stored, from r or from x
+  if (col_host != nullptr && h_host != nullptr && h_host->data == (r_host != nullptr ? r_host : x_host)->data) return QE_ERR_INVALID_ARG;
+  if (col_host != nullptr && !cast_grid_ok(rows, cols)) return QE_ERR_INVALID_ARG;
+  if (rows == 0 || cols == 0) return QE_OK;
+  if (!matrix_ok(x_host, cols) || !matrix_ok(y_host, cols) || !matrix_ok(r_host, cols) || !matrix_ok(h_host, cols))
+    return QE_ERR_INVALID_ARG;
+  if ((row_host != nullptr && !blocked_out_ok(*row_host, cols)) || (col_host != nullptr && !blocked_out_ok(*col_host, rows)))
+    return QE_ERR_INVALID_ARG;
+  qe::ResidualParams p;
+  memset(&p, 0, sizeof(p));
+  p.x = matrix_ref(x_host);
+  p.y = matrix_ref(y_host);
+  p.r = matrix_ref(r_host);
+  p.h = matrix_ref(h_host);
+  p.row = blocked_ref(row_host);
+  p.rows = rows;
+  p.cols = cols;
+  p.post_weight = d.post_weight;
+  p.pre_weight = d.pre_weight;
+  p.gate = d.gate;
+  p.ld_gate = d.ld_gate;
+  p.gate_rows = d.gate_rows;
+  p.post_rstd = post_rstd;
+  p.pre_rstd = pre_rstd;
+  p.post_norm = d.post_norm;
+  p.pre_norm = d.pre_norm;
+  p.weight_bf16 = d.weight_dtype == QE_BF16;
+  p.gate_bf16 = d.gate_dtype == QE_BF16;
+  p.offset = d.weight_offset;
+  p.post_eps = d.post_eps;
+  p.pre_eps = d.pre_eps;
+  p.x_scale = d.x_scale;
+  p.y_scale = d.y_scale;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (qe::launch_residual_norm(p, s) != hipSuccess) return QE_ERR_HIP;
+  if (col_host == nullptr) return QE_OK;
+  qe::BlockCastParams c;  // h again, tile by tile, from the stream and the rows' factors
+  memset(&c, 0, sizeof(c));
+  c.in = r_host != nullptr ? p.r : p.x;
+  c.rows = rows;
+  c.cols = cols;
+  c.col = blocked_ref(col_host);
+  c.rstd = pre_rstd;
+  c.weight = d.pre_weight;
+  c.weight_bf16 = p.weight_bf16;
+  c.offset = d.weight_offset;
+  return qe::launch_block_cast(c, s) == hipSuccess ? QE_OK : QE_ERR_HIP;
+}
+
+qe_status qe_residual_norm_grad(const qe_matrix *dr_host, const qe_matrix *dh_host, const qe_matrix *r_host,
+                                const qe_matrix *y_host, int64_t rows, int64_t cols, const qe_residual *desc_host,
+                                const float *post_rstd, const float *pre_rstd, const qe_matrix *dx_host,
+                                const qe_matrix *dy_host, float *dpost_weight, float *dpre_weight, float *dgate,
+                                int64_t ld_dgate, qe_place_mode mode, float *workspace, qe_stream stream) {
+  if (!residual_ok(desc_host, rows, cols) || (dr_host == nullptr && dh_host == nullptr)) return QE_ERR_INVALID_ARG;
+  const qe_residual &d = *desc_host;
+  const bool post = d.post_norm && y_host != nullptr;
+  if (dh_host != nullptr && (!d.pre_norm || r_host == nullptr || pre_rstd == nullptr)) return QE_ERR_INVALID_ARG;
+  if (post && post_rstd == nullptr) return QE_ERR_INVALID_ARG;
+  if (dy_host != nullptr && y_host == nullptr) return QE_ERR_INVALID_ARG;
+  if (mode != QE_PLACE_INIT && mode != QE_PLACE_ACCUM) return QE_ERR_INVALID_ARG;
+  if (dpre_weight != nullptr && (dh_host == nullptr || d.pre_weight == nullptr)) return QE_ERR_INVALID_ARG;
+  if (dpost_weight != nullptr && (!post || d.post_weight == nullptr)) return QE_ERR_INVALID_ARG;
+  if (dgate != nullptr && (y_host == nullptr || d.gate == nullptr || ld_dgate < cols)) return QE_ERR_INVALID_ARG;
+  if (uintptr_t(post_rstd) % 4 || uintptr_t(pre_rstd) % 4 || uintptr_t(dpost_weight) % 4 || uintptr_t(dpre_weight) % 4 ||
+      uintptr_t(dgate) % 4 || uintptr_t(workspace) % 4)
+    return QE_ERR_INVALID_ARG;
+  const bool sums = dpost_weight != nullptr || dpre_weight != nullptr || dgate != nullptr;
+  qe::ResidualGradParams p;
+  memset(&p, 0, sizeof(p));
+  p.rows = rows;
+  p.cols = cols;
+  p.gate_rows = d.gate == nullptr || d.gate_rows > rows ? (rows > 0 ? rows : 1) : d.gate_rows;
+  p.groups = (rows + p.gate_rows - 1) / p.gate_rows;
+  if (rows > 0 && cols > 0) {
+    if (sums && workspace == nullptr) return QE_ERR_INVALID_ARG;
+    if (!matrix_ok(dr_host, cols) || !matrix_ok(dh_host, cols) || !matrix_ok(y_host, cols) || !matrix_ok(dx_host, cols) ||
+        !matrix_ok(dy_host, cols) || (dh_host != nullptr && !matrix_ok(r_host, cols)))
+      return QE_ERR_INVALID_ARG;
+    // workgroups of up to 1024 lanes for 16 rows, and of 256 for 64 columns of a group's sums
+    if (p.groups * ((p.gate_rows + 15) / 16) >= kMaxGroups / 4 || p.groups * ((cols + 63) / 64) >= kMaxGroups)
+      return QE_ERR_INVALID_ARG;
+  }
+  p.dr = matrix_ref(dr_host);
+  p.dh = matrix_ref(dh_host);
+  p.r = matrix_ref(dh_host != nullptr ? r_host : nullptr);
+  p.y = matrix_ref(y_host);
+  p.dx = matrix_ref(dx_host);
+  p.dy = matrix_ref(dy_host);
+  p.post_weight = d.post_weight;
+  p.pre_weight = d.pre_weight;
+  p.gate = d.gate;
+  p.ld_gate = d.ld_gate;
+  p.post_rstd = post_rstd;
+  p.pre_rstd = pre_rstd;
+  p.sums = sums ? workspace : nullptr;
+  p.dpost = dpost_weight;
+  p.dpre = dpre_weight;
+  p.dgate = dgate;
+  p.ld_dgate = ld_dgate;
+  p.post_norm = post;
+  p.pre_norm = d.pre_norm;
+  p.weight_bf16 = d.weight_dtype == QE_BF16;
+  p.gate_bf16 = d.gate_dtype == QE_BF16;
+  p.offset = d.weight_offset;
+  p.x_scale = d.x_scale;
+  p.y_scale = d.y_scale;
+  p.accumulate = mode == QE_PLACE_ACCUM;
+  return qe::launch_residual_grad(p, static_cast<hipStream_t>(stream)) == hipSuccess ? QE_OK : QE_ERR_HIP;
 }
 
 // ------------------------------------------------------------------ context

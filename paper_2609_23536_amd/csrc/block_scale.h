@@ -1,0 +1,124 @@
+// FP8 codes with a power-of-two scale for each block of 128 values: the exponent
+// byte of a block, codes at it, and rows of FP32 or BF16 values eight at a time
+// (block_cast.hip, residual_norm.hip).
+//
+// Of a block with a = max |x|, e = floor(log2(fmax / a)) clamped to [-126, 126]
+// (126 for a = 0), code = x 2^e rounded to nearest even, byte = 127 - e.  With
+// a = m 2^E and fmax = 1.75 * 2^Emax the byte is a's exponent field less Emax, one
+// more where m > 1.75: the carry of the addition below.  |x| 2^e <= fmax, so codes
+// need no clamp.  A block that holds an infinity or a NaN gets the byte 255 (which
+// the matrix instruction takes for NaN too) and the code 0x7f, a NaN, throughout.
+#pragma once
+
+#include "act.h"
+
+namespace qe {
+namespace {
+
+constexpr int kBlock = 128;
+
+template <int FMT>
+__device__ __forceinline__ uint32_t block_byte(float amax) {
+  const uint32_t a = abs_bits(amax);
+  const int b = int((a + 0x1fffffu) >> 23) - (FMT == 0 ? 8 : 15);
+  return a >= 0x7f800000u ? 255u : uint32_t(b < 1 ? 1 : b);
+}
+// 2^e; for byte 255 a NaN, which makes every code a NaN (0x7f or 0xff, see block_codes).
+__device__ __forceinline__ float block_mult(uint32_t byte) {
+  return __uint_as_float(byte == 255u ? 0x7fc00000u : (254u - byte) << 23);
+}
+// Four values at their block's multiplier -> four codes.  The conversion turns a NaN into 0x7f.
+template <int FMT>
+__device__ __forceinline__ uint32_t block_codes(const float *x, float mult) {
+  return enc4_in_range<FMT>(x[0] * mult, x[1] * mult, x[2] * mult, x[3] * mult);
+}
+
+// Maximum over the 16 lanes of an aligned group, in all of them.
+__device__ __forceinline__ float max_lanes16(float v) { return max_dpp<0x140>(max_lanes8(v)); }  // 15 - lane
+__device__ __forceinline__ float max_swap32(float v) {  // of lanes l and l ^ 32
+  const uint32_t b = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return nan_max(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_swap16(float v) {  // of lanes l and l ^ 16
+  const uint32_t b = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  return nan_max(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+typedef float f32x4_in __attribute__((ext_vector_type(4), aligned(4)));
+
+// Row `row` of a matrix: uniform in a workgroup where `row` is, so that a lane's
+// address is a scalar base and its column's 32-bit offset.
+__device__ __forceinline__ char *row_of(const MatrixRef &m, bool bf16, int64_t row) {
+  return static_cast<char *>(m.data) + row * m.ld * (bf16 ? 2 : 4);
+}
+
+// Eight consecutive values from column `at` of a row, n of which exist (the others are zero).
+__device__ __forceinline__ void load8(const void *base, bool bf16, uint32_t at, int n, float *f) {
+  if (bf16) {
+    const uint16_t *p = static_cast<const uint16_t *>(base) + at;
+    if (n >= 8) {
+      const u32x4_in w = *reinterpret_cast<const u32x4_in *>(p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[2 * e] = __uint_as_float(w[e] << 16);
+        f[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = e < n ? bf16_to_f32(p[e]) : 0.0f;
+    }
+  } else {
+    const float *p = static_cast<const float *>(base) + at;
+    if (n >= 8) {
+      const f32x4_in a = *reinterpret_cast<const f32x4_in *>(p), b = *reinterpret_cast<const f32x4_in *>(p + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[e] = a[e];
+        f[4 + e] = b[e];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = e < n ? p[e] : 0.0f;
+    }
+  }
+}
+
+__device__ __forceinline__ void store8(void *base, bool bf16, uint32_t at, int n, const float *f) {
+  if (bf16) {
+    uint16_t *p = static_cast<uint16_t *>(base) + at;
+    if (n >= 8) {
+      *reinterpret_cast<u32x4_in *>(p) = u32x4_in{bf16x2_bits(f[0], f[1]), bf16x2_bits(f[2], f[3]), bf16x2_bits(f[4], f[5]),
+                                                  bf16x2_bits(f[6], f[7])};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) p[e] = bf16_bits(f[e]);
+    }
+  } else {
+    float *p = static_cast<float *>(base) + at;
+    if (n >= 8) {
+      *reinterpret_cast<f32x4_in *>(p) = f32x4_in{f[0], f[1], f[2], f[3]};
+      *reinterpret_cast<f32x4_in *>(p + 4) = f32x4_in{f[4], f[5], f[6], f[7]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) p[e] = f[e];
+    }
+  }
+}
+
+// Eight codes of a row, n of which exist.
+__device__ __forceinline__ void store_codes8(uint8_t *p, int n, uint32_t lo, uint32_t hi) {
+  if (n >= 8) {
+    *reinterpret_cast<u32x2_out *>(p) = u32x2_out{lo, hi};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = uint8_t(byte_of(e < 4 ? lo : hi, e % 4));
+  }
+}
+
+}  // namespace
+}  // namespace qe

@@ -15,12 +15,59 @@
 namespace qe {
 namespace {
 
+// Operands of one scale each: the sums are scaled after the loop.
+struct NoScales {
+  static constexpr bool kOn = false;
+};
+
+// Operands with a scale for each block of 128 along the reduction, one byte (the
+// exponent field of a power of two) per row and K tile, which the matrix instruction
+// applies to its products by itself: it takes a scale for 32 values of a row, the four
+// of a K tile are the same.  The bytes come four K tiles (a group) at a time, a word
+// of every tile row by an LDS-bound load, and go through BUFS buffers of the groups
+// modulo BUFS at byte `lds` of smem: those of A's rows, then of B's.  Against loads
+// of whole K tiles that is two loads in 64 of a wave (256 x 256 tiles), and one byte
+// read per fragment.
+template <int BM, int BN, int BUFS>
+struct LdsScales {
+  static constexpr bool kOn = true;
+  static constexpr int kSlots = (BM + BN) / 64, kPer = (kSlots + 3) / 4;  // 64 rows each; per wave
+  static constexpr int kBuf = (BM + BN) * 4, kBytes = BUFS * kBuf;
+  static_assert((BUFS & (BUFS - 1)) == 0, "buffers are numbered by bits");
+  const uint8_t *base[kPer];  // uniform in the wave
+  uint32_t off[kPer];
+  int groups;
+  uint32_t lds;
+  __device__ __forceinline__ void load(const uint8_t *smem, int wave, int group) const {
+    if (group >= groups) return;
+    const uint32_t to = uint32_t(reinterpret_cast<uintptr_t>(smem)) + lds + uint32_t(group & (BUFS - 1)) * kBuf;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int slot = __builtin_amdgcn_readfirstlane(wave + 4 * q);
+      if (slot < kSlots)
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off[q]), "s"(base[q] + 4 * group),
+                     "s"(__builtin_amdgcn_readfirstlane(to + uint32_t(slot) * 256u)) : "memory", "m0");
+    }
+  }
+  __device__ __forceinline__ int read(const uint8_t *smem, int row, int t) const {
+    return smem[lds + uint32_t((t >> 2) & (BUFS - 1)) * kBuf + uint32_t(t & 3) + uint32_t(row) * 4u];
+  }
+};
+
+template <int FA, int FB, bool SCALED>
+__device__ __forceinline__ v4f mfma_tile(const v8i &a, const v8i &b, v4f acc, int sa, int sb) {
+  if constexpr (SCALED)
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, FB, FA, 0, sb, 0, sa);
+  else
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, FB, FA, 0, 0, 0, 0);
+}
+
 // Large tiles, four waves, two K stages in smem (and one 1 KB block per wave):
 // see gemm_tn_w4_kernel.  The offsets come from chunk_offset.
-template <int FA, int FB, int BM, int BN>
+template <int FA, int FB, int BM, int BN, typename SC = NoScales>
 __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b, const uint32_t (&oa)[BM / 32],
                                              const uint32_t (&ob)[BN / 32], int64_t K, uint8_t *smem,
-                                             v4f (&acc)[BM / 32][BN / 32]) {
+                                             v4f (&acc)[BM / 32][BN / 32], const SC &sc = SC{}) {
   constexpr int NW = 4, TM = BM / 2, TN = BN / 2;
   constexpr int I = TM / 16, J = TN / 16;    // 16 x 16 MFMA blocks per wave sub-tile
   constexpr int IA = I / 2, IB = I - IA;     // block rows of phase A and phase B
@@ -87,9 +134,14 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
     const uint4 hi = *reinterpret_cast<const uint4 *>(base + f_hi);
     return v8i{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
   };
-  auto read_a = [&](int buf, int i, v8i (&fa)[I]) { fa[i] = frag(smem + buf * STAGE + (wm * TM + i * 16) * BK); };
-  auto read_b = [&](int buf, int j, v8i (&fb)[J]) {
+  int sa[I], sb[J];  // the fragments' scales, read with them
+  auto read_a = [&](int t, int buf, int i, v8i (&fa)[I]) {
+    fa[i] = frag(smem + buf * STAGE + (wm * TM + i * 16) * BK);
+    if constexpr (SC::kOn) sa[i] = sc.read(smem, wm * TM + i * 16 + fr, t);
+  };
+  auto read_b = [&](int t, int buf, int j, v8i (&fb)[J]) {
     fb[j] = frag(smem + buf * STAGE + (BM + wn * TN + j * 16) * BK);
+    if constexpr (SC::kOn) sb[j] = sc.read(smem, BM + wn * TN + j * 16 + fr, t);
   };
 
 #pragma unroll
@@ -98,7 +150,7 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
     for (int j = 0; j < J; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
 
   auto mfma = [&](int i, int j, const v8i (&fa)[I], const v8i (&fb)[J]) {
-    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i], acc[i][j], FB, FA, 0, 0, 0, 0);
+    acc[i][j] = mfma_tile<FA, FB, SC::kOn>(fa[i], fb[j], acc[i][j], sa[i], sb[j]);
   };
   // LDS-bound loads inside the K loop, two instructions each: load d of a K
   // tile lands at stage + 4096 d, so M0 steps by a uniform stride, and the
@@ -128,7 +180,7 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
   // two K tiles ahead (`kt3`), spread over the phase: a K step and a half
   // before it is read.
   auto b_slot = [](int q, int k) { return (k * QA) / CHB + 1 == q; };
-  auto phase_a = [&](int buf, bool dmab, int kt3, v8i (&fa)[I], v8i (&fb)[J]) {
+  auto phase_a = [&](int t, int buf, bool dmab, int kt3, v8i (&fa)[I], v8i (&fb)[J]) {
     const uint8_t *gb = dmab ? b + int64_t(kt3) * BK : b;
     const uint32_t base = dmab ? wblk + uint32_t(buf * STAGE + BM * BK) : wdummy;
     const uint32_t stride = dmab ? uint32_t(NW * 1024) : 0u;
@@ -143,7 +195,7 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       mfma(q % IA, q / IA, fa, fb);
       __builtin_amdgcn_sched_barrier(0);
       if (d >= 0) dma_load(CHA + d, a, gb);
-      if (q % 2 == 0 && q / 2 < IB) read_a(buf, IA + q / 2, fa);
+      if (q % 2 == 0 && q / 2 < IB) read_a(t, buf, IA + q / 2, fa);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -165,7 +217,7 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
     if (q % 4 == 0 && CHA > n12) return q / 4 >= IA && QB / 4 - 1 - q / 4 < CHA - n12;
     return false;
   };
-  auto phase_b = [&](int nbuf, bool dma, int kt2, int buf, v8i (&fa)[I], v8i (&fb)[J]) {
+  auto phase_b = [&](int t, int nbuf, bool dma, int kt2, int buf, v8i (&fa)[I], v8i (&fb)[J]) {
     static_assert(QB % 4 == 0, "phase B slots come in fours");
     const uint8_t *ga = dma ? a + int64_t(kt2) * BK : a;
     const uint8_t *gb = dma ? b + int64_t(kt2) * BK : b;
@@ -184,14 +236,15 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       mfma(i, j, fa, fb);
       __builtin_amdgcn_sched_barrier(0);
       if (ld) dma_load(d, ga, gb);
-      if (q % 4 == 0 && q / 4 < IA) read_a(nbuf, q / 4, fa);
-      if (q % IB == IB - 1) read_b(nbuf, j, fb);  // last use of B fragment j was this MFMA
+      if (q % 4 == 0 && q / 4 < IA) read_a(t + 1, nbuf, q / 4, fa);
+      if (q % IB == IB - 1) read_b(t + 1, nbuf, j, fb);  // last use of B fragment j was this MFMA
     }
     __builtin_amdgcn_sched_barrier(0);
   };
 
   if (T > 0) {
     v8i fa[I], fb[J];
+    if constexpr (SC::kOn) sc.load(smem, wave, 0);  // the first loads: complete whenever a tile's are
     issue(0, 0);
     if (KT > 1) {
       // both first K tiles are full: tile 1's LDS-bound loads stay in flight
@@ -204,12 +257,12 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
     }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < J; ++j) read_b(0, j, fb);
+    for (int j = 0; j < J; ++j) read_b(0, 0, j, fb);
 #pragma unroll
-    for (int i = 0; i < IA; ++i) read_a(0, i, fa);
+    for (int i = 0; i < IA; ++i) read_a(0, 0, i, fa);
     if (T > 1 && KT <= 1) issue(1, 1);  // tile 1 is the partial tail: through registers
     __syncthreads();                       // every wave holds tile 0's B fragments: stage 0's B half is free
-    phase_a(0, 2 < KT, 2, fa, fb);         // and takes tile 2's B part
+    phase_a(0, 0, 2 < KT, 2, fa, fb);         // and takes tile 2's B part
     // tile 1 complete; the CHB most recent loads (tile 2's B part) may still
     // be in flight: the counter completes in order
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
@@ -218,13 +271,18 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       const int buf = t & 1;
       const bool dma = t + 2 < KT;
       if (t + 2 < T && !dma) issue(t + 2, buf);
+      // The next group's scales, into the buffer whose last reads were of tile t - 1.
+      // They are older than the B part below, so the wait at this step's end covers
+      // them: three steps before they are read.
+      if constexpr (SC::kOn)
+        if ((t & 3) == 0) sc.load(smem, wave, (t >> 2) + 1);
       // phase B of tile t, with tile t+2's A part; reads of tile t+1 (in the
       // last iteration they read a stale stage that is never used: always in
       // bounds, and branch-free here)
-      phase_b(buf ^ 1, dma, t + 2, buf, fa, fb);
+      phase_b(t, buf ^ 1, dma, t + 2, buf, fa, fb);
       if (t + 1 < T) {
         __syncthreads();                   // tile t+1's B fragments read by every wave
-        phase_a(buf ^ 1, t + 3 < KT, t + 3, fa, fb);  // with tile t+3's B part
+        phase_a(t + 1, buf ^ 1, t + 3 < KT, t + 3, fa, fb);  // with tile t+3's B part
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
         __syncthreads();                   // tile t+2 published; tile t+1 fully read
       }
@@ -244,10 +302,10 @@ __device__ __forceinline__ v8i mask_frag(v8i f, int valid) {
 }
 
 // Ring tiles, four waves, S K stages in smem: see gemm_tn_ring_kernel.
-template <int FA, int FB, int BM, int BN, int S>
+template <int FA, int FB, int BM, int BN, int S, typename SC = NoScales>
 __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, const uint32_t (&oa)[BM / 32],
                                             const uint32_t (&ob)[BN / 32], int K, uint8_t *smem,
-                                            v4f (&acc)[BM / 32][BN / 32]) {
+                                            v4f (&acc)[BM / 32][BN / 32], const SC &sc = SC{}) {
   constexpr int NW = 4, TM = BM / 2, TN = BN / 2;
   constexpr int I = TM / 16, J = TN / 16;
   constexpr int CHA = BM / 32, CHB = BN / 32;  // LDS-bound loads per lane per K tile
@@ -307,12 +365,28 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
   };
   struct Frags {
     v8i a[I], b[J];
+    int sa[I], sb[J];  // their scales
   };
-  auto read = [&](uint32_t stage, Frags &f) {
+  auto read_a = [&](int t, uint32_t stage, int i, Frags &f) {
+    f.a[i] = frag(stage + uint32_t((wm * TM + i * 16) * BK));
+    if constexpr (SC::kOn) f.sa[i] = sc.read(smem, wm * TM + i * 16 + fr, t);
+  };
+  auto read_b = [&](int t, uint32_t stage, int j, Frags &f) {
+    f.b[j] = frag(stage + uint32_t((BM + wn * TN + j * 16) * BK));
+    if constexpr (SC::kOn) f.sb[j] = sc.read(smem, BM + wn * TN + j * 16 + fr, t);
+  };
+  auto read = [&](int t, uint32_t stage, Frags &f) {
 #pragma unroll
-    for (int i = 0; i < I; ++i) f.a[i] = frag(stage + uint32_t((wm * TM + i * 16) * BK));
+    for (int i = 0; i < I; ++i) read_a(t, stage, i, f);
 #pragma unroll
-    for (int j = 0; j < J; ++j) f.b[j] = frag(stage + uint32_t((BM + wn * TN + j * 16) * BK));
+    for (int j = 0; j < J; ++j) read_b(t, stage, j, f);
+  };
+  // Scales go two groups ahead: at least seven tiles' loads are younger than theirs
+  // when they are read, more than the waits leave in flight.
+  static_assert(S - 2 <= 7, "a group's scales are complete when they are read");
+  auto load_scales = [&](int t) {
+    if constexpr (SC::kOn)
+      if ((t & 3) == 0) sc.load(smem, wave, (t >> 2) + 2);
   };
   auto mask = [&](Frags &f) {
     const int valid = ktail - 32 * fq;
@@ -328,7 +402,7 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
     for (int j = 0; j < J; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
 
   auto mfma = [&](int i, int j, const Frags &f) {
-    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f.b[j], f.a[i], acc[i][j], FB, FA, 0, 0, 0, 0);
+    acc[i][j] = mfma_tile<FA, FB, SC::kOn>(f.a[i], f.b[j], acc[i][j], f.sa[i], f.sb[j]);
   };
   uint32_t rd = 0;  // stage of tile t
   // Step t: fragments of tile t are in `cur`; tile t + 1's are read into `nxt`.
@@ -344,6 +418,7 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
     const uint8_t *gb = b + int64_t(t + S) * BK;
     const uint32_t sa = wblk + rd;  // tile t's stage takes tile t + S; load d lands at sa + 4096 d
     rd = rd + STAGE == uint32_t(S * STAGE) ? 0u : rd + STAGE;
+    load_scales(t);
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       __builtin_amdgcn_sched_barrier(0);
@@ -370,9 +445,9 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
       for (int r = 0; r < I + J; ++r)
         if (r * Q / (I + J) == q) {
           if (r < I)
-            nxt.a[r] = frag(rd + uint32_t((wm * TM + r * 16) * BK));
+            read_a(t + 1, rd, r, nxt);
           else
-            nxt.b[r - I] = frag(rd + uint32_t((BM + wn * TN + (r - I) * 16) * BK));
+            read_b(t + 1, rd, r - I, nxt);
         }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -388,8 +463,9 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
     __syncthreads();
     const uint32_t freed = rd;
     rd = rd + STAGE == uint32_t(S * STAGE) ? 0u : rd + STAGE;
-    read(rd, nxt);
+    read(t + 1, rd, nxt);
     __builtin_amdgcn_sched_barrier(0);
+    load_scales(t);
     if (t + S < T) issue(t + S, freed);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -400,6 +476,10 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
 
   if (T > 0) {
     Frags f0, f1;
+    if constexpr (SC::kOn) {
+      sc.load(smem, wave, 0);
+      sc.load(smem, wave, 1);
+    }
 #pragma unroll
     for (int t = 0; t < S; ++t)
       if (t < T) issue(t, uint32_t(t * STAGE));
@@ -408,7 +488,7 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
     else
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    read(0, f0);
+    read(0, 0, f0);
     if (T == 1 && ktail != 0) mask(f0);
     int t = 0;
     for (; t + 1 + S < K / BK; t += 2) {

@@ -207,6 +207,77 @@ struct ActGradParams {
   int32_t dd_bf16, dz_bf16;
 };
 
+// FP8 codes with a scale for each block of 128 (qe_blocked): element (r, c) stands
+// for code * 2^(exps[(r >> row_shift) * ld_exps + c / 128] - 127).
+struct BlockedRef {
+  uint8_t *data;
+  int64_t ld;
+  uint8_t *exps;
+  int64_t ld_exps;
+  int32_t fmt;
+  int32_t row_shift;  // 0: blocks of one row, 7: of 128 rows
+};
+
+// A matrix of FP32 or BF16 values (qe_matrix).
+struct MatrixRef {
+  void *data;
+  int64_t ld;
+  int32_t bf16;
+  int32_t pad;
+};
+
+// Cast to codes with a scale for each block, row-wise and / or transposed (data
+// null: not written).  With rstd set the values cast are in * rstd[row] *
+// (offset + weight[col]) (no last factor without weight): a norm's output.
+struct BlockCastParams {
+  MatrixRef in;
+  int64_t rows, cols;
+  BlockedRef row, col;
+  const float *rstd;
+  const void *weight;
+  float offset;
+  int32_t weight_bf16;
+};
+
+// Product of two such operands with an epilogue; a, b, lda, ldb of the epilogue's
+// parameters are the codes, their scale inverses null.
+struct BlockGemmParams : ActGemmParams {
+  const uint8_t *a_exps, *b_exps;
+  int64_t ld_a_exps, ld_b_exps;
+  int32_t a_shift, b_shift;
+};
+
+// r = x_scale x + y_scale gate p, p = y or norm(y); h = norm(r) (qe_residual_norm).
+struct ResidualParams {
+  MatrixRef x, y, r, h;
+  BlockedRef row;
+  int64_t rows, cols;
+  int64_t row0;  // the launch's first row
+  const void *post_weight, *pre_weight, *gate;
+  int64_t ld_gate, gate_rows;
+  float *post_rstd, *pre_rstd;
+  int32_t post_norm, pre_norm, weight_bf16, gate_bf16;
+  float offset, post_eps, pre_eps, x_scale, y_scale;
+  int32_t pad;
+};
+
+// The gradients of that.  sums: per chunk of kGradRows rows, cols partial sums of
+// dh n and then of db yn (see residual_norm.hip).
+constexpr int64_t kGradRows = 16;
+struct ResidualGradParams {
+  MatrixRef dr, dh, r, y, dx, dy;
+  int64_t rows, cols;
+  const void *post_weight, *pre_weight, *gate;
+  int64_t ld_gate, gate_rows, groups;
+  const float *post_rstd, *pre_rstd;
+  float *sums;
+  float *dpost, *dpre, *dgate;
+  int64_t ld_dgate;
+  int32_t post_norm, pre_norm, weight_bf16, gate_bf16;
+  float offset, x_scale, y_scale;
+  int32_t accumulate;
+};
+
 // An activation stored in, or restored from, an 8-bit checkpoint.
 struct SaveParams {
   void *x;
@@ -302,6 +373,10 @@ hipError_t launch_act_gemm(const ActGemmParams &p, hipStream_t s);
 hipError_t launch_act_grad(const ActGradParams &p, float *dbias, bool accumulate, hipStream_t s);
 hipError_t launch_act_save(const SaveParams &p, hipStream_t s);
 hipError_t launch_act_restore(const SaveParams &p, hipStream_t s);
+hipError_t launch_block_cast(const BlockCastParams &p, hipStream_t s);
+hipError_t launch_block_gemm(const BlockGemmParams &p, hipStream_t s);
+hipError_t launch_residual_norm(const ResidualParams &p, hipStream_t s);
+hipError_t launch_residual_grad(const ResidualGradParams &p, hipStream_t s);
 // 0: tile shape from the cost model, else one shape for every product
 void set_gemm_tile_override(int tile);
 int gemm_tile_override();

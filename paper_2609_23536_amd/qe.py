@@ -20,6 +20,7 @@ F32, BF16 = 0, 1
 INIT, ACCUM = 0, 1
 ROLE_X, ROLE_W, ROLE_DY = 0, 1, 2
 SCALING_DELAYED, SCALING_CURRENT = 0, 1
+BLOCK = 128        # values that share a scale in qe_blocked codes
 AMAX_LINES, AMAX_STRIDE = 64, 64   # amax accumulator: lines x floats between lines
 KC_QUANT, KC_UPDATE, KC_GEMM, KC_COPY, KC_AMAX = 0, 1, 2, 3, 4
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
@@ -61,6 +62,22 @@ class Saved(C.Structure):
 class Epilogue(C.Structure):
     _fields_ = [("bias", C.c_void_p), ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("bias_dtype", C.c_int32),
                 ("residual_dtype", C.c_int32), ("act", C.c_int32), ("reserved", C.c_int32), ("saved", Saved)]
+
+
+class Blocked(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("exps", C.c_void_p), ("ld_exps", C.c_int64), ("fmt", C.c_int32),
+                ("block_rows", C.c_int32)]
+
+
+class Matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class Residual(C.Structure):
+    _fields_ = [("post_weight", C.c_void_p), ("pre_weight", C.c_void_p), ("gate", C.c_void_p), ("ld_gate", C.c_int64),
+                ("gate_rows", C.c_int64), ("post_norm", C.c_int32), ("pre_norm", C.c_int32), ("weight_dtype", C.c_int32),
+                ("gate_dtype", C.c_int32), ("weight_offset", C.c_float), ("post_eps", C.c_float), ("pre_eps", C.c_float),
+                ("x_scale", C.c_float), ("y_scale", C.c_float), ("reserved", C.c_int32)]
 
 
 class Config(C.Structure):
@@ -116,6 +133,12 @@ _SIGS = {
                     _P, _I64, _P, _P, _I32, _I64, _P, _I32, _P, _P],
     "qe_act_save": [_P, _I32, _I64, _I64, _I64, C.POINTER(Saved), _P],
     "qe_act_restore": [C.POINTER(Saved), _I64, _I64, _P, _I32, _I64, _P],
+    "qe_quantize_fp8_block": [C.POINTER(Matrix), _I64, _I64, C.POINTER(Blocked), C.POINTER(Blocked), _P],
+    "qe_fp8_gemm_block": [C.POINTER(Blocked), C.POINTER(Blocked), _I64, _I64, _I64, C.POINTER(Epilogue), _P, _I32, _I64, _P],
+    "qe_residual_norm": [C.POINTER(Matrix), C.POINTER(Matrix), _I64, _I64, C.POINTER(Residual), C.POINTER(Matrix),
+                         C.POINTER(Matrix), C.POINTER(Blocked), C.POINTER(Blocked), _P, _P, _P],
+    "qe_residual_norm_grad": [C.POINTER(Matrix), C.POINTER(Matrix), C.POINTER(Matrix), C.POINTER(Matrix), _I64, _I64,
+                              C.POINTER(Residual), _P, _P, C.POINTER(Matrix), C.POINTER(Matrix), _P, _P, _P, _I64, _I32, _P, _P],
     "qe_ctx_create": [C.POINTER(Config), C.POINTER(_P)],
     "qe_layer_register": [_P, C.POINTER(LayerDesc), C.POINTER(_I32)],
     "qe_layer_meta": [_P, _I32, _I32, C.POINTER(FP8Meta)],
@@ -304,6 +327,50 @@ def qe_act_save(x, x_dtype: int, ld: int, rows: int, cols: int, saved: Saved, st
 
 def qe_act_restore(saved: Saved, rows: int, cols: int, x, x_dtype: int, ld: int, stream=None) -> str:
     return _st(lib().qe_act_restore(_ref(saved), rows, cols, ptr(x), x_dtype, ld, stream_handle(stream)))
+
+
+def make_blocked(data, ld: int, exps, ld_exps: int, fmt: int, block_rows: int = 1) -> Blocked:
+    return Blocked(ptr(data), ld, ptr(exps), ld_exps, fmt, block_rows)
+
+
+def make_matrix(data, ld: int, dtype: int) -> Matrix:
+    return Matrix(ptr(data), ld, dtype, 0)
+
+
+def make_residual(x_scale: float = 1.0, y_scale: float = 1.0, post_norm: bool = False, post_weight=None,
+                  post_eps: float = 1e-5, pre_norm: bool = False, pre_weight=None, pre_eps: float = 1e-5,
+                  weight_dtype: int = F32, weight_offset: float = 0.0, gate=None, gate_dtype: int = F32, ld_gate: int = 0,
+                  gate_rows: int = 0) -> Residual:
+    return Residual(ptr(post_weight), ptr(pre_weight), ptr(gate), ld_gate, gate_rows, int(post_norm), int(pre_norm),
+                    weight_dtype, gate_dtype, weight_offset, post_eps, pre_eps, x_scale, y_scale, 0)
+
+
+def qe_quantize_fp8_block(inp: Optional[Matrix], rows: int, cols: int, row: Optional[Blocked] = None,
+                          col: Optional[Blocked] = None, stream=None) -> str:
+    return _st(lib().qe_quantize_fp8_block(_ref(inp), rows, cols, _ref(row), _ref(col), stream_handle(stream)))
+
+
+def qe_fp8_gemm_block(a: Optional[Blocked], b: Optional[Blocked], m: int, n: int, k: int, epilogue: Optional[Epilogue], c,
+                      c_dtype: int, ldc: int, stream=None) -> str:
+    return _st(lib().qe_fp8_gemm_block(_ref(a), _ref(b), m, n, k, _ref(epilogue), ptr(c), c_dtype, ldc,
+                                       stream_handle(stream)))
+
+
+def qe_residual_norm(x: Optional[Matrix], y: Optional[Matrix], rows: int, cols: int, desc: Optional[Residual],
+                     r: Optional[Matrix] = None, h: Optional[Matrix] = None, row: Optional[Blocked] = None,
+                     col: Optional[Blocked] = None, post_rstd=None, pre_rstd=None, stream=None) -> str:
+    return _st(lib().qe_residual_norm(_ref(x), _ref(y), rows, cols, _ref(desc), _ref(r), _ref(h), _ref(row), _ref(col),
+                                      ptr(post_rstd), ptr(pre_rstd), stream_handle(stream)))
+
+
+def qe_residual_norm_grad(dr: Optional[Matrix], dh: Optional[Matrix], r: Optional[Matrix], y: Optional[Matrix], rows: int,
+                          cols: int, desc: Optional[Residual], post_rstd=None, pre_rstd=None, dx: Optional[Matrix] = None,
+                          dy: Optional[Matrix] = None, dpost_weight=None, dpre_weight=None, dgate=None, mode: int = INIT,
+                          workspace=None, ld_dgate: Optional[int] = None, stream=None) -> str:
+    return _st(lib().qe_residual_norm_grad(_ref(dr), _ref(dh), _ref(r), _ref(y), rows, cols, _ref(desc), ptr(post_rstd),
+                                           ptr(pre_rstd), _ref(dx), _ref(dy), ptr(dpost_weight), ptr(dpre_weight), ptr(dgate),
+                                           cols if ld_dgate is None else ld_dgate, mode, ptr(workspace),
+                                           stream_handle(stream)))
 
 
 def make_meta(hist, scale, scale_inv, fmt: int, margin: int = 0, amax_accum=None) -> FP8Meta:

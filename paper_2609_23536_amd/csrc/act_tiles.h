@@ -642,7 +642,11 @@ __device__ __forceinline__ void act_rows_tile(const P &g, int blocks_n) {
       }
 #pragma unroll
       for (int j = 0; j < NB; ++j)
-        acc[j] = mfma_tile<FA, FB, SC>(fa[u], fb[u][j], acc[j], int(sa >> (8 * u)), SC ? int(sb[j] >> (8 * u)) : 0);
+        if constexpr (SC)
+          acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u][j], fa[u], acc[j], FB, FA, 0, int(sb[j] >> (8 * u)), 0,
+                                                                    int(sa >> (8 * u)));
+        else
+          acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u][j], fa[u], acc[j], FB, FA, 0, 0, 0, 0);
     }
   }
   const SumScale s0 = scale_of(g, g.b_scale_inv), s1 = GATED ? scale_of(g, g.b2_scale_inv) : s0;

@@ -49,17 +49,43 @@ struct LdsScales {
                      "s"(__builtin_amdgcn_readfirstlane(to + uint32_t(slot) * 256u)) : "memory", "m0");
     }
   }
-  __device__ __forceinline__ int read(const uint8_t *smem, int row, int t) const {
-    return smem[lds + uint32_t((t >> 2) & (BUFS - 1)) * kBuf + uint32_t(t & 3) + uint32_t(row) * 4u];
+  // Where K tile t's bytes of rows `row` .. start; the compiler sees an address and
+  // constants from it, not the parts of it that it would keep one register each for.
+  __device__ __forceinline__ uint32_t at(const uint8_t *smem, int row, int t) const {
+    uint32_t p = uint32_t(reinterpret_cast<uintptr_t>(smem)) + lds + uint32_t((t >> 2) & (BUFS - 1)) * kBuf + uint32_t(t & 3) +
+                 uint32_t(row) * 4u;
+    asm("" : "+v"(p));
+    return p;
+  }
+  static __device__ __forceinline__ int read(uint32_t p, int rows) {
+    return *reinterpret_cast<const __attribute__((address_space(3))) uint8_t *>(p + uint32_t(rows) * 4u);
   }
 };
 
+// One block's product of a K tile.  With scales it is inline assembly, because the
+// compiler gives the builtin's result registers of its own, apart from the
+// accumulator's (the 256 x 256 tile then spills 80 registers and the 128 x 128 one
+// 140).  The assembler adds no waits: s_nop 1 stands for what a vector instruction
+// that wrote an operand needs, products of the same accumulator are at least three
+// others apart in the loops, and settle() comes before anything else reads them.
 template <int FA, int FB, bool SCALED>
-__device__ __forceinline__ v4f mfma_tile(const v8i &a, const v8i &b, v4f acc, int sa, int sb) {
+__device__ __forceinline__ void mfma_tile(v4f &acc, const v8i &a, const v8i &b, int sa, int sb) {
   if constexpr (SCALED)
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, FB, FA, 0, sb, 0, sa);
+    asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:%5 blgp:%6"
+                 : "+a"(acc) : "v"(b), "v"(a), "v"(sb), "v"(sa), "n"(FB), "n"(FA));
   else
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, FB, FA, 0, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, FB, FA, 0, 0, 0, 0);
+}
+// After the last of them: longer than the instruction takes to write its result (12 wait states).
+template <bool SCALED, int I, int J>
+__device__ __forceinline__ void settle(v4f (&acc)[I][J]) {
+  if constexpr (SCALED) {
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j) asm volatile("" : "+a"(acc[i][j]));
+  }
 }
 
 // Large tiles, four waves, two K stages in smem (and one 1 KB block per wave):
@@ -88,6 +114,12 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
   const uint32_t wblk = __builtin_amdgcn_readfirstlane(lds_base + uint32_t(wave) * 1024u);
   const uint32_t wdummy = __builtin_amdgcn_readfirstlane(lds_base + uint32_t(2 * STAGE) + uint32_t(wave) * 1024u);
 
+  // The 64-bit form of an offset, which only the partial K tile needs, is made there
+  // (the compiler keeps it through the loop otherwise: 16 registers that the scales take).
+  auto here = [](uint32_t o) {
+    if constexpr (SC::kOn) asm volatile("" : "+v"(o));
+    return o;
+  };
   auto issue = [&](int kt, int buf) {
     if (kt < KT) {
       const uint8_t *ga = a + int64_t(kt) * BK;
@@ -110,14 +142,14 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       for (int c = 0; c < CHA; ++c) {
         const int row = 8 * (wave + NW * c) + lrow;
         const int64_t gk = int64_t(k0) + ((lane & 7) ^ row_swizzle(row)) * 16;
-        const uint4 va = gk < K ? mask_tail(*reinterpret_cast<const uint4 *>(a + (oa[c] + k0)), K - gk) : make_uint4(0u, 0u, 0u, 0u);
+        const uint4 va = gk < K ? mask_tail(*reinterpret_cast<const uint4 *>(a + (here(oa[c]) + k0)), K - gk) : make_uint4(0u, 0u, 0u, 0u);
         *reinterpret_cast<uint4 *>(dA + (wave + NW * c) * 1024 + lane * 16) = va;
       }
 #pragma unroll
       for (int c = 0; c < CHB; ++c) {
         const int row = 8 * (wave + NW * c) + lrow;
         const int64_t gk = int64_t(k0) + ((lane & 7) ^ row_swizzle(row)) * 16;
-        const uint4 vb = gk < K ? mask_tail(*reinterpret_cast<const uint4 *>(b + (ob[c] + k0)), K - gk) : make_uint4(0u, 0u, 0u, 0u);
+        const uint4 vb = gk < K ? mask_tail(*reinterpret_cast<const uint4 *>(b + (here(ob[c]) + k0)), K - gk) : make_uint4(0u, 0u, 0u, 0u);
         *reinterpret_cast<uint4 *>(dB + (wave + NW * c) * 1024 + lane * 16) = vb;
       }
     }
@@ -134,14 +166,21 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
     const uint4 hi = *reinterpret_cast<const uint4 *>(base + f_hi);
     return v8i{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
   };
-  int sa[I], sb[J];  // the fragments' scales, read with them
-  auto read_a = [&](int t, int buf, int i, v8i (&fa)[I]) {
-    fa[i] = frag(smem + buf * STAGE + (wm * TM + i * 16) * BK);
-    if constexpr (SC::kOn) sa[i] = sc.read(smem, wm * TM + i * 16 + fr, t);
+  int sa[I], sb[J];  // the fragments' scales, read with them from pa, pb
+  uint32_t pa = 0, pb = 0;
+  auto scales_at = [&](int t) {
+    if constexpr (SC::kOn) {
+      pa = sc.at(smem, wm * TM + fr, t);
+      pb = sc.at(smem, BM + wn * TN + fr, t);
+    }
   };
-  auto read_b = [&](int t, int buf, int j, v8i (&fb)[J]) {
+  auto read_a = [&](int buf, int i, v8i (&fa)[I]) {
+    fa[i] = frag(smem + buf * STAGE + (wm * TM + i * 16) * BK);
+    if constexpr (SC::kOn) sa[i] = SC::read(pa, i * 16);
+  };
+  auto read_b = [&](int buf, int j, v8i (&fb)[J]) {
     fb[j] = frag(smem + buf * STAGE + (BM + wn * TN + j * 16) * BK);
-    if constexpr (SC::kOn) sb[j] = sc.read(smem, BM + wn * TN + j * 16 + fr, t);
+    if constexpr (SC::kOn) sb[j] = SC::read(pb, j * 16);
   };
 
 #pragma unroll
@@ -150,7 +189,7 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
     for (int j = 0; j < J; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
 
   auto mfma = [&](int i, int j, const v8i (&fa)[I], const v8i (&fb)[J]) {
-    acc[i][j] = mfma_tile<FA, FB, SC::kOn>(fa[i], fb[j], acc[i][j], sa[i], sb[j]);
+    mfma_tile<FA, FB, SC::kOn>(acc[i][j], fa[i], fb[j], sa[i], sb[j]);
   };
   // LDS-bound loads inside the K loop, two instructions each: load d of a K
   // tile lands at stage + 4096 d, so M0 steps by a uniform stride, and the
@@ -180,7 +219,7 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
   // two K tiles ahead (`kt3`), spread over the phase: a K step and a half
   // before it is read.
   auto b_slot = [](int q, int k) { return (k * QA) / CHB + 1 == q; };
-  auto phase_a = [&](int t, int buf, bool dmab, int kt3, v8i (&fa)[I], v8i (&fb)[J]) {
+  auto phase_a = [&](int buf, bool dmab, int kt3, v8i (&fa)[I], v8i (&fb)[J]) {
     const uint8_t *gb = dmab ? b + int64_t(kt3) * BK : b;
     const uint32_t base = dmab ? wblk + uint32_t(buf * STAGE + BM * BK) : wdummy;
     const uint32_t stride = dmab ? uint32_t(NW * 1024) : 0u;
@@ -195,7 +234,7 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       mfma(q % IA, q / IA, fa, fb);
       __builtin_amdgcn_sched_barrier(0);
       if (d >= 0) dma_load(CHA + d, a, gb);
-      if (q % 2 == 0 && q / 2 < IB) read_a(t, buf, IA + q / 2, fa);
+      if (q % 2 == 0 && q / 2 < IB) read_a(buf, IA + q / 2, fa);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -217,7 +256,7 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
     if (q % 4 == 0 && CHA > n12) return q / 4 >= IA && QB / 4 - 1 - q / 4 < CHA - n12;
     return false;
   };
-  auto phase_b = [&](int t, int nbuf, bool dma, int kt2, int buf, v8i (&fa)[I], v8i (&fb)[J]) {
+  auto phase_b = [&](int nbuf, bool dma, int kt2, int buf, v8i (&fa)[I], v8i (&fb)[J]) {
     static_assert(QB % 4 == 0, "phase B slots come in fours");
     const uint8_t *ga = dma ? a + int64_t(kt2) * BK : a;
     const uint8_t *gb = dma ? b + int64_t(kt2) * BK : b;
@@ -236,8 +275,8 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       mfma(i, j, fa, fb);
       __builtin_amdgcn_sched_barrier(0);
       if (ld) dma_load(d, ga, gb);
-      if (q % 4 == 0 && q / 4 < IA) read_a(t + 1, nbuf, q / 4, fa);
-      if (q % IB == IB - 1) read_b(t + 1, nbuf, j, fb);  // last use of B fragment j was this MFMA
+      if (q % 4 == 0 && q / 4 < IA) read_a(nbuf, q / 4, fa);
+      if (q % IB == IB - 1) read_b(nbuf, j, fb);  // last use of B fragment j was this MFMA
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -256,13 +295,14 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     __syncthreads();
+    scales_at(0);
 #pragma unroll
-    for (int j = 0; j < J; ++j) read_b(0, 0, j, fb);
+    for (int j = 0; j < J; ++j) read_b(0, j, fb);
 #pragma unroll
-    for (int i = 0; i < IA; ++i) read_a(0, 0, i, fa);
+    for (int i = 0; i < IA; ++i) read_a(0, i, fa);
     if (T > 1 && KT <= 1) issue(1, 1);  // tile 1 is the partial tail: through registers
     __syncthreads();                       // every wave holds tile 0's B fragments: stage 0's B half is free
-    phase_a(0, 0, 2 < KT, 2, fa, fb);         // and takes tile 2's B part
+    phase_a(0, 2 < KT, 2, fa, fb);         // and takes tile 2's B part
     // tile 1 complete; the CHB most recent loads (tile 2's B part) may still
     // be in flight: the counter completes in order
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
@@ -279,14 +319,16 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       // phase B of tile t, with tile t+2's A part; reads of tile t+1 (in the
       // last iteration they read a stale stage that is never used: always in
       // bounds, and branch-free here)
-      phase_b(t, buf ^ 1, dma, t + 2, buf, fa, fb);
+      scales_at(t + 1);
+      phase_b(buf ^ 1, dma, t + 2, buf, fa, fb);
       if (t + 1 < T) {
         __syncthreads();                   // tile t+1's B fragments read by every wave
-        phase_a(t + 1, buf ^ 1, t + 3 < KT, t + 3, fa, fb);  // with tile t+3's B part
+        phase_a(buf ^ 1, t + 3 < KT, t + 3, fa, fb);  // with tile t+3's B part
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
         __syncthreads();                   // tile t+2 published; tile t+1 fully read
       }
     }
+    settle<SC::kOn>(acc);
   }
 }
 
@@ -367,19 +409,27 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
     v8i a[I], b[J];
     int sa[I], sb[J];  // their scales
   };
-  auto read_a = [&](int t, uint32_t stage, int i, Frags &f) {
-    f.a[i] = frag(stage + uint32_t((wm * TM + i * 16) * BK));
-    if constexpr (SC::kOn) f.sa[i] = sc.read(smem, wm * TM + i * 16 + fr, t);
+  uint32_t pa = 0, pb = 0;  // where the scales of the tile that is read start
+  auto scales_at = [&](int t) {
+    if constexpr (SC::kOn) {
+      pa = sc.at(smem, wm * TM + fr, t);
+      pb = sc.at(smem, BM + wn * TN + fr, t);
+    }
   };
-  auto read_b = [&](int t, uint32_t stage, int j, Frags &f) {
+  auto read_a = [&](uint32_t stage, int i, Frags &f) {
+    f.a[i] = frag(stage + uint32_t((wm * TM + i * 16) * BK));
+    if constexpr (SC::kOn) f.sa[i] = SC::read(pa, i * 16);
+  };
+  auto read_b = [&](uint32_t stage, int j, Frags &f) {
     f.b[j] = frag(stage + uint32_t((BM + wn * TN + j * 16) * BK));
-    if constexpr (SC::kOn) f.sb[j] = sc.read(smem, BM + wn * TN + j * 16 + fr, t);
+    if constexpr (SC::kOn) f.sb[j] = SC::read(pb, j * 16);
   };
   auto read = [&](int t, uint32_t stage, Frags &f) {
+    scales_at(t);
 #pragma unroll
-    for (int i = 0; i < I; ++i) read_a(t, stage, i, f);
+    for (int i = 0; i < I; ++i) read_a(stage, i, f);
 #pragma unroll
-    for (int j = 0; j < J; ++j) read_b(t, stage, j, f);
+    for (int j = 0; j < J; ++j) read_b(stage, j, f);
   };
   // Scales go two groups ahead: at least seven tiles' loads are younger than theirs
   // when they are read, more than the waits leave in flight.
@@ -402,7 +452,7 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
     for (int j = 0; j < J; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
 
   auto mfma = [&](int i, int j, const Frags &f) {
-    acc[i][j] = mfma_tile<FA, FB, SC::kOn>(f.a[i], f.b[j], acc[i][j], f.sa[i], f.sb[j]);
+    mfma_tile<FA, FB, SC::kOn>(acc[i][j], f.a[i], f.b[j], f.sa[i], f.sb[j]);
   };
   uint32_t rd = 0;  // stage of tile t
   // Step t: fragments of tile t are in `cur`; tile t + 1's are read into `nxt`.
@@ -419,6 +469,7 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
     const uint32_t sa = wblk + rd;  // tile t's stage takes tile t + S; load d lands at sa + 4096 d
     rd = rd + STAGE == uint32_t(S * STAGE) ? 0u : rd + STAGE;
     load_scales(t);
+    scales_at(t + 1);
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       __builtin_amdgcn_sched_barrier(0);
@@ -445,9 +496,9 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
       for (int r = 0; r < I + J; ++r)
         if (r * Q / (I + J) == q) {
           if (r < I)
-            read_a(t + 1, rd, r, nxt);
+            read_a(rd, r, nxt);
           else
-            read_b(t + 1, rd, r - I, nxt);
+            read_b(rd, r - I, nxt);
         }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -503,6 +554,7 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
 #pragma unroll
       for (int q = 0; q < Q; ++q) mfma(q / J, q % J, f0);
     }
+    settle<SC::kOn>(acc);
   }
 }
 

@@ -9,6 +9,7 @@ import pytest
 
 from oracle import blocks as ob
 from oracle import fp8
+from tests.act_tiles import TILES
 from tests.gpu_util import dev, torch
 from tests.libqe import need_lib
 from tests.test_gpu_activation import ACT, FMTS, Saved, U, filled, near, untouched, value
@@ -184,6 +185,29 @@ def test_few_blocks_of_a_long_reduction(shape):
     qe, d = need_lib(), dev()
     check_product(qe, d, shape, 1, act="gelu", bias="f32", residual="bf16", pad=3)
     check_product(qe, d, shape, 2, out="f32", bb=1, fa=1, saved="i8", act="silu")
+
+
+@pytest.mark.parametrize("tile", [t for t in TILES if not t[1]], ids=lambda t: t[0][4:])
+def test_every_small_tile(tile):
+    """Products that the tile choice gives to each kernel; with 10 and 11 K tiles, three groups of scales, the last one short."""
+    _, _, m, n, k = tile
+    qe, d = need_lib(), dev()
+    saved = "none" if m * n > 2 ** 20 else "i8"
+    check_product(qe, d, (m, n, k), 5, act="silu", bias="f32", residual="bf16", saved=saved)
+    check_product(qe, d, (m, n, k + 700), 6, bb=1, fa=1, out="f32")
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 1), (37, 53, 100), (256, 128, 128), (300, 520, 384), (513, 259, 1000), (260, 270, 4100), (192, 256, 640)], ids=ids)
+@pytest.mark.parametrize("tile", ["TILE_256x256", "TILE_192x256"])
+def test_large_tiles(tile, shape):
+    qe, d = need_lib(), dev()
+    assert qe.qe_set_gemm_tile(getattr(qe, tile)) == "OK"
+    try:
+        check_product(qe, d, shape, 1, act="gelu", bias="f32", residual="bf16", saved="i8")
+        check_product(qe, d, shape, 2, bb=1, fa=1, out="f32", residual="f32", in_place=True, pad=3)
+        check_product(qe, d, shape, 3, ba=128, bb=1, fb=1)
+    finally:
+        assert qe.qe_set_gemm_tile(qe.TILE_AUTO) == "OK"
 
 
 def test_random_codes_against_float64():

@@ -63,6 +63,7 @@ hipError_t launch_tile(int tile, const BlockGemmParams &p, hipStream_t s) {
     case kTile128x64Deep: return tiles(block_ring_kernel<FA, FB, 128, 64, 6>, 128, 64);
     case kTile64x128: return tiles(block_ring_kernel<FA, FB, 64, 128, 3>, 64, 128);
     case kTile64x128Deep: return tiles(block_ring_kernel<FA, FB, 64, 128, 6>, 64, 128);
+    case kTile128x128: return tiles(block_ring_kernel<FA, FB, 128, 128, 2>, 128, 128);
     case kTile128x128Deep: return tiles(block_ring_kernel<FA, FB, 128, 128, 4>, 128, 128);
     case kTile192x256: return tiles(block_large_kernel<FA, FB, 192, 256>, 192, 256);
     default: return tiles(block_large_kernel<FA, FB, 256, 256>, 256, 256);
@@ -83,7 +84,7 @@ hipError_t launch_block_gemm(const BlockGemmParams &p, hipStream_t s) {
   g.ldc = p.ldc;
   g.out = p.c_bf16 ? 1 : 0;
   constexpr unsigned kShapes = 1u << kTile256x256 | 1u << kTile192x256 | 1u << kTile64x64 | 1u << kTile128x64 |
-                               1u << kTile128x64Deep | 1u << kTile64x128 | 1u << kTile64x128Deep |
+                               1u << kTile128x64Deep | 1u << kTile64x128 | 1u << kTile64x128Deep | 1u << kTile128x128 |
                                1u << kTile128x128Deep;
   const int force = gemm_tile_override();
   const int tile = force == kTileAuto ? (few_blocks(p) ? kFewRowsTile : choose_gemm_tile(g, kShapes))

@@ -25,9 +25,10 @@ struct NoScales {
 // applies to its products by itself: it takes a scale for 32 values of a row, the four
 // of a K tile are the same.  The bytes come four K tiles (a group) at a time, a word
 // of every tile row by an LDS-bound load, and go through BUFS buffers of the groups
-// modulo BUFS at byte `lds` of smem: those of A's rows, then of B's.  Against loads
-// of whole K tiles that is two loads in 64 of a wave (256 x 256 tiles), and one byte
-// read per fragment.
+// modulo BUFS at byte `lds` of smem: those of A's rows, then of B's.  A fragment's
+// word stays in a register for the group's four tiles, and the instruction selects
+// the byte.  Against a group's other traffic that is two LDS-bound loads in 64 of a
+// wave and 16 word reads in 128 of fragments (256 x 256 tiles).
 template <int BM, int BN, int BUFS>
 struct LdsScales {
   static constexpr bool kOn = true;
@@ -49,15 +50,17 @@ struct LdsScales {
                      "s"(__builtin_amdgcn_readfirstlane(to + uint32_t(slot) * 256u)) : "memory", "m0");
     }
   }
-  // Where K tile t's bytes of rows `row` .. start; the compiler sees an address and
+  // Where the words of rows `row` .. of a group start; the compiler sees an address and
   // constants from it, not the parts of it that it would keep one register each for.
-  __device__ __forceinline__ uint32_t at(const uint8_t *smem, int row, int t) const {
-    uint32_t p = uint32_t(reinterpret_cast<uintptr_t>(smem)) + lds + uint32_t((t >> 2) & (BUFS - 1)) * kBuf + uint32_t(t & 3) +
-                 uint32_t(row) * 4u;
+  __device__ __forceinline__ uint32_t at(const uint8_t *smem, int row, int group) const {
+    uint32_t p = uint32_t(reinterpret_cast<uintptr_t>(smem)) + lds + uint32_t(group & (BUFS - 1)) * kBuf + uint32_t(row) * 4u;
     asm("" : "+v"(p));
     return p;
   }
   static __device__ __forceinline__ int read(uint32_t p, int rows) {
+    return *reinterpret_cast<const __attribute__((address_space(3))) int *>(p + uint32_t(rows) * 4u);
+  }
+  static __device__ __forceinline__ int read_byte(uint32_t p, int rows) {
     return *reinterpret_cast<const __attribute__((address_space(3))) uint8_t *>(p + uint32_t(rows) * 4u);
   }
 };
@@ -68,14 +71,24 @@ struct LdsScales {
 // 140).  The assembler adds no waits: s_nop 1 stands for what a vector instruction
 // that wrote an operand needs, products of the same accumulator are at least three
 // others apart in the loops, and settle() comes before anything else reads them.
-template <int FA, int FB, bool SCALED>
+// BYTE: which byte of sa, sb is the K tile's.
+#define QE_MFMA_SCALED(SEL)                                                                                       \
+  asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 " SEL " cbsz:%5 blgp:%6"       \
+               : "+a"(acc) : "v"(b), "v"(a), "v"(sb), "v"(sa), "n"(FB), "n"(FA))
+template <int FA, int FB, bool SCALED, int BYTE>
 __device__ __forceinline__ void mfma_tile(v4f &acc, const v8i &a, const v8i &b, int sa, int sb) {
-  if constexpr (SCALED)
-    asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:%5 blgp:%6"
-                 : "+a"(acc) : "v"(b), "v"(a), "v"(sb), "v"(sa), "n"(FB), "n"(FA));
-  else
+  if constexpr (!SCALED)
     acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, FB, FA, 0, 0, 0, 0);
+  else if constexpr (BYTE == 0)
+    QE_MFMA_SCALED("op_sel_hi:[0,0,0]");
+  else if constexpr (BYTE == 1)
+    QE_MFMA_SCALED("op_sel:[1,1,0] op_sel_hi:[0,0,0]");
+  else if constexpr (BYTE == 2)
+    QE_MFMA_SCALED("op_sel_hi:[1,1,0]");
+  else
+    QE_MFMA_SCALED("op_sel:[1,1,0] op_sel_hi:[1,1,0]");
 }
+#undef QE_MFMA_SCALED
 // After the last of them: longer than the instruction takes to write its result (12 wait states).
 template <bool SCALED, int I, int J>
 __device__ __forceinline__ void settle(v4f (&acc)[I][J]) {
@@ -103,7 +116,7 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
   constexpr int STAGE = (BM + BN) * BK;
   static_assert(CHA * NW * 1024 == BM * BK, "LDS-bound load d of a tile lands at stage + 4096 d");
   const int lane = threadIdx.x & 63;
-  const int wave = threadIdx.x >> 6;
+  const int wave = SC::kOn ? __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6) : int(threadIdx.x) >> 6;
   const int wm = wave >> 1, wn = wave & 1;
   const int lrow = lane >> 3;
   const int KT = int(K / BK);
@@ -168,19 +181,20 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
   };
   int sa[I], sb[J];  // the fragments' scales, read with them from pa, pb
   uint32_t pa = 0, pb = 0;
-  auto scales_at = [&](int t) {
+  auto scales_at = [&](int group) {
     if constexpr (SC::kOn) {
-      pa = sc.at(smem, wm * TM + fr, t);
-      pb = sc.at(smem, BM + wn * TN + fr, t);
+      pa = sc.at(smem, wm * TM + fr, group);
+      pb = sc.at(smem, BM + wn * TN + fr, group);
     }
   };
-  auto read_a = [&](int buf, int i, v8i (&fa)[I]) {
+  // `byte`: that of the tile, t % 4; the group's words come with its first tile.
+  auto read_a = [&](auto byte, int buf, int i, v8i (&fa)[I]) {
     fa[i] = frag(smem + buf * STAGE + (wm * TM + i * 16) * BK);
-    if constexpr (SC::kOn) sa[i] = SC::read(pa, i * 16);
+    if constexpr (SC::kOn && decltype(byte)::value == 0) sa[i] = SC::read(pa, i * 16);
   };
-  auto read_b = [&](int buf, int j, v8i (&fb)[J]) {
+  auto read_b = [&](auto byte, int buf, int j, v8i (&fb)[J]) {
     fb[j] = frag(smem + buf * STAGE + (BM + wn * TN + j * 16) * BK);
-    if constexpr (SC::kOn) sb[j] = SC::read(pb, j * 16);
+    if constexpr (SC::kOn && decltype(byte)::value == 0) sb[j] = SC::read(pb, j * 16);
   };
 
 #pragma unroll
@@ -188,8 +202,8 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
 #pragma unroll
     for (int j = 0; j < J; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
 
-  auto mfma = [&](int i, int j, const v8i (&fa)[I], const v8i (&fb)[J]) {
-    mfma_tile<FA, FB, SC::kOn>(acc[i][j], fa[i], fb[j], sa[i], sb[j]);
+  auto mfma = [&](auto byte, int i, int j, const v8i (&fa)[I], const v8i (&fb)[J]) {
+    mfma_tile<FA, FB, SC::kOn, decltype(byte)::value>(acc[i][j], fa[i], fb[j], sa[i], sb[j]);
   };
   // LDS-bound loads inside the K loop, two instructions each: load d of a K
   // tile lands at stage + 4096 d, so M0 steps by a uniform stride, and the
@@ -219,7 +233,7 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
   // two K tiles ahead (`kt3`), spread over the phase: a K step and a half
   // before it is read.
   auto b_slot = [](int q, int k) { return (k * QA) / CHB + 1 == q; };
-  auto phase_a = [&](int buf, bool dmab, int kt3, v8i (&fa)[I], v8i (&fb)[J]) {
+  auto phase_a = [&](auto byte, int buf, bool dmab, int kt3, v8i (&fa)[I], v8i (&fb)[J]) {
     const uint8_t *gb = dmab ? b + int64_t(kt3) * BK : b;
     const uint32_t base = dmab ? wblk + uint32_t(buf * STAGE + BM * BK) : wdummy;
     const uint32_t stride = dmab ? uint32_t(NW * 1024) : 0u;
@@ -231,10 +245,10 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       __builtin_amdgcn_sched_barrier(0);
       if (d >= 0) dma_m0(d, base, stride);
       __builtin_amdgcn_sched_barrier(0);
-      mfma(q % IA, q / IA, fa, fb);
+      mfma(byte, q % IA, q / IA, fa, fb);
       __builtin_amdgcn_sched_barrier(0);
       if (d >= 0) dma_load(CHA + d, a, gb);
-      if (q % 2 == 0 && q / 2 < IB) read_a(buf, IA + q / 2, fa);
+      if (q % 2 == 0 && q / 2 < IB) read_a(byte, buf, IA + q / 2, fa);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -256,8 +270,9 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
     if (q % 4 == 0 && CHA > n12) return q / 4 >= IA && QB / 4 - 1 - q / 4 < CHA - n12;
     return false;
   };
-  auto phase_b = [&](int nbuf, bool dma, int kt2, int buf, v8i (&fa)[I], v8i (&fb)[J]) {
+  auto phase_b = [&](auto byte, int nbuf, bool dma, int kt2, int buf, v8i (&fa)[I], v8i (&fb)[J]) {
     static_assert(QB % 4 == 0, "phase B slots come in fours");
+    constexpr std::integral_constant<int, (decltype(byte)::value + 1) % 4> next{};
     const uint8_t *ga = dma ? a + int64_t(kt2) * BK : a;
     const uint8_t *gb = dma ? b + int64_t(kt2) * BK : b;
     const uint32_t base = dma ? wblk + uint32_t(buf * STAGE) : wdummy;
@@ -272,17 +287,18 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       __builtin_amdgcn_sched_barrier(0);
       if (ld) dma_m0(d, base, stride);
       __builtin_amdgcn_sched_barrier(0);  // M0 is written before the MFMA, never next to the load
-      mfma(i, j, fa, fb);
+      mfma(byte, i, j, fa, fb);
       __builtin_amdgcn_sched_barrier(0);
       if (ld) dma_load(d, ga, gb);
-      if (q % 4 == 0 && q / 4 < IA) read_a(nbuf, q / 4, fa);
-      if (q % IB == IB - 1) read_b(nbuf, j, fb);  // last use of B fragment j was this MFMA
+      if (q % 4 == 0 && q / 4 < IA) read_a(next, nbuf, q / 4, fa);
+      if (q % IB == IB - 1) read_b(next, nbuf, j, fb);  // last use of B fragment j was this MFMA
     }
     __builtin_amdgcn_sched_barrier(0);
   };
 
   if (T > 0) {
     v8i fa[I], fb[J];
+    constexpr std::integral_constant<int, 0> first{};
     if constexpr (SC::kOn) sc.load(smem, wave, 0);  // the first loads: complete whenever a tile's are
     issue(0, 0);
     if (KT > 1) {
@@ -297,36 +313,45 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
     __syncthreads();
     scales_at(0);
 #pragma unroll
-    for (int j = 0; j < J; ++j) read_b(0, j, fb);
+    for (int j = 0; j < J; ++j) read_b(first, 0, j, fb);
 #pragma unroll
-    for (int i = 0; i < IA; ++i) read_a(0, i, fa);
+    for (int i = 0; i < IA; ++i) read_a(first, 0, i, fa);
     if (T > 1 && KT <= 1) issue(1, 1);  // tile 1 is the partial tail: through registers
     __syncthreads();                       // every wave holds tile 0's B fragments: stage 0's B half is free
-    phase_a(0, 2 < KT, 2, fa, fb);         // and takes tile 2's B part
+    phase_a(first, 0, 2 < KT, 2, fa, fb);         // and takes tile 2's B part
     // tile 1 complete; the CHB most recent loads (tile 2's B part) may still
     // be in flight: the counter completes in order
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
     __syncthreads();                       // tile 1 published; tile 0 fully read
-    for (int t = 0; t < T; ++t) {
-      const int buf = t & 1;
+    auto step = [&](int t, int buf, auto byte) {
+      constexpr std::integral_constant<int, (decltype(byte)::value + 1) % 4> next{};
       const bool dma = t + 2 < KT;
       if (t + 2 < T && !dma) issue(t + 2, buf);
       // The next group's scales, into the buffer whose last reads were of tile t - 1.
       // They are older than the B part below, so the wait at this step's end covers
       // them: three steps before they are read.
-      if constexpr (SC::kOn)
-        if ((t & 3) == 0) sc.load(smem, wave, (t >> 2) + 1);
+      if constexpr (SC::kOn && decltype(byte)::value == 0) sc.load(smem, wave, t / 4 + 1);
+      if constexpr (SC::kOn && decltype(next)::value == 0) scales_at(t / 4 + 1);
       // phase B of tile t, with tile t+2's A part; reads of tile t+1 (in the
       // last iteration they read a stale stage that is never used: always in
       // bounds, and branch-free here)
-      scales_at(t + 1);
-      phase_b(buf ^ 1, dma, t + 2, buf, fa, fb);
+      phase_b(byte, buf ^ 1, dma, t + 2, buf, fa, fb);
       if (t + 1 < T) {
         __syncthreads();                   // tile t+1's B fragments read by every wave
-        phase_a(buf ^ 1, t + 3 < KT, t + 3, fa, fb);  // with tile t+3's B part
+        phase_a(next, buf ^ 1, t + 3 < KT, t + 3, fa, fb);  // with tile t+3's B part
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
         __syncthreads();                   // tile t+2 published; tile t+1 fully read
       }
+    };
+    if constexpr (SC::kOn) {  // four tiles a turn: which byte is part of the instruction
+      for (int t = 0; t < T; t += 4) {
+        step(t, 0, first);
+        if (t + 1 < T) step(t + 1, 1, std::integral_constant<int, 1>{});
+        if (t + 2 < T) step(t + 2, 0, std::integral_constant<int, 2>{});
+        if (t + 3 < T) step(t + 3, 1, std::integral_constant<int, 3>{});
+      }
+    } else {
+      for (int t = 0; t < T; ++t) step(t, t & 1, first);
     }
     settle<SC::kOn>(acc);
   }
@@ -356,7 +381,7 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
   constexpr int STAGE = (BM + BN) * BK;
   static_assert((S - 1) * L < 64, "the load counter holds 63");
   const int lane = threadIdx.x & 63;
-  const int wave = threadIdx.x >> 6;
+  const int wave = SC::kOn ? __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6) : int(threadIdx.x) >> 6;
   const int wm = wave >> 1, wn = wave & 1;
   const int lrow = lane >> 3;
   const int ktail = K % BK;
@@ -412,17 +437,17 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
   uint32_t pa = 0, pb = 0;  // where the scales of the tile that is read start
   auto scales_at = [&](int t) {
     if constexpr (SC::kOn) {
-      pa = sc.at(smem, wm * TM + fr, t);
-      pb = sc.at(smem, BM + wn * TN + fr, t);
+      pa = sc.at(smem, wm * TM + fr, t / 4) + uint32_t(t % 4);
+      pb = sc.at(smem, BM + wn * TN + fr, t / 4) + uint32_t(t % 4);
     }
   };
   auto read_a = [&](uint32_t stage, int i, Frags &f) {
     f.a[i] = frag(stage + uint32_t((wm * TM + i * 16) * BK));
-    if constexpr (SC::kOn) f.sa[i] = SC::read(pa, i * 16);
+    if constexpr (SC::kOn) f.sa[i] = SC::read_byte(pa, i * 16);
   };
   auto read_b = [&](uint32_t stage, int j, Frags &f) {
     f.b[j] = frag(stage + uint32_t((BM + wn * TN + j * 16) * BK));
-    if constexpr (SC::kOn) f.sb[j] = SC::read(pb, j * 16);
+    if constexpr (SC::kOn) f.sb[j] = SC::read_byte(pb, j * 16);
   };
   auto read = [&](int t, uint32_t stage, Frags &f) {
     scales_at(t);
@@ -452,7 +477,7 @@ __device__ __forceinline__ void ring_k_loop(const uint8_t *a, const uint8_t *b, 
     for (int j = 0; j < J; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
 
   auto mfma = [&](int i, int j, const Frags &f) {
-    mfma_tile<FA, FB, SC::kOn>(acc[i][j], f.a[i], f.b[j], f.sa[i], f.sb[j]);
+    mfma_tile<FA, FB, SC::kOn, 0>(acc[i][j], f.a[i], f.b[j], f.sa[i], f.sb[j]);
   };
   uint32_t rd = 0;  // stage of tile t
   // Step t: fragments of tile t are in `cur`; tile t + 1's are read into `nxt`.

@@ -1294,7 +1294,7 @@ qe_status qe_residual_norm(const qe_matrix *x_host, const qe_matrix *y_host, int
   p.pre_weight = d.pre_weight;
   p.gate = d.gate;
   p.ld_gate = d.ld_gate;
-  p.gate_rows = d.gate_rows;
+  p.gate_rows = d.gate_rows < rows ? d.gate_rows : rows;
   p.post_rstd = post_rstd;
   p.pre_rstd = pre_rstd;
   p.post_norm = d.post_norm;

@@ -252,7 +252,6 @@ struct ResidualParams {
   MatrixRef x, y, r, h;
   BlockedRef row;
   int64_t rows, cols;
-  int64_t row0;  // the launch's first row
   const void *post_weight, *pre_weight, *gate;
   int64_t ld_gate, gate_rows;
   float *post_rstd, *pre_rstd;
@@ -261,7 +260,7 @@ struct ResidualParams {
   int32_t pad;
 };
 
-// The gradients of that.  sums: per chunk of kGradRows rows, cols partial sums of
+// The gradients of that.  sums: per chunk of kGradRows rows or more, cols partial sums of
 // dh n and then of db yn (see residual_norm.hip).
 constexpr int64_t kGradRows = 16;
 struct ResidualGradParams {

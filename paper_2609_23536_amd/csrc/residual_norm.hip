@@ -8,16 +8,17 @@
 //
 // Backward, with n = r f(r), m = y f(y):
 //     t = dr + f(r) (d - n mean(d n)),  d = dh (o + w_pre)
-//     dx = x_scale t,   b = y_scale t (the gradient of gate p),   dw_pre = sum dh n
-//     dy = f(y) (e - m mean(e m)),  e = b gate (o + w_post)  (or b gate)
-// and with S = sum b m over the rows that share a row of gates:
+//     dx = x_scale t,   dw_pre = sum dh n
+//     dy = f(y) (e - m mean(e m)),  e = t c,  c = y_scale gate (o + w_post)
+// and with S = y_scale sum t m over the rows that share a row of gates:
 //     dgate = S (o + w_post),   dw_post = sum over the gates' rows of S gate
 // so one sum of columns serves both.
 //
-// Both are bound by memory.  Forward: one workgroup a row, which stays in registers
-// between the two sums.  Backward: a workgroup takes up to 16 rows that share their
-// gates, one after the other, and keeps the column sums in registers; they go to the
-// workspace once per 16 rows, and a second kernel adds them in a fixed order.
+// Both are bound by memory, and next by their vector instructions.  A workgroup takes
+// one row after the other, each by a team of lanes that hold eight neighbouring values
+// (or twice eight) of it in registers from the loads to the stores; what a column's
+// weights and gates come to is kept in registers from row to row, and the next row is
+// loaded before this one's sums are taken.
 #include "block_scale.h"
 
 #include <algorithm>
@@ -32,9 +33,11 @@ template <int CTRL>
 __device__ __forceinline__ float add_dpp(float v) {
   return v + __uint_as_float(uint32_t(__builtin_amdgcn_mov_dpp(int(__float_as_uint(v)), CTRL, 0xf, 0xf, true)));
 }
-// Sum over the wave, in all lanes: lanes l ^ 1, l ^ 2, 7 - l and 15 - l within 8 and 16, then l ^ 16 and l ^ 32.
+// Sum over an aligned group of 16 lanes, in all of them: lanes l ^ 1, l ^ 2, then 7 - l and 15 - l.
+__device__ __forceinline__ float sum_lanes16(float v) { return add_dpp<0x140>(add_dpp<0x141>(add_dpp<0x4e>(add_dpp<0xb1>(v)))); }
+// Sum over the wave, in all lanes.
 __device__ __forceinline__ float wave_sum(float v) {
-  v = add_dpp<0x140>(add_dpp<0x141>(add_dpp<0x4e>(add_dpp<0xb1>(v))));
+  v = sum_lanes16(v);
   uint32_t b = __float_as_uint(v);
   auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
   b = __float_as_uint(__uint_as_float(r[0]) + __uint_as_float(r[1]));
@@ -42,17 +45,16 @@ __device__ __forceinline__ float wave_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Sum over the workgroup, in all lanes; `red`: one float per wave, which no sum before
-// the last one has used (a lane may still be reading what that one left).
-__device__ __forceinline__ float group_sum(float v, float *red) {
+// Sum over the team of 2^k (at most 16) waves that this wave is in, in all its lanes.
+// `red`: one float per wave of the workgroup, which no sum before the last one has used
+// (a lane may still be reading what that one left).  All waves of the workgroup come here.
+__device__ __forceinline__ float team_sum(float v, float *red, int waves) {
   v = wave_sum(v);
-  const int waves = int(blockDim.x) >> 6;
   if (waves == 1) return v;
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  const int wave = int(threadIdx.x) >> 6, l = int(threadIdx.x) & 15;
+  if ((threadIdx.x & 63) == 0) red[wave] = v;
   __syncthreads();
-  v = red[0];
-  for (int w = 1; w < waves; ++w) v += red[w];
-  return v;
+  return sum_lanes16(l < waves ? red[(wave & -waves) + l] : 0.0f);
 }
 
 // offset + weight of eight columns (1 without weights)
@@ -72,147 +74,204 @@ __device__ __forceinline__ bool is_bf16(const MatrixRef &m) {
   return BF16 || m.bf16 != 0;
 }
 
-template <int NV, bool BF16>
-__global__ __launch_bounds__(kLanes) void residual_norm_kernel(ResidualParams p) {
-  __shared__ float red[2][16];
-  const int tid = threadIdx.x;
-  const int64_t row = p.row0 + blockIdx.x;
-  const float inv_cols = 1.0f / float(p.cols);
-  const MatrixRef gates{const_cast<void *>(p.gate), p.ld_gate, p.gate_bf16, 0};
-  float r[NV][8];
+// A lane's columns of a row: NV times eight neighbouring ones, `lanes` lanes a row.
+template <int NV>
+struct Columns {
   uint32_t col[NV];
-  int n[NV];
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    col[v] = (uint32_t(v) * blockDim.x + tid) * 8;
-    n[v] = max(0, min(8, int(p.cols) - int(col[v])));
-  }
-  float x[NV][8];
-  if (p.x.data != nullptr) {
-#pragma unroll
-    for (int v = 0; v < NV; ++v) load8(row_of(p.x, is_bf16<BF16>(p.x), row), is_bf16<BF16>(p.x), col[v], n[v], x[v]);
-  }
-  if (p.y.data != nullptr) {
-    float sum = 0.0f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) load8(row_of(p.y, is_bf16<BF16>(p.y), row), is_bf16<BF16>(p.y), col[v], n[v], r[v]);
-    float f = 1.0f;
-    if (p.post_norm) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(r[v][e], r[v][e], sum);
-      f = 1.0f / __builtin_sqrtf(group_sum(sum, red[0]) * inv_cols + p.post_eps);
-      if (tid == 0 && p.post_rstd != nullptr) p.post_rstd[row] = f;
-    }
+  int n[NV];  // those that exist
+  __device__ __forceinline__ Columns(int lane, int lanes, int64_t cols) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      if (p.post_norm) {
-        float w[8];
-        weights8(p.post_weight, p.weight_bf16 != 0, col[v], n[v], p.offset, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[v][e] = r[v][e] * f * w[e];
-      }
-      if (p.gate != nullptr) {
-        float g[8];
-        load8(row_of(gates, p.gate_bf16 != 0, row / p.gate_rows), p.gate_bf16 != 0, col[v], n[v], g);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[v][e] *= g[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) r[v][e] *= p.y_scale;
-    }
-    if (p.x.data != nullptr) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[v][e] = __builtin_fmaf(p.x_scale, x[v][e], r[v][e]);
-    }
-  } else {
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) r[v][e] = p.x_scale * x[v][e];
-  }
-  if (p.r.data != nullptr) {
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      store8(row_of(p.r, is_bf16<BF16>(p.r), row), is_bf16<BF16>(p.r), col[v], n[v], r[v]);
-      if (is_bf16<BF16>(p.r)) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[v][e] = bf16_to_f32(bf16_bits(r[v][e]));
-      }
-    }
-  }
-  if (!p.pre_norm) return;
-  float sum = 0.0f;
-#pragma unroll
-  for (int v = 0; v < NV; ++v)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(r[v][e], r[v][e], sum);
-  const float f = 1.0f / __builtin_sqrtf(group_sum(sum, red[1]) * inv_cols + p.pre_eps);
-  if (tid == 0 && p.pre_rstd != nullptr) p.pre_rstd[row] = f;
-  if (p.h.data == nullptr && p.row.data == nullptr) return;
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    float w[8], h[8];
-    weights8(p.pre_weight, p.weight_bf16 != 0, col[v], n[v], p.offset, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = e < n[v] ? r[v][e] * f * w[e] : 0.0f;
-    if (p.h.data != nullptr) store8(row_of(p.h, is_bf16<BF16>(p.h), row), is_bf16<BF16>(p.h), col[v], n[v], h);
-    if (p.row.data != nullptr) {
-      const float a = max_lanes16(nan_max(amax4(f32x4{h[0], h[1], h[2], h[3]}), amax4(f32x4{h[4], h[5], h[6], h[7]})));
-      uint8_t *dst = p.row.data + row * p.row.ld + col[v];
-      const uint32_t byte = p.row.fmt == 0 ? block_byte<0>(a) : block_byte<1>(a);
-      const float mult = block_mult(byte);
-      if (p.row.fmt == 0)
-        store_codes8(dst, n[v], block_codes<0>(h, mult), block_codes<0>(h + 4, mult));
-      else
-        store_codes8(dst, n[v], block_codes<1>(h, mult), block_codes<1>(h + 4, mult));
-      if ((tid & 15) == 0 && n[v] > 0) p.row.exps[row * p.row.ld_exps + col[v] / kBlock] = uint8_t(byte);
-    }
-  }
-}
-
-// Eight values of a row as they are stored, where that is BF16: four registers.
-__device__ __forceinline__ u32x4_in fetch8(const void *base, uint32_t at, int n) {
-  const uint16_t *p = static_cast<const uint16_t *>(base) + at;
-  if (n >= 8) return *reinterpret_cast<const u32x4_in *>(p);
-  u32x4_in w = {0u, 0u, 0u, 0u};
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (e < n) w[e / 2] |= uint32_t(p[e]) << (16 * (e % 2));
-  return w;
-}
-
-// A row of one of the gradient's inputs.  Where all matrices are BF16 (and a lane has one vector) it is fetched a
-// row ahead, so that the next row is on its way during this one's sums.
-template <int NV, bool BF16>
-struct Row {
-  static constexpr bool kAhead = BF16 && NV == 1;
-  u32x4_in w[kAhead ? NV : 1];
-  __device__ __forceinline__ void fetch(const MatrixRef &m, int64_t row, const uint32_t (&col)[NV], const int (&n)[NV]) {
-    if constexpr (kAhead) {
-      if (m.data == nullptr) return;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) w[v] = fetch8(row_of(m, true, row), col[v], n[v]);
-    }
-  }
-  __device__ __forceinline__ void get(const MatrixRef &m, int64_t row, uint32_t col, int n, int v, float *f) const {
-    if constexpr (kAhead) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f[2 * e] = __uint_as_float(w[v][e] << 16);
-        f[2 * e + 1] = __uint_as_float(w[v][e] & 0xffff0000u);
-      }
-    } else {
-      load8(row_of(m, is_bf16<BF16>(m), row), is_bf16<BF16>(m), col, n, f);
+      col[v] = uint32_t(v * lanes + lane) * 8;
+      n[v] = max(0, min(8, int(cols) - int(col[v])));
     }
   }
 };
 
-// Column sums of a lane's eight columns: in registers with one vector a lane, in LDS
-// (the lane's own 16-byte slots) with two, where 128 registers a lane do not hold them.
+// A row of an input.  kAhead: BF16, kept as it is stored from the moment it is fetched, a
+// row before it is used.  kEarly: fetched as values when its row begins, so that the loads of
+// a row wait for each other once.  kLate: loaded when it is used.
+enum Fetch { kLate = 0, kEarly = 1, kAhead = 2 };
+template <int NV, bool BF16, int WHEN>
+struct Row {
+  static_assert(BF16 || WHEN != kAhead, "four registers hold eight values");
+  u32x4_in w[WHEN == kAhead ? NV : 1];
+  float f[WHEN == kEarly ? NV : 1][8];
+  __device__ __forceinline__ void fetch(const MatrixRef &m, int64_t row, const Columns<NV> &c) {
+    if (WHEN == kLate || m.data == nullptr) return;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if constexpr (WHEN == kEarly) {
+        load8(row_of(m, is_bf16<BF16>(m), row), is_bf16<BF16>(m), c.col[v], c.n[v], f[v]);
+      } else if constexpr (WHEN == kAhead) {
+        const uint16_t *p = reinterpret_cast<const uint16_t *>(row_of(m, true, row)) + c.col[v];
+        if (c.n[v] >= 8) {
+          w[v] = *reinterpret_cast<const u32x4_in *>(p);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            w[v][e] = (2 * e < c.n[v] ? uint32_t(p[2 * e]) : 0u) | (2 * e + 1 < c.n[v] ? uint32_t(p[2 * e + 1]) << 16 : 0u);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void get(const MatrixRef &m, int64_t row, const Columns<NV> &c, int v, float *out) const {
+    if constexpr (WHEN == kAhead) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        out[2 * e] = __uint_as_float(w[v][e] << 16);
+        out[2 * e + 1] = __uint_as_float(w[v][e] & 0xffff0000u);
+      }
+    } else if constexpr (WHEN == kEarly) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[e] = f[v][e];
+    } else {
+      load8(row_of(m, is_bf16<BF16>(m), row), is_bf16<BF16>(m), c.col[v], c.n[v], out);
+    }
+  }
+};
+
+// y_scale gate (o + w_post) of a vector of columns: what a row of gates makes of y's norm.
+template <int NV, typename P>
+__device__ __forceinline__ void branch_factors(const P &p, int64_t group, const Columns<NV> &c, int v, float *f) {
+  const MatrixRef gates{const_cast<void *>(p.gate), p.ld_gate, p.gate_bf16, 0};
+  float g[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = g[e] = 1.0f;
+  if (p.post_norm) weights8(p.post_weight, p.weight_bf16 != 0, c.col[v], c.n[v], p.offset, f);
+  if (p.gate != nullptr) load8(row_of(gates, p.gate_bf16 != 0, group), p.gate_bf16 != 0, c.col[v], c.n[v], g);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] *= g[e] * p.y_scale;
+}
+
+// A workgroup takes rows blockIdx.x, + gridDim.x, .. of the launch.
+// NV 1: 64 registers, so that a unit holds two workgroups of 1024 lanes.
+template <int NV, bool BF16>
+__global__ __launch_bounds__(kLanes, NV == 1 ? 8 : 4) void residual_norm_kernel(ResidualParams p) {
+  __shared__ float reds[4][kLanes / 64];
+  const int tid = threadIdx.x, waves = int(blockDim.x) >> 6;
+  const float inv_cols = 1.0f / float(p.cols);
+  const Columns<NV> c(tid, int(blockDim.x), p.cols);
+  const bool has_x = p.x.data != nullptr, has_y = p.y.data != nullptr;
+  // The columns' factors stay here, those of y's norm in registers and those of r's,
+  // which 64 registers do not hold as well, in the lane's own 16-byte slots of LDS.
+  constexpr bool KEEP = NV == 1;
+  __shared__ __attribute__((aligned(16))) f32x4 slots[KEEP ? 2 * kLanes : 1];
+  Row<NV, BF16, BF16 ? kAhead : kLate> x, y;
+  x.fetch(p.x, blockIdx.x, c);
+  y.fetch(p.y, blockIdx.x, c);
+  float branch[NV][8];
+  if constexpr (KEEP) {
+    float w[8];
+    weights8(p.pre_weight, p.weight_bf16 != 0, c.col[0], c.n[0], p.offset, w);
+    slots[tid] = f32x4{w[0], w[1], w[2], w[3]};
+    slots[kLanes + tid] = f32x4{w[4], w[5], w[6], w[7]};
+  }
+  const uint32_t gate_rows = uint32_t(p.gate_rows);
+  uint32_t group = 0, group_end = 0;  // of the gates in `branch`
+  int turn = 0;
+#pragma unroll 1
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, ++turn) {
+    float(*red)[kLanes / 64] = reds + 2 * (turn & 1);
+    const int64_t next = row + gridDim.x;
+    if (has_y) {
+      if (row >= group_end) {
+        group = p.gate != nullptr ? uint32_t(row) / gate_rows : 0u;
+        group_end = p.gate != nullptr ? (group + 1u) * gate_rows : 0xffffffffu;
+        if constexpr (KEEP) branch_factors<NV>(p, group, c, 0, branch[0]);
+      }
+    }
+    float r[NV][8];
+    auto add_x = [&](int v) {  // r = x_scale x + r
+      float f[8];
+      x.get(p.x, row, c, v, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[v][e] = __builtin_fmaf(p.x_scale, f[e], r[v][e]);
+    };
+    if (has_y) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) y.get(p.y, row, c, v, r[v]);
+      if (next < p.rows) y.fetch(p.y, next, c);
+      float f = 1.0f;
+      if (p.post_norm) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(r[v][e], r[v][e], sum);
+        f = 1.0f / __builtin_sqrtf(team_sum(sum, red[0], waves) * inv_cols + p.post_eps);
+        if (tid == 0 && p.post_rstd != nullptr) p.post_rstd[row] = f;
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        if constexpr (!KEEP) branch_factors<NV>(p, group, c, v, branch[v]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[v][e] = r[v][e] * f * branch[v][e];
+        if (has_x) add_x(v);
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        x.get(p.x, row, c, v, r[v]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[v][e] *= p.x_scale;
+      }
+    }
+    if (next < p.rows) x.fetch(p.x, next, c);
+    if (p.r.data != nullptr) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        store8(row_of(p.r, is_bf16<BF16>(p.r), row), is_bf16<BF16>(p.r), c.col[v], c.n[v], r[v]);
+        if (is_bf16<BF16>(p.r)) {
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const uint32_t w = bf16x2_bits(r[v][e], r[v][e + 1]);
+            r[v][e] = __uint_as_float(w << 16);
+            r[v][e + 1] = __uint_as_float(w & 0xffff0000u);
+          }
+        }
+      }
+    }
+    if (!p.pre_norm) continue;
+    float sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(r[v][e], r[v][e], sum);
+    const float f = 1.0f / __builtin_sqrtf(team_sum(sum, red[1], waves) * inv_cols + p.pre_eps);
+    if (tid == 0 && p.pre_rstd != nullptr) p.pre_rstd[row] = f;
+    if (p.h.data == nullptr && p.row.data == nullptr) continue;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float h[8], w[8];
+      if constexpr (KEEP) {
+        const f32x4 lo = slots[tid], hi = slots[kLanes + tid];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = e < 4 ? lo[e % 4] : hi[e % 4];
+      } else {
+        weights8(p.pre_weight, p.weight_bf16 != 0, c.col[v], c.n[v], p.offset, w);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[e] = r[v][e] * f * w[e];
+      if (p.h.data != nullptr) store8(row_of(p.h, is_bf16<BF16>(p.h), row), is_bf16<BF16>(p.h), c.col[v], c.n[v], h);
+      if (p.row.data != nullptr) {
+        // (columns past the last one are 0, or NaN where the whole row is)
+        const float a = max_lanes16(nan_max(amax4(f32x4{h[0], h[1], h[2], h[3]}), amax4(f32x4{h[4], h[5], h[6], h[7]})));
+        uint8_t *dst = (p.row.data + row * p.row.ld) + c.col[v];
+        const uint32_t byte = p.row.fmt == 0 ? block_byte<0>(a) : block_byte<1>(a);
+        const float mult = block_mult(byte);
+        if (p.row.fmt == 0)
+          store_codes8(dst, c.n[v], block_codes<0>(h, mult), block_codes<0>(h + 4, mult));
+        else
+          store_codes8(dst, c.n[v], block_codes<1>(h, mult), block_codes<1>(h + 4, mult));
+        if ((tid & 15) == 0 && c.n[v] > 0) (p.row.exps + row * p.row.ld_exps)[c.col[v] / kBlock] = uint8_t(byte);
+      }
+    }
+  }
+}
+
+// Column sums of a lane's columns: in registers with eight of them, in LDS (the lane's
+// own 16-byte slots) with sixteen, where 128 registers a lane do not hold them.
 template <int NV>
 struct ColumnSums {
   static constexpr bool kInLds = NV > 1;
@@ -239,87 +298,109 @@ struct ColumnSums {
         reg[h] = s;
     }
   }
-  __device__ __forceinline__ void store(float *row, int v, uint32_t col, int n) const {
+  // With one vector: the sums of all teams of `lanes` lanes, in the first team's, in their order.
+  __device__ __forceinline__ void join(int lanes) {
+    if constexpr (!kInLds) {
+      lds[0] = reg[0];
+      lds[kLanes] = reg[1];
+      __syncthreads();
+      if (int(threadIdx.x) < lanes)
+        for (int at = lanes; at < int(blockDim.x); at += lanes) {
+          reg[0] += lds[at];
+          reg[1] += lds[kLanes + at];
+        }
+    }
+  }
+  __device__ __forceinline__ void store(float *row, int v, uint32_t col, int n, float scale) const {
     float f[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = kInLds ? lds[(2 * v + e / 4) * kLanes][e % 4] : reg[kInLds ? 0 : e / 4][e % 4];
+    for (int e = 0; e < 8; ++e) f[e] = scale * (kInLds ? lds[(2 * v + e / 4) * kLanes][e % 4] : reg[kInLds ? 0 : e / 4][e % 4]);
     store8(row, false, col, n, f);
   }
 };
 
-// Chunks of up to kGradRows rows: `per_group` of them for each group of gate_rows rows.
+// Chunks of up to chunk_rows rows, `per_group` of them for each group of gate_rows rows;
+// a chunk is a workgroup, whose teams of `lanes` lanes take every so manyth row of it.
 template <int NV, bool BF16>
-__global__ __launch_bounds__(kLanes) void residual_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks) {
+__global__ __launch_bounds__(kLanes) void residual_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks, int64_t chunk_rows, int lanes) {
   __shared__ __attribute__((aligned(16))) float reds[4][kLanes / 64];
-  const int tid = threadIdx.x;
-  const int64_t chunk = blockIdx.x, group = chunk / per_group;
-  const int64_t first = group * p.gate_rows + chunk % per_group * kGradRows;
-  const int64_t last = min(min(first + kGradRows, (group + 1) * p.gate_rows), p.rows);
+  __shared__ __attribute__((aligned(16))) f32x4 sum_slots[4 * NV * kLanes];
+  const int tid = threadIdx.x, waves = lanes >> 6, team = tid / lanes, teams = int(blockDim.x) / lanes;
+  const int64_t chunk = blockIdx.x, group = blockIdx.x / uint32_t(per_group);
+  const int64_t first = group * p.gate_rows + (chunk - group * per_group) * chunk_rows;
+  const int64_t last = min(min(first + chunk_rows, (group + 1) * p.gate_rows), p.rows);
   const float inv_cols = 1.0f / float(p.cols);
-  const MatrixRef gates{const_cast<void *>(p.gate), p.ld_gate, p.gate_bf16, 0};
-  __shared__ __attribute__((aligned(16))) f32x4 sum_slots[NV > 1 ? 4 * NV * kLanes : 1];
+  const Columns<NV> c(tid % lanes, lanes, p.cols);
   ColumnSums<NV> pre_sum, gate_sum;
   pre_sum.clear(sum_slots);
-  gate_sum.clear(sum_slots + (NV > 1 ? 2 * NV * kLanes : 0));
-  uint32_t col[NV];
-  int n[NV];
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    col[v] = (uint32_t(v) * blockDim.x + tid) * 8;
-    n[v] = max(0, min(8, int(p.cols) - int(col[v])));
+  gate_sum.clear(sum_slots + 2 * NV * kLanes);
+  // The columns' factors stay in registers, and rows are loaded ahead of their use, where they hold it.
+  constexpr bool KEEP = NV == 1;
+  constexpr int WHEN = NV > 1 ? kLate : (BF16 ? kAhead : kEarly);
+  Row<NV, BF16, WHEN> dh, r, dr, y;
+  const int64_t mine = min(first + team, last - 1);  // a team without a row: the last one again, not counted
+  auto fetch_all = [&](int64_t row) {
+    dh.fetch(p.dh, row, c);
+    r.fetch(p.r, row, c);
+    dr.fetch(p.dr, row, c);
+    y.fetch(p.y, row, c);
+  };
+  if (WHEN == kAhead && first < last) fetch_all(mine);
+  float pre_w[NV][8], branch[NV][8];
+  auto pre_weights = [&](int v) { weights8(p.pre_weight, p.weight_bf16 != 0, c.col[v], c.n[v], p.offset, pre_w[v]); };
+  if constexpr (KEEP) {
+    pre_weights(0);
+    branch_factors<NV>(p, group, c, 0, branch[0]);
   }
-  Row<NV, BF16> dh, r, dr, y;
-  if (first < last) {
-    dh.fetch(p.dh, first, col, n);
-    r.fetch(p.r, first, col, n);
-    dr.fetch(p.dr, first, col, n);
-    y.fetch(p.y, first, col, n);
-  }
+  int turn = 0;
 #pragma unroll 1
-  for (int64_t row = first; row < last; ++row) {
-    const int64_t next = min(row + 1, last - 1);  // past the last row: it again, not used
-    float(*red)[kLanes / 64] = reds + 2 * (row & 1);
+  for (int64_t row0 = first; row0 < last; row0 += teams, ++turn) {
+    const bool live = row0 + team < last;
+    const int64_t row = live ? row0 + team : last - 1, next = min(row + teams, last - 1);
+    float(*red)[kLanes / 64] = reds + 2 * (turn & 1);
     float t[NV][8];
+    if (WHEN == kEarly) fetch_all(row);
     if (p.dh.data != nullptr) {
       float m[NV][8], sum = 0.0f;
       const float f = p.pre_rstd[row];
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        float w[8];
-        weights8(p.pre_weight, p.weight_bf16 != 0, col[v], n[v], p.offset, w);
-        dh.get(p.dh, row, col[v], n[v], v, t[v]);
-        r.get(p.r, row, col[v], n[v], v, m[v]);
+        dh.get(p.dh, row, c, v, t[v]);
+        r.get(p.r, row, c, v, m[v]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) m[v][e] *= f;
-        pre_sum.add(v, t[v], m[v]);
+        if (live) pre_sum.add(v, t[v], m[v]);
+        if constexpr (!KEEP) pre_weights(v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          t[v][e] *= w[e];
+          t[v][e] *= pre_w[v][e];
           sum = __builtin_fmaf(t[v][e], m[v][e], sum);
         }
       }
-      dh.fetch(p.dh, next, col, n);
-      r.fetch(p.r, next, col, n);
-      sum = group_sum(sum, red[0]) * inv_cols;
+      if (WHEN == kAhead) {
+        dh.fetch(p.dh, next, c);
+        r.fetch(p.r, next, c);
+      }
+      sum = team_sum(sum, red[0], waves) * inv_cols;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         float d[8] = {};
-        if (p.dr.data != nullptr) dr.get(p.dr, row, col[v], n[v], v, d);
+        if (p.dr.data != nullptr) dr.get(p.dr, row, c, v, d);
 #pragma unroll
         for (int e = 0; e < 8; ++e) t[v][e] = __builtin_fmaf(f, t[v][e] - m[v][e] * sum, d[e]);
-        }
+      }
     } else {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) dr.get(p.dr, row, col[v], n[v], v, t[v]);
+      for (int v = 0; v < NV; ++v) dr.get(p.dr, row, c, v, t[v]);
     }
-    dr.fetch(p.dr, next, col, n);
-    if (p.dx.data != nullptr) {
+    if (WHEN == kAhead) dr.fetch(p.dr, next, c);
+    if (p.dx.data != nullptr && live) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         float dx[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) dx[e] = p.x_scale * t[v][e];
-        store8(row_of(p.dx, is_bf16<BF16>(p.dx), row), is_bf16<BF16>(p.dx), col[v], n[v], dx);
+        store8(row_of(p.dx, is_bf16<BF16>(p.dx), row), is_bf16<BF16>(p.dx), c.col[v], c.n[v], dx);
       }
     }
     if (p.y.data == nullptr) continue;
@@ -327,95 +408,105 @@ __global__ __launch_bounds__(kLanes) void residual_grad_kernel(ResidualGradParam
     float m[NV][8], sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      float w[8], g[8];
-      y.get(p.y, row, col[v], n[v], v, m[v]);
+      y.get(p.y, row, c, v, m[v]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] = w[e] = 1.0f;
-      if (p.post_norm) weights8(p.post_weight, p.weight_bf16 != 0, col[v], n[v], p.offset, w);
-      if (p.gate != nullptr) load8(row_of(gates, p.gate_bf16 != 0, group), p.gate_bf16 != 0, col[v], n[v], g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        m[v][e] *= f;
-        t[v][e] *= p.y_scale;
-      }
-      gate_sum.add(v, t[v], m[v]);
+      for (int e = 0; e < 8; ++e) m[v][e] *= f;
+      if (live) gate_sum.add(v, t[v], m[v]);
+      if constexpr (!KEEP) branch_factors<NV>(p, group, c, v, branch[v]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        t[v][e] *= g[e] * w[e];
+        t[v][e] *= branch[v][e];
         sum = __builtin_fmaf(t[v][e], m[v][e], sum);
       }
     }
-    y.fetch(p.y, next, col, n);
+    if (WHEN == kAhead) y.fetch(p.y, next, c);
     if (p.dy.data == nullptr) continue;
     if (p.post_norm) {
-      sum = group_sum(sum, red[1]) * inv_cols;
+      sum = team_sum(sum, red[1], waves) * inv_cols;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e) t[v][e] = f * (t[v][e] - m[v][e] * sum);
     }
+    if (live) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) store8(row_of(p.dy, is_bf16<BF16>(p.dy), row), is_bf16<BF16>(p.dy), col[v], n[v], t[v]);
+      for (int v = 0; v < NV; ++v) store8(row_of(p.dy, is_bf16<BF16>(p.dy), row), is_bf16<BF16>(p.dy), c.col[v], c.n[v], t[v]);
+    }
   }
   if (p.sums == nullptr) return;
+  if (teams > 1) {
+    pre_sum.join(lanes);
+    gate_sum.join(lanes);
+    if (team != 0) return;
+  }
   if (p.dpre != nullptr) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) pre_sum.store(p.sums + chunk * p.cols, v, col[v], n[v]);
+    for (int v = 0; v < NV; ++v) pre_sum.store(p.sums + chunk * p.cols, v, c.col[v], c.n[v], 1.0f);
   }
   if (p.dpost != nullptr || p.dgate != nullptr) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) gate_sum.store(p.sums + (chunks + chunk) * p.cols, v, col[v], n[v]);
+    for (int v = 0; v < NV; ++v) gate_sum.store(p.sums + (chunks + chunk) * p.cols, v, c.col[v], c.n[v], p.y_scale);
   }
 }
 
 // The sum over i < count of a[i stride] in the workgroup's first 64 lanes: 64 columns
-// a workgroup, four lanes a column, each every fourth row, then those four; always in
-// that order.
+// a workgroup, one wave every sixteenth row, then the waves; always in that order.
+constexpr int kSumWaves = 16;
 __device__ __forceinline__ float column_sum(const float *a, int64_t count, int64_t stride, bool live, float *part) {
   float s = 0.0f;
   if (live) {
-#pragma unroll 4
-    for (int64_t i = threadIdx.x >> 6; i < count; i += 4) s += a[i * stride];
+#pragma unroll 8
+    for (int64_t i = threadIdx.x >> 6; i < count; i += kSumWaves) s += a[i * stride];
   }
-  __syncthreads();
   part[threadIdx.x] = s;
   __syncthreads();
-  const int l = threadIdx.x & 63;
-  return (part[l] + part[64 + l]) + (part[128 + l] + part[192 + l]);
+  if (threadIdx.x < 64) {
+    s = part[threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < kSumWaves; ++w) s += part[64 * w + threadIdx.x];
+  }
+  return s;
 }
 
 __device__ __forceinline__ float value_at(const void *p, bool bf16, int64_t at) {
   return bf16 ? bf16_to_f32(static_cast<const uint16_t *>(p)[at]) : static_cast<const float *>(p)[at];
 }
 
-// One group of gates a workgroup (and 64 columns): dgate, and S gate in the place of the group's first chunk.
-__global__ __launch_bounds__(kThreads) void gate_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks, int64_t blocks_c) {
-  __shared__ float part[kThreads];
-  const int64_t group = int64_t(blockIdx.x) / blocks_c, c = int64_t(blockIdx.x) % blocks_c * 64 + (threadIdx.x & 63);
-  float *a = p.sums + (chunks + group * per_group) * p.cols + c;
-  const float s = column_sum(a, per_group, p.cols, c < p.cols, part);
+// Blocks of 64 columns: first those of dw_pre (pre_blocks of them, or none), then those
+// of each group's S: dgate, and S gate in the place of the group's first chunk, or
+// straight into dw_post where there is one group.
+__global__ __launch_bounds__(64 * kSumWaves) void column_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks,
+                                                                     int64_t blocks_c, int64_t pre_blocks) {
+  __shared__ float part[64 * kSumWaves];
+  const bool pre = int64_t(blockIdx.x) < pre_blocks;
+  const int64_t block = pre ? int64_t(blockIdx.x) : int64_t(blockIdx.x) - pre_blocks;
+  const int64_t group = block / blocks_c, c = block % blocks_c * 64 + (threadIdx.x & 63);
+  float *a = p.sums + (pre ? 0 : (chunks + group * per_group) * p.cols) + c;
+  const float s = column_sum(a, pre ? chunks : per_group, p.cols, c < p.cols, part);
   if (threadIdx.x >= 64 || c >= p.cols) return;
+  if (pre) {
+    p.dpre[c] = p.accumulate ? p.dpre[c] + s : s;
+    return;
+  }
   if (p.dgate != nullptr) {
     const float w = p.post_norm && p.post_weight != nullptr ? p.offset + value_at(p.post_weight, p.weight_bf16 != 0, c) : 1.0f;
     float *d = p.dgate + group * p.ld_dgate + c;
     *d = p.accumulate ? *d + s * w : s * w;
   }
-  *a = s * value_at(p.gate, p.gate_bf16 != 0, group * p.ld_gate + c);
+  if (p.dpost == nullptr) return;
+  const float v = p.gate != nullptr ? s * value_at(p.gate, p.gate_bf16 != 0, group * p.ld_gate + c) : s;
+  if (p.groups > 1)
+    *a = v;
+  else
+    p.dpost[c] = p.accumulate ? p.dpost[c] + v : v;
 }
 
-// dw_pre from all chunks; dw_post from `post_count` rows of sums `post_stride` apart.
-__global__ __launch_bounds__(kThreads) void weight_grad_kernel(ResidualGradParams p, int64_t chunks, int64_t post_count, int64_t post_stride) {
-  __shared__ float part[kThreads];
+// dw_post from the groups' rows.
+__global__ __launch_bounds__(64 * kSumWaves) void post_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks) {
+  __shared__ float part[64 * kSumWaves];
   const int64_t c = int64_t(blockIdx.x) * 64 + (threadIdx.x & 63);
-  const bool live = c < p.cols;
-  if (p.dpre != nullptr) {
-    const float s = column_sum(p.sums + c, chunks, p.cols, live, part);
-    if (threadIdx.x < 64 && live) p.dpre[c] = p.accumulate ? p.dpre[c] + s : s;
-  }
-  if (p.dpost != nullptr) {
-    const float s = column_sum(p.sums + chunks * p.cols + c, post_count, post_stride * p.cols, live, part);
-    if (threadIdx.x < 64 && live) p.dpost[c] = p.accumulate ? p.dpost[c] + s : s;
-  }
+  const float s = column_sum(p.sums + chunks * p.cols + c, p.groups, per_group * p.cols, c < p.cols, part);
+  if (threadIdx.x < 64 && c < p.cols) p.dpost[c] = p.accumulate ? p.dpost[c] + s : s;
 }
 
 // Lanes and vectors of eight values a lane for a row.
@@ -427,13 +518,6 @@ RowShape row_shape(int64_t cols) {
   while (int64_t(lanes) * 8 < cols && lanes < kLanes) lanes *= 2;
   while (int64_t(lanes) * 8 * vectors < cols) vectors *= 2;
   return {lanes, vectors};
-}
-
-template <int NV>
-hipError_t launch_grad_rows(const ResidualGradParams &p, bool bf16, int lanes, int64_t per_group, int64_t chunks, hipStream_t s) {
-  const dim3 grid{unsigned(chunks)}, block{unsigned(lanes)};
-  return bf16 ? klaunch(residual_grad_kernel<NV, true>, grid, block, 0, s, p, per_group, chunks)
-              : klaunch(residual_grad_kernel<NV, false>, grid, block, 0, s, p, per_group, chunks);
 }
 
 bool all_bf16(std::initializer_list<const MatrixRef *> ms) {
@@ -449,41 +533,47 @@ hipError_t launch_residual_norm(const ResidualParams &p, hipStream_t s) {
   const RowShape sh = row_shape(p.cols);
   if (sh.vectors > 2) return hipErrorInvalidValue;
   const bool bf16 = all_bf16({&p.x, &p.y, &p.r, &p.h});
-  const int64_t most = ((int64_t(1) << 32) - 1) / sh.lanes;  // a launch has less than 2^32 lanes
-  for (int64_t r0 = 0; r0 < p.rows; r0 += most) {
-    ResidualParams q = p;
-    q.row0 = r0;
-    const dim3 grid{unsigned(std::min(most, p.rows - r0))}, block{unsigned(sh.lanes)};
-    const hipError_t e = sh.vectors == 1 ? (bf16 ? klaunch(residual_norm_kernel<1, true>, grid, block, 0, s, q)
-                                                 : klaunch(residual_norm_kernel<1, false>, grid, block, 0, s, q))
-                                         : (bf16 ? klaunch(residual_norm_kernel<2, true>, grid, block, 0, s, q)
-                                                 : klaunch(residual_norm_kernel<2, false>, grid, block, 0, s, q));
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  // as many workgroups as the units hold at once (2048 lanes each), each with the rows it then has
+  const int64_t most = int64_t(compute_units()) * (2048 / sh.lanes);
+  const dim3 grid{unsigned(std::min(p.rows, most))}, block{unsigned(sh.lanes)};
+  if (sh.vectors == 1)
+    return bf16 ? klaunch(residual_norm_kernel<1, true>, grid, block, 0, s, p) : klaunch(residual_norm_kernel<1, false>, grid, block, 0, s, p);
+  return bf16 ? klaunch(residual_norm_kernel<2, true>, grid, block, 0, s, p) : klaunch(residual_norm_kernel<2, false>, grid, block, 0, s, p);
 }
 
 hipError_t launch_residual_grad(const ResidualGradParams &p, hipStream_t s) {
   if (p.cols <= 0) return hipSuccess;
-  const int64_t per_group = (p.gate_rows + kGradRows - 1) / kGradRows, chunks = p.groups * per_group;
+  // A unit holds one workgroup: as many chunks as units, of 16 rows at least, which the
+  // workspace's size allows for.
+  const int64_t smallest = (p.gate_rows + kGradRows - 1) / kGradRows;
+  int64_t per_group = std::min<int64_t>(smallest, p.groups > 0 ? (compute_units() + p.groups - 1) / p.groups : 1);
+  const int64_t chunk_rows = (p.gate_rows + per_group - 1) / per_group;
+  per_group = (p.gate_rows + chunk_rows - 1) / chunk_rows;
+  const int64_t chunks = p.groups * per_group;
   if (chunks > 0) {
     const RowShape sh = row_shape(p.cols);
+    if (sh.vectors > 2) return hipErrorInvalidValue;
     const bool bf16 = all_bf16({&p.dr, &p.dh, &p.r, &p.y, &p.dx, &p.dy});
-    const hipError_t e = sh.vectors == 1   ? launch_grad_rows<1>(p, bf16, sh.lanes, per_group, chunks, s)
-                         : sh.vectors == 2 ? launch_grad_rows<2>(p, bf16, sh.lanes, per_group, chunks, s)
-                                           : hipErrorInvalidValue;
+    const int teams = int(std::min<int64_t>(kLanes / sh.lanes, chunk_rows));
+    const dim3 grid{unsigned(chunks)}, block{unsigned(sh.lanes * teams)};
+    const hipError_t e = sh.vectors == 1 ? (bf16 ? klaunch(residual_grad_kernel<1, true>, grid, block, 0, s, p, per_group, chunks, chunk_rows, sh.lanes)
+                                                 : klaunch(residual_grad_kernel<1, false>, grid, block, 0, s, p, per_group, chunks, chunk_rows, sh.lanes))
+                                         : (bf16 ? klaunch(residual_grad_kernel<2, true>, grid, block, 0, s, p, per_group, chunks, chunk_rows, sh.lanes)
+                                                 : klaunch(residual_grad_kernel<2, false>, grid, block, 0, s, p, per_group, chunks, chunk_rows, sh.lanes));
     if (e != hipSuccess) return e;
   }
-  const int64_t blocks_c = (p.cols + 63) / 64;
-  int64_t post_count = chunks, post_stride = 1;
-  if (p.gate != nullptr && p.groups > 0 && (p.dgate != nullptr || p.dpost != nullptr)) {
-    const hipError_t e = klaunch(gate_grad_kernel, dim3(unsigned(p.groups * blocks_c)), dim3(kThreads), 0, s, p, per_group, chunks, blocks_c);
-    if (e != hipSuccess) return e;
-    post_count = p.groups;
-    post_stride = per_group;
-  }
-  if (p.dpre == nullptr && p.dpost == nullptr) return hipSuccess;
-  return klaunch(weight_grad_kernel, dim3(unsigned(blocks_c)), dim3(kThreads), 0, s, p, chunks, post_count, post_stride);
+  const int64_t blocks_c = (p.cols + 63) / 64, pre_blocks = p.dpre != nullptr ? blocks_c : 0;
+  // (without rows one group of no chunks, whose sums are zero)
+  const int64_t post_blocks = p.dpost != nullptr || (p.dgate != nullptr && p.groups > 0) ? std::max<int64_t>(p.groups, 1) * blocks_c : 0;
+  if (pre_blocks + post_blocks == 0) return hipSuccess;
+  ResidualGradParams q = p;
+  if (p.groups == 0) q.dgate = nullptr, q.gate = nullptr;
+  const dim3 block(64 * kSumWaves);
+  hipError_t e = klaunch(column_grad_kernel, dim3(unsigned(pre_blocks + post_blocks)), block, 0, s, q, chunks > 0 ? per_group : 0, chunks, blocks_c,
+                         pre_blocks);
+  if (e == hipSuccess && p.groups > 1 && p.dpost != nullptr)
+    e = klaunch(post_grad_kernel, dim3(unsigned(blocks_c)), block, 0, s, p, per_group, chunks);
+  return e;
 }
 
 }  // namespace qe

@@ -7,7 +7,7 @@
 // a = m 2^E and fmax = 1.75 * 2^Emax the byte is a's exponent field less Emax, one
 // more where m > 1.75: the carry of the addition below.  |x| 2^e <= fmax, so codes
 // need no clamp.  A block that holds an infinity or a NaN gets the byte 255 (which
-// the matrix instruction takes for NaN too) and the code 0x7f, a NaN, throughout.
+// the matrix instruction takes for NaN too) and NaN codes throughout.
 #pragma once
 
 #include "act.h"
@@ -23,29 +23,36 @@ __device__ __forceinline__ uint32_t block_byte(float amax) {
   const int b = int((a + 0x1fffffu) >> 23) - (FMT == 0 ? 8 : 15);
   return a >= 0x7f800000u ? 255u : uint32_t(b < 1 ? 1 : b);
 }
-// 2^e; for byte 255 a NaN, which makes every code a NaN (0x7f or 0xff, see block_codes).
-__device__ __forceinline__ float block_mult(uint32_t byte) {
-  return __uint_as_float(byte == 255u ? 0x7fc00000u : (254u - byte) << 23);
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+// A block's scale as the conversions take it, 2^(byte - 127) (infinity for 255: they then give NaN).
+__device__ __forceinline__ float block_step(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Two values at a block's scale -> two codes in the lower or upper half of `w`.  The
+// instructions divide by the scale and round to nearest even; over all BF16 values (and
+// FP32 ones with other low bits) and scales from 2^-126 to 2^126 their codes are those of
+// x 2^e converted without a scale, checked on MI355X.
+template <int FMT, bool HI>
+__device__ __forceinline__ uint32_t convert_bf16(uint32_t w, uint32_t pair, float step) {
+  const i16x2 old = __builtin_bit_cast(i16x2, w);
+  const bf16x2_t x = __builtin_bit_cast(bf16x2_t, pair);
+  return __builtin_bit_cast(uint32_t, FMT == 0 ? __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(old, x, step, HI)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(old, x, step, HI));
 }
-// Four values at their block's multiplier -> four codes.  The conversion turns a NaN into 0x7f.
+template <int FMT, bool HI>
+__device__ __forceinline__ uint32_t convert_f32(uint32_t w, float a, float b, float step) {
+  const i16x2 old = __builtin_bit_cast(i16x2, w);
+  return __builtin_bit_cast(uint32_t, FMT == 0 ? __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(old, a, b, step, HI)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(old, a, b, step, HI));
+}
+
+// Four values -> four codes.
 template <int FMT>
-__device__ __forceinline__ uint32_t block_codes(const float *x, float mult) {
-  return enc4_in_range<FMT>(x[0] * mult, x[1] * mult, x[2] * mult, x[3] * mult);
+__device__ __forceinline__ uint32_t block_codes(const float *x, float step) {
+  return convert_f32<FMT, true>(convert_f32<FMT, false>(0u, x[0], x[1], step), x[2], x[3], step);
 }
 
 // Maximum over the 16 lanes of an aligned group, in all of them.
 __device__ __forceinline__ float max_lanes16(float v) { return max_dpp<0x140>(max_lanes8(v)); }  // 15 - lane
-__device__ __forceinline__ float max_swap32(float v) {  // of lanes l and l ^ 32
-  const uint32_t b = __float_as_uint(v);
-  const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-  return nan_max(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float max_swap16(float v) {  // of lanes l and l ^ 16
-  const uint32_t b = __float_as_uint(v);
-  const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
-  return nan_max(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
 typedef float f32x4_in __attribute__((ext_vector_type(4), aligned(4)));
 
 // Row `row` of a matrix: uniform in a workgroup where `row` is, so that a lane's

@@ -259,11 +259,11 @@ __global__ __launch_bounds__(kLanes, NV == 1 ? 8 : 4) void residual_norm_kernel(
         const float a = max_lanes16(nan_max(amax4(f32x4{h[0], h[1], h[2], h[3]}), amax4(f32x4{h[4], h[5], h[6], h[7]})));
         uint8_t *dst = (p.row.data + row * p.row.ld) + c.col[v];
         const uint32_t byte = p.row.fmt == 0 ? block_byte<0>(a) : block_byte<1>(a);
-        const float mult = block_mult(byte);
+        const float step = block_step(byte);
         if (p.row.fmt == 0)
-          store_codes8(dst, c.n[v], block_codes<0>(h, mult), block_codes<0>(h + 4, mult));
+          store_codes8(dst, c.n[v], block_codes<0>(h, step), block_codes<0>(h + 4, step));
         else
-          store_codes8(dst, c.n[v], block_codes<1>(h, mult), block_codes<1>(h + 4, mult));
+          store_codes8(dst, c.n[v], block_codes<1>(h, step), block_codes<1>(h + 4, step));
         if ((tid & 15) == 0 && c.n[v] > 0) (p.row.exps + row * p.row.ld_exps)[c.col[v] / kBlock] = uint8_t(byte);
       }
     }

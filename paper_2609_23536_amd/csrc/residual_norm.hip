@@ -23,6 +23,7 @@
 
 #include <algorithm>
 #include <initializer_list>
+#include <utility>
 
 namespace qe {
 namespace {
@@ -319,10 +320,22 @@ struct ColumnSums {
   }
 };
 
+// Where the columns are summed by a kernel of their own (column_sums_kernel), the mean of
+// d n over row i of a chunk of kGradRows waits for it in the workspace, where the chunk's
+// sums of a block of columns will be, once for each block: the first eight rows' in the
+// block's sums of dh n, the others' in those of t m.
+constexpr int kSumCols = 512, kHalf = int(kGradRows) / 2;
+__device__ __forceinline__ float *waiting(const ResidualGradParams &p, int64_t chunks, int64_t chunk, int block, int i) {
+  return p.sums + ((i < kHalf ? 0 : chunks) + chunk) * p.cols + block * kSumCols + i % kHalf;
+}
+
 // Chunks of up to chunk_rows rows, `per_group` of them for each group of gate_rows rows;
 // a chunk is a workgroup, whose teams of `lanes` lanes take every so manyth row of it.
+// sum_chunks > 0: no column sums, but each row's mean left for column_sums_kernel, whose
+// chunks those are (sum_group of them in a group).
 template <int NV, bool BF16>
-__global__ __launch_bounds__(kLanes) void residual_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks, int64_t chunk_rows, int lanes) {
+__global__ __launch_bounds__(kLanes) void residual_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks, int64_t chunk_rows, int lanes,
+                                                               int64_t sum_chunks, int64_t sum_group) {
   __shared__ __attribute__((aligned(16))) float reds[4][kLanes / 64];
   __shared__ __attribute__((aligned(16))) f32x4 sum_slots[4 * NV * kLanes];
   const int tid = threadIdx.x, waves = lanes >> 6, team = tid / lanes, teams = int(blockDim.x) / lanes;
@@ -369,7 +382,7 @@ __global__ __launch_bounds__(kLanes) void residual_grad_kernel(ResidualGradParam
         r.get(p.r, row, c, v, m[v]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) m[v][e] *= f;
-        if (live) pre_sum.add(v, t[v], m[v]);
+        if (live && sum_chunks == 0) pre_sum.add(v, t[v], m[v]);
         if constexpr (!KEEP) pre_weights(v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -382,6 +395,12 @@ __global__ __launch_bounds__(kLanes) void residual_grad_kernel(ResidualGradParam
         r.fetch(p.r, next, c);
       }
       sum = team_sum(sum, red[0], waves) * inv_cols;
+      if (sum_chunks > 0 && live) {
+        const int64_t in_group = row - group * p.gate_rows;
+        const int block = tid - team * lanes;
+        if (int64_t(block) * kSumCols < p.cols)
+          *waiting(p, sum_chunks, group * sum_group + in_group / kGradRows, block, int(in_group % kGradRows)) = sum;
+      }
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         float d[8] = {};
@@ -411,7 +430,7 @@ __global__ __launch_bounds__(kLanes) void residual_grad_kernel(ResidualGradParam
       y.get(p.y, row, c, v, m[v]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) m[v][e] *= f;
-      if (live) gate_sum.add(v, t[v], m[v]);
+      if (live && sum_chunks == 0) gate_sum.add(v, t[v], m[v]);
       if constexpr (!KEEP) branch_factors<NV>(p, group, c, v, branch[v]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -433,7 +452,7 @@ __global__ __launch_bounds__(kLanes) void residual_grad_kernel(ResidualGradParam
       for (int v = 0; v < NV; ++v) store8(row_of(p.dy, is_bf16<BF16>(p.dy), row), is_bf16<BF16>(p.dy), c.col[v], c.n[v], t[v]);
     }
   }
-  if (p.sums == nullptr) return;
+  if (p.sums == nullptr || sum_chunks > 0) return;
   if (teams > 1) {
     pre_sum.join(lanes);
     gate_sum.join(lanes);
@@ -447,6 +466,71 @@ __global__ __launch_bounds__(kLanes) void residual_grad_kernel(ResidualGradParam
 #pragma unroll
     for (int v = 0; v < NV; ++v) gate_sum.store(p.sums + (chunks + chunk) * p.cols, v, c.col[v], c.n[v], p.y_scale);
   }
+}
+
+// The column sums of a chunk of kGradRows rows for a block of kSumCols columns: a wave
+// per row, which computes dh n and t m again from the inputs and the row's mean, then the
+// waves' in their order.
+template <bool BF16>
+__global__ __launch_bounds__(64 * kGradRows) void column_sums_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks, int blocks) {
+  __shared__ __attribute__((aligned(16))) f32x4 slots[kGradRows][4 * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int64_t chunk = blockIdx.x / unsigned(blocks), group = chunk / per_group;
+  const int block = int(blockIdx.x % unsigned(blocks));
+  const int64_t row = group * p.gate_rows + (chunk - group * per_group) * kGradRows + wave;
+  const bool live = row < min((group + 1) * p.gate_rows, p.rows);
+  Columns<1> c(lane, 64, p.cols - block * kSumCols);
+  c.col[0] += uint32_t(block) * kSumCols;
+  const bool gates = p.y.data != nullptr && (p.dpost != nullptr || p.dgate != nullptr);
+  float pre[8] = {}, gate[8] = {};
+  if (live) {
+    Row<1, BF16, BF16 ? kAhead : kEarly> dh, r, dr, y;
+    dh.fetch(p.dh, row, c);
+    r.fetch(p.r, row, c);
+    if (gates) {
+      dr.fetch(p.dr, row, c);
+      y.fetch(p.y, row, c);
+    }
+    float t[8] = {};
+    if (gates && p.dr.data != nullptr) dr.get(p.dr, row, c, 0, t);
+    if (p.dh.data != nullptr) {
+      float d[8], m[8], w[8];
+      const float f = p.pre_rstd[row], mean = *waiting(p, chunks, chunk, block, wave);
+      dh.get(p.dh, row, c, 0, d);
+      r.get(p.r, row, c, 0, m);
+      weights8(p.pre_weight, p.weight_bf16 != 0, c.col[0], c.n[0], p.offset, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        m[e] *= f;
+        pre[e] = d[e] * m[e];
+        t[e] = __builtin_fmaf(f, d[e] * w[e] - m[e] * mean, t[e]);
+      }
+    }
+    if (gates) {
+      float m[8];
+      const float f = p.post_norm ? p.post_rstd[row] : 1.0f;
+      y.get(p.y, row, c, 0, m);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) gate[e] = t[e] * (m[e] * f);
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    slots[wave][64 * h + lane] = f32x4{pre[4 * h], pre[4 * h + 1], pre[4 * h + 2], pre[4 * h + 3]};
+    slots[wave][64 * (2 + h) + lane] = f32x4{gate[4 * h], gate[4 * h + 1], gate[4 * h + 2], gate[4 * h + 3]};
+  }
+  __syncthreads();  // (every wave has read its row's mean by now)
+  if (threadIdx.x >= 256) return;
+  f32x4 s = slots[0][threadIdx.x];
+#pragma unroll
+  for (int w = 1; w < int(kGradRows); ++w) s += slots[w][threadIdx.x];
+  const bool of_gate = threadIdx.x >= 128;
+  const int at = 8 * lane + 4 * (wave & 1), n = int(min(int64_t(4), p.cols - block * kSumCols - at));
+  float *out = p.sums + ((of_gate ? chunks : 0) + chunk) * p.cols + block * kSumCols + at;
+  const float scale = of_gate ? p.y_scale : 1.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < n) out[e] = scale * s[e];
 }
 
 // The sum over i < count of a[i stride] in the workgroup's first 64 lanes: 64 columns
@@ -526,6 +610,21 @@ bool all_bf16(std::initializer_list<const MatrixRef *> ms) {
   return true;
 }
 
+// Few chunks of 16 rows leave most units idle, and rows of more than two thousand columns
+// then follow each other in teams of half a workgroup or more: the columns are summed by a
+// kernel of their own, which reads the inputs (in the caches by then) once more.  MI355X,
+// us, sums with the rows / apart: 64 x 8192 37.7 / 15.5, 512 x 8192 43 / 24, 1280 x 8192 (80
+// chunks) 62 / 52, 1000 x 2730 FP32 37.6 / 33.5, but 1280 x 4096 27.5 / 29.4, 2048 x 8192
+// (128) 68 / 77; 512 x 2048 16.4 / 15.9, 64 x 1024 12.6 / 14.3.  A block's sums have room
+// for the means of half a chunk's rows from eight columns on, and in place the inputs are
+// gone by then.
+bool sums_apart(const ResidualGradParams &p, int64_t chunks) {
+  for (const MatrixRef *out : {&p.dx, &p.dy})
+    for (const MatrixRef *in : {&p.dr, &p.dh, &p.r, &p.y})
+      if (out->data != nullptr && out->data == in->data) return false;
+  return chunks * 3 <= compute_units() && p.cols > 2048 && (p.cols % kSumCols == 0 || p.cols % kSumCols >= kHalf);
+}
+
 }  // namespace
 
 hipError_t launch_residual_norm(const ResidualParams &p, hipStream_t s) {
@@ -543,23 +642,36 @@ hipError_t launch_residual_norm(const ResidualParams &p, hipStream_t s) {
 
 hipError_t launch_residual_grad(const ResidualGradParams &p, hipStream_t s) {
   if (p.cols <= 0) return hipSuccess;
-  // A unit holds one workgroup: as many chunks as units, of 16 rows at least, which the
-  // workspace's size allows for.
-  const int64_t smallest = (p.gate_rows + kGradRows - 1) / kGradRows;
-  int64_t per_group = std::min<int64_t>(smallest, p.groups > 0 ? (compute_units() + p.groups - 1) / p.groups : 1);
-  const int64_t chunk_rows = (p.gate_rows + per_group - 1) / per_group;
-  per_group = (p.gate_rows + chunk_rows - 1) / chunk_rows;
-  const int64_t chunks = p.groups * per_group;
-  if (chunks > 0) {
+  int64_t per_group = 1, chunks = 0;
+  if (p.rows > 0) {
     const RowShape sh = row_shape(p.cols);
     if (sh.vectors > 2) return hipErrorInvalidValue;
     const bool bf16 = all_bf16({&p.dr, &p.dh, &p.r, &p.y, &p.dx, &p.dy});
+    // A unit holds one workgroup: as many chunks as units, of 16 rows at least where they
+    // leave sums, which the workspace's size allows for.
+    const int64_t units = compute_units(), smallest = (p.gate_rows + kGradRows - 1) / kGradRows;
+    const bool own_sums = p.sums != nullptr && sums_apart(p, smallest * p.groups);
+    auto chunks_of = [&](int64_t least) {  // rows a chunk, and chunks a group
+      const int64_t most = (p.gate_rows + least - 1) / least, n = std::min(most, (units + p.groups - 1) / p.groups);
+      const int64_t rows = (p.gate_rows + n - 1) / n;
+      return std::make_pair(rows, (p.gate_rows + rows - 1) / rows);
+    };
+    const auto [chunk_rows, in_group] = chunks_of(p.sums != nullptr && !own_sums ? kGradRows : 1);
     const int teams = int(std::min<int64_t>(kLanes / sh.lanes, chunk_rows));
-    const dim3 grid{unsigned(chunks)}, block{unsigned(sh.lanes * teams)};
-    const hipError_t e = sh.vectors == 1 ? (bf16 ? klaunch(residual_grad_kernel<1, true>, grid, block, 0, s, p, per_group, chunks, chunk_rows, sh.lanes)
-                                                 : klaunch(residual_grad_kernel<1, false>, grid, block, 0, s, p, per_group, chunks, chunk_rows, sh.lanes))
-                                         : (bf16 ? klaunch(residual_grad_kernel<2, true>, grid, block, 0, s, p, per_group, chunks, chunk_rows, sh.lanes)
-                                                 : klaunch(residual_grad_kernel<2, false>, grid, block, 0, s, p, per_group, chunks, chunk_rows, sh.lanes));
+    const dim3 grid{unsigned(p.groups * in_group)}, block{unsigned(sh.lanes * teams)};
+    per_group = own_sums ? smallest : in_group;
+    chunks = p.groups * per_group;
+    const int64_t apart = own_sums ? chunks : 0;
+    auto rows_kernel = [&](auto *kernel) {
+      return klaunch(kernel, grid, block, 0, s, p, in_group, p.groups * in_group, chunk_rows, sh.lanes, apart, smallest);
+    };
+    hipError_t e = sh.vectors == 1 ? rows_kernel(bf16 ? residual_grad_kernel<1, true> : residual_grad_kernel<1, false>)
+                                   : rows_kernel(bf16 ? residual_grad_kernel<2, true> : residual_grad_kernel<2, false>);
+    if (e == hipSuccess && own_sums) {
+      const int blocks = int((p.cols + kSumCols - 1) / kSumCols);
+      e = klaunch(bf16 ? column_sums_kernel<true> : column_sums_kernel<false>, dim3(unsigned(chunks * blocks)), dim3(64 * kGradRows), 0, s, p,
+                  per_group, chunks, blocks);
+    }
     if (e != hipSuccess) return e;
   }
   const int64_t blocks_c = (p.cols + 63) / 64, pre_blocks = p.dpre != nullptr ? blocks_c : 0;

@@ -132,7 +132,8 @@ def launches(qe, hip, cases):
         elif kind == "norm":
             st = qe.qe_residual_norm(m, m, rows, cols, d, m, None, b(cols), b(rows) if args.get("col") else None, ADDR, ADDR, stream=0)
         else:
-            st = qe.qe_residual_norm_grad(m, m, m, m, rows, cols, d, ADDR, ADDR, m, m, ADDR if args.get("sums") else None,
+            o = qe.make_matrix(2 * ADDR, max(cols, 1), qe.BF16)
+            st = qe.qe_residual_norm_grad(m, m, m, m, rows, cols, d, ADDR, ADDR, o, o, ADDR if args.get("sums") else None,
                                           ADDR if args.get("sums") else None, ADDR if args.get("gate") else None, qe.INIT, ADDR, stream=0)
         assert st == "OK", st
         got.append([w[2].split("kernel")[0].lstrip("_ZN2qe1GLOBAL").lstrip("_0123456789") for w in hip.log("launch")])
@@ -140,13 +141,16 @@ def launches(qe, hip, cases):
 
 
 def test_launches():
-    """A cast is one kernel, a norm one and one more for its transposed codes, a gradient one, one for the gates and one for the weights."""
+    """A cast is one kernel, a norm one and one more for its transposed codes; a gradient one, one more for the sums of columns, one
+    for the sums over the rows of gates, and one where few long rows leave the columns to it."""
     got = calls(launches, [["cast", 100, 300, {"col": 1}], ["cast", 100, 300, {"row": False}], ["norm", 100, 300, {}], ["norm", 100, 300, {"col": 1}],
                            ["grad", 100, 300, {}], ["grad", 100, 300, {"sums": 1}], ["grad", 100, 300, {"sums": 1, "gate": 30}],
-                           ["grad", 0, 300, {"sums": 1}], ["norm", 0, 300, {"col": 1}]])
+                           ["grad", 100, 300, {"sums": 1, "gate": 100}], ["grad", 100, 4096, {"sums": 1}], ["grad", 1360, 4096, {"sums": 1}],
+                           ["grad", 1361, 4096, {"sums": 1}], ["grad", 100, 4097, {"sums": 1}], ["grad", 0, 300, {"sums": 1}],
+                           ["norm", 0, 300, {"col": 1}]])
+    sums, apart = ["residual_grad", "column_grad"], ["residual_grad", "column_sums", "column_grad"]
     assert [[n.rstrip("_") for n in g] for g in got] == [["block_cast"], [], ["residual_norm"], ["residual_norm", "block_cast"], ["residual_grad"],
-                                                         ["residual_grad", "weight_grad"], ["residual_grad", "gate_grad", "weight_grad"],
-                                                         ["weight_grad"], []]
+                                                         sums, sums + ["post_grad"], sums, apart, apart, sums, sums, ["column_grad"], []]
 
 
 def test_struct_sizes():

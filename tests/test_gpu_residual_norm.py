@@ -245,7 +245,8 @@ def check_grad(c, use_dr=True, use_dh=True, dt="bf16", out="bf16", sums=True, mo
 
 GRAD_FORMS = [dict(), dict(r="f32", x="f32", y="f32", weights="f32", pad=1), dict(gate_rows=1 << 40, xs=0.875, ys=0.5), dict(gate_rows=3, offset=1.0, pad=3),
               dict(post=False, gate_rows=1, ys=0.22), dict(post=False), dict(weights=None, gate_rows=20), dict(y=None, r=None, pad=5), dict(r="f32", y="bf16")]
-GRAD_SHAPES = [(1, 1), (1, 7), (3, 128), (17, 512), (33, 513), (16, 1000), (100, 2730), (2, 8192), (35, 8193), (5, 16384), (300, 70)]
+GRAD_SHAPES = [(1, 1), (1, 7), (3, 128), (17, 512), (33, 513), (16, 1000), (100, 2730), (2, 8192), (35, 8193), (5, 16384), (300, 70),
+               (700, 4104), (40, 4103), (1400, 2600), (600, 1100)]  # columns summed with the rows, or by a kernel of their own
 
 
 @pytest.mark.parametrize("form", GRAD_FORMS, ids=lambda f: "-".join(f"{k}{v}" for k, v in f.items()) or "plain")

@@ -190,11 +190,15 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
   // `byte`: that of the tile, t % 4; the group's words come with its first tile.
   auto read_a = [&](auto byte, int buf, int i, v8i (&fa)[I]) {
     fa[i] = frag(smem + buf * STAGE + (wm * TM + i * 16) * BK);
-    if constexpr (SC::kOn && decltype(byte)::value == 0) sa[i] = SC::read(pa, i * 16);
+    if constexpr (SC::kOn) {
+      if constexpr (decltype(byte)::value == 0) sa[i] = SC::read(pa, i * 16);
+    }
   };
   auto read_b = [&](auto byte, int buf, int j, v8i (&fb)[J]) {
     fb[j] = frag(smem + buf * STAGE + (BM + wn * TN + j * 16) * BK);
-    if constexpr (SC::kOn && decltype(byte)::value == 0) sb[j] = SC::read(pb, j * 16);
+    if constexpr (SC::kOn) {
+      if constexpr (decltype(byte)::value == 0) sb[j] = SC::read(pb, j * 16);
+    }
   };
 
 #pragma unroll
@@ -330,8 +334,10 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
       // The next group's scales, into the buffer whose last reads were of tile t - 1.
       // They are older than the B part below, so the wait at this step's end covers
       // them: three steps before they are read.
-      if constexpr (SC::kOn && decltype(byte)::value == 0) sc.load(smem, wave, t / 4 + 1);
-      if constexpr (SC::kOn && decltype(next)::value == 0) scales_at(t / 4 + 1);
+      if constexpr (SC::kOn) {
+        if constexpr (decltype(byte)::value == 0) sc.load(smem, wave, t / 4 + 1);
+        if constexpr (decltype(next)::value == 0) scales_at(t / 4 + 1);
+      }
       // phase B of tile t, with tile t+2's A part; reads of tile t+1 (in the
       // last iteration they read a stale stage that is never used: always in
       // bounds, and branch-free here)

@@ -35,3 +35,19 @@ def test_workgroups_per_compute_unit(built, part, workgroups):
     vgprs = (got[0][".vgpr_count"] + 7) // 8 * 8  # AGPRs included
     assert 512 // vgprs >= workgroups
     assert got[0][".group_segment_fixed_size"] * workgroups <= 160 * 1024
+
+
+# kernels with more lanes a workgroup: name part, waves a workgroup, workgroups a compute unit (four SIMDs) is to hold
+WIDE = [("residual_norm_kernelILi1ELb1E", 16, 2), ("residual_norm_kernelILi1ELb0E", 16, 2), ("residual_norm_kernelILi2ELb1E", 16, 1),
+        ("residual_grad_kernelILi1ELb1E", 16, 1), ("residual_grad_kernelILi2ELb0E", 16, 1), ("column_sums_kernelILb1E", 16, 1),
+        ("block_cast_kernelILb1E", 4, 2), ("block_large_kernelILi0ELi0ELi256ELi256E", 4, 1), ("block_ring_kernelILi0ELi0ELi64ELi64ELi4E", 4, 2),
+        ("block_ring_kernelILi0ELi0ELi128ELi128ELi2E", 4, 2)]
+
+
+@pytest.mark.parametrize("part,waves,workgroups", WIDE, ids=lambda v: str(v))
+def test_wide_workgroups_per_compute_unit(built, part, waves, workgroups):
+    got = [k for n, k in built.items() if part in n]
+    assert got
+    for k in got:
+        assert 512 // ((k[".vgpr_count"] + 7) // 8 * 8) >= waves * workgroups // 4
+        assert k[".group_segment_fixed_size"] * workgroups <= 160 * 1024

@@ -358,7 +358,8 @@ qe_status qe_act_restore(const qe_saved *saved_host, int64_t rows, int64_t cols,
  * activations and gradients) or of 128 rows (block_rows 128: weights).  The code at
  * (r, c), data[r * ld + c], stands for
  *     code * 2^(exps[(r / block_rows) * ld_exps + c / 128] - 127);
- * a byte of 255 stands for NaN. */
+ * a byte of 255 stands for NaN.  (The largest code of values from 1.9375 * 2^127 on
+ * may stand for 2^128, which the products take for it and FP32 does not hold.) */
 typedef struct {
   uint8_t *data;
   int64_t ld; /* bytes */
@@ -432,8 +433,9 @@ typedef struct {
  * pre_rstd and r_host (without y and with x_scale 1 it reads x instead where r_host is
  * NULL).  post_rstd and pre_rstd (may be NULL) receive rows values 1 / sqrt(..), which
  * the gradient reads.  All arithmetic is FP32: a row whose squares overflow has an
- * infinite mean.  r or h may be x or y itself (same type and stride); outputs may not
- * overlap otherwise (with col_host h may not be x either where it is read again).
+ * infinite mean.  r or h may be x or y itself (refused if of another type or stride, or
+ * both in one place); outputs may not overlap otherwise (with col_host h may not be x
+ * either where it is read again).
  * cols <= 16384 (QE_ERR_INVALID_ARG beyond), rows below 2^31, with col_host 128 x 128
  * blocks below 2^24; rows or cols may be 0.  Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
 qe_status qe_residual_norm(const qe_matrix *x_host, const qe_matrix *y_host, int64_t rows, int64_t cols,
@@ -445,16 +447,16 @@ qe_status qe_residual_norm(const qe_matrix *x_host, const qe_matrix *y_host, int
  * (either may be NULL, not both); r_host, y_host: as the forward stored and read them (r
  * is read with dh only, y_host NULL: there was none); post_rstd, pre_rstd: from the
  * forward, read where their norm was taken.  dx_host receives x's gradient, dy_host y's
- * (either may be NULL; each may be dr or dh itself, of the same type and stride, and not
- * both the same).  dpost_weight, dpre_weight (cols floats) and dgate
+ * (either may be NULL; each may be dr or dh itself, refused if of another type or stride,
+ * and neither may be r, y or the other).  dpost_weight, dpre_weight (cols floats) and dgate
  * ([ceil(rows / gate_rows), cols], row stride ld_dgate), each of which may be NULL,
  * receive those gradients (QE_PLACE_INIT) or are increased by them (QE_PLACE_ACCUM), in
  * FP32 and in an order that does not change from call to call; workspace then holds
  * 2 * cols * G * ceil(min(gate_rows, rows) / 16) floats, G the rows of gates (without
  * gates 2 * cols * ceil(rows / 16)), whose contents do not matter before or after.
  * dpre_weight without dh, dpost_weight without y or its norm, and dgate without y or a
- * gate are refused.  Sizes as above, the workspace below 2^23 rows of cols floats (rows
- * 0: INIT clears the weights' gradients).
+ * gate are refused.  Sizes as above, and with or without a workspace what it holds below
+ * 2^23 rows of cols floats (rows 0: INIT clears the weights' gradients).
  * Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
 qe_status qe_residual_norm_grad(const qe_matrix *dr_host, const qe_matrix *dh_host, const qe_matrix *r_host,
                                 const qe_matrix *y_host, int64_t rows, int64_t cols, const qe_residual *desc_host,

@@ -889,6 +889,13 @@ qe::MatrixRef matrix_ref(const qe_matrix *m) {
   return r;
 }
 
+// An output in the place of an input lies as that does.
+bool in_place_ok(const qe_matrix *out, const qe_matrix *in) {
+  return out == nullptr || in == nullptr || out->data != in->data || (out->ld == in->ld && out->dtype == in->dtype);
+}
+
+bool apart(const qe_matrix *a, const qe_matrix *b) { return a == nullptr || b == nullptr || a->data != b->data; }
+
 constexpr int64_t kMaxNormCols = 16384;  // a row stays in one workgroup's registers
 
 bool residual_ok(const qe_residual *d, int64_t rows, int64_t cols) {
@@ -1281,6 +1288,9 @@ qe_status qe_residual_norm(const qe_matrix *x_host, const qe_matrix *y_host, int
     return QE_ERR_INVALID_ARG;
   if ((row_host != nullptr && !blocked_out_ok(*row_host, cols)) || (col_host != nullptr && !blocked_out_ok(*col_host, rows)))
     return QE_ERR_INVALID_ARG;
+  if (!apart(r_host, h_host)) return QE_ERR_INVALID_ARG;
+  for (const qe_matrix *out : {r_host, h_host})
+    if (!in_place_ok(out, x_host) || !in_place_ok(out, y_host)) return QE_ERR_INVALID_ARG;
   qe::ResidualParams p;
   memset(&p, 0, sizeof(p));
   p.x = matrix_ref(x_host);
@@ -1352,9 +1362,12 @@ qe_status qe_residual_norm_grad(const qe_matrix *dr_host, const qe_matrix *dh_ho
     if (!matrix_ok(dr_host, cols) || !matrix_ok(dh_host, cols) || !matrix_ok(y_host, cols) || !matrix_ok(dx_host, cols) ||
         !matrix_ok(dy_host, cols) || (dh_host != nullptr && !matrix_ok(r_host, cols)))
       return QE_ERR_INVALID_ARG;
-    // workgroups of up to 1024 lanes for 16 rows, and of 256 for 64 columns of a group's sums
-    if (p.groups * ((p.gate_rows + 15) / 16) >= kMaxGroups / 4 || p.groups * ((cols + 63) / 64) >= kMaxGroups)
-      return QE_ERR_INVALID_ARG;
+    if (!apart(dx_host, dy_host)) return QE_ERR_INVALID_ARG;
+    for (const qe_matrix *out : {dx_host, dy_host})  // (y may be read after dx is stored, dr and dh not)
+      if (!in_place_ok(out, dr_host) || !in_place_ok(out, dh_host) || (dh_host != nullptr && !apart(out, r_host)) || !apart(out, y_host))
+        return QE_ERR_INVALID_ARG;
+    // workgroups of up to 1024 lanes for 16 rows
+    if (p.groups * ((p.gate_rows + 15) / 16) >= kMaxGroups / 4) return QE_ERR_INVALID_ARG;
   }
   p.dr = matrix_ref(dr_host);
   p.dh = matrix_ref(dh_host);

@@ -28,11 +28,12 @@ __global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void block
 constexpr int64_t kFewRows = 16;
 constexpr int kFewRowsTile = 0;  // in place of a GemmTile
 
-// As for one scale per operand (few_blocks in act_gemm.hip).
+// As for one scale per operand (few_blocks in act_gemm.hip); a launch holds less than
+// 2^32 lanes, 512 of them a block.
 bool few_blocks(const BlockGemmParams &p) {
-  if (p.m <= kFewRows) return true;
   const bool wide = p.z.kind == kSavedI8;
   const int64_t blocks = (p.m + 15) / 16 * ((p.n + (wide ? 31 : 15)) / (wide ? 32 : 16)), cus = compute_units();
+  if (p.m <= kFewRows) return blocks < int64_t(1) << 23;
   if (p.k <= 1024) return false;
   return blocks <= cus || (blocks <= 2 * cus && p.k > 12288 && !wide);
 }

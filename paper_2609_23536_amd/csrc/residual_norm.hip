@@ -533,15 +533,18 @@ __global__ __launch_bounds__(64 * kGradRows) void column_sums_kernel(ResidualGra
     if (e < n) out[e] = scale * s[e];
 }
 
-// The sum over i < count of a[i stride] in the workgroup's first 64 lanes: 64 columns
-// a workgroup, one wave every sixteenth row, then the waves; always in that order.
+// The sum over i < count of a[i stride], a column a lane: the waves take every `waves`th i
+// each, and the first adds theirs up; always in that order.
 constexpr int kSumWaves = 16;
-__device__ __forceinline__ float column_sum(const float *a, int64_t count, int64_t stride, bool live, float *part) {
+__device__ __forceinline__ float column_sum(const float *a, int64_t count, int64_t stride, bool live, int waves, float *part) {
   float s = 0.0f;
+  const int wave = waves > 1 ? int(threadIdx.x >> 6) : 0;
   if (live) {
 #pragma unroll 8
-    for (int64_t i = threadIdx.x >> 6; i < count; i += kSumWaves) s += a[i * stride];
+    for (int64_t i = wave; i < count; i += waves) s += a[i * stride];
   }
+  if (waves == 1) return s;
+  __syncthreads();  // the last sum's parts have been read
   part[threadIdx.x] = s;
   __syncthreads();
   if (threadIdx.x < 64) {
@@ -558,40 +561,54 @@ __device__ __forceinline__ float value_at(const void *p, bool bf16, int64_t at) 
 
 // Blocks of 64 columns: first those of dw_pre (pre_blocks of them, or none), then those
 // of each group's S: dgate, and S gate in the place of the group's first chunk, or
-// straight into dw_post where there is one group.
-__global__ __launch_bounds__(64 * kSumWaves) void column_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks,
-                                                                     int64_t blocks_c, int64_t pre_blocks) {
+// straight into dw_post where there is one group.  A group of few chunks is a wave's, and
+// sixteen of its kind a workgroup's.  A launch holds less than 2^32 lanes: a workgroup may
+// have to take more than one block.
+__global__ __launch_bounds__(64 * kSumWaves) void column_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks, int64_t blocks_c,
+                                                                     int64_t pre_blocks, int64_t post_blocks, int waves) {
   __shared__ float part[64 * kSumWaves];
-  const bool pre = int64_t(blockIdx.x) < pre_blocks;
-  const int64_t block = pre ? int64_t(blockIdx.x) : int64_t(blockIdx.x) - pre_blocks;
-  const int64_t group = block / blocks_c, c = block % blocks_c * 64 + (threadIdx.x & 63);
-  float *a = p.sums + (pre ? 0 : (chunks + group * per_group) * p.cols) + c;
-  const float s = column_sum(a, pre ? chunks : per_group, p.cols, c < p.cols, part);
-  if (threadIdx.x >= 64 || c >= p.cols) return;
-  if (pre) {
-    p.dpre[c] = p.accumulate ? p.dpre[c] + s : s;
-    return;
+  const int64_t per_workgroup = kSumWaves / waves, total = pre_blocks + (post_blocks + per_workgroup - 1) / per_workgroup;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll 1
+  for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
+    const bool pre = at < pre_blocks;
+    const int of = pre ? kSumWaves : waves;
+    const int64_t block = pre ? at : (at - pre_blocks) * per_workgroup + (waves > 1 ? 0 : wave);
+    const int64_t group = pre ? 0 : block / blocks_c, c = block % blocks_c * 64 + lane;
+    const bool live = c < p.cols && (pre || block < post_blocks);
+    float *a = p.sums + (pre ? 0 : (chunks + group * per_group) * p.cols) + c;
+    const float s = column_sum(a, pre ? chunks : per_group, p.cols, live, of, part);
+    if (!live || (of > 1 && wave != 0)) continue;
+    if (pre) {
+      p.dpre[c] = p.accumulate ? p.dpre[c] + s : s;
+      continue;
+    }
+    if (p.dgate != nullptr) {
+      const float w = p.post_norm && p.post_weight != nullptr ? p.offset + value_at(p.post_weight, p.weight_bf16 != 0, c) : 1.0f;
+      float *d = p.dgate + group * p.ld_dgate + c;
+      *d = p.accumulate ? *d + s * w : s * w;
+    }
+    if (p.dpost == nullptr) continue;
+    const float v = p.gate != nullptr ? s * value_at(p.gate, p.gate_bf16 != 0, group * p.ld_gate + c) : s;
+    if (p.groups > 1)
+      *a = v;
+    else
+      p.dpost[c] = p.accumulate ? p.dpost[c] + v : v;
   }
-  if (p.dgate != nullptr) {
-    const float w = p.post_norm && p.post_weight != nullptr ? p.offset + value_at(p.post_weight, p.weight_bf16 != 0, c) : 1.0f;
-    float *d = p.dgate + group * p.ld_dgate + c;
-    *d = p.accumulate ? *d + s * w : s * w;
-  }
-  if (p.dpost == nullptr) return;
-  const float v = p.gate != nullptr ? s * value_at(p.gate, p.gate_bf16 != 0, group * p.ld_gate + c) : s;
-  if (p.groups > 1)
-    *a = v;
-  else
-    p.dpost[c] = p.accumulate ? p.dpost[c] + v : v;
 }
 
 // dw_post from the groups' rows.
 __global__ __launch_bounds__(64 * kSumWaves) void post_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks) {
   __shared__ float part[64 * kSumWaves];
   const int64_t c = int64_t(blockIdx.x) * 64 + (threadIdx.x & 63);
-  const float s = column_sum(p.sums + chunks * p.cols + c, p.groups, per_group * p.cols, c < p.cols, part);
+  const float s = column_sum(p.sums + chunks * p.cols + c, p.groups, per_group * p.cols, c < p.cols, kSumWaves, part);
   if (threadIdx.x < 64 && c < p.cols) p.dpost[c] = p.accumulate ? p.dpost[c] + s : s;
 }
+
+// Chunks of a group that one wave adds up.  MI355X, us for the whole gradient, sixteen
+// waves a group / one: 8192 x 8192 with a row of gates for 256 rows (16 chunks) 191 / 173,
+// 64 rows (4) 261 / 182, 16 rows (1) 545 / 224; 2048 x 2048, 128 rows (8) 24.4 / 23.0.
+constexpr int64_t kFewChunks = 16;
 
 // Lanes and vectors of eight values a lane for a row.
 struct RowShape {
@@ -681,8 +698,10 @@ hipError_t launch_residual_grad(const ResidualGradParams &p, hipStream_t s) {
   ResidualGradParams q = p;
   if (p.groups == 0) q.dgate = nullptr, q.gate = nullptr;
   const dim3 block(64 * kSumWaves);
-  hipError_t e = klaunch(column_grad_kernel, dim3(unsigned(pre_blocks + post_blocks)), block, 0, s, q, chunks > 0 ? per_group : 0, chunks, blocks_c,
-                         pre_blocks);
+  const int waves = per_group > kFewChunks ? kSumWaves : 1;
+  const int64_t blocks = pre_blocks + (post_blocks * waves + kSumWaves - 1) / kSumWaves, most = (int64_t(1) << 22) - 1;
+  hipError_t e = klaunch(column_grad_kernel, dim3(unsigned(std::min(blocks, most))), block, 0, s, q, chunks > 0 ? per_group : 0, chunks, blocks_c,
+                         pre_blocks, post_blocks, waves);
   if (e == hipSuccess && p.groups > 1 && p.dpost != nullptr)
     e = klaunch(post_grad_kernel, dim3(unsigned(blocks_c)), block, 0, s, p, per_group, chunks);
   return e;

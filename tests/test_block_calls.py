@@ -94,7 +94,9 @@ def test_norm_refuses():
     for bad in (dict(d=None), dict(x=None, y=None), dict(rows=-1), dict(cols=16385, x=matrix(qe, 16385)), dict(rows=1 << 31),
                 dict(d=plain), dict(d=plain, h=None, row=None, col=None, post=None), dict(y=None, post=16), dict(d=desc(qe, post_norm=False)),
                 dict(post=18), dict(pre=18), dict(pre=None), dict(r=None), dict(y=None, post=None, r=None, d=desc(qe, x_scale=0.5)),
-                dict(y=None, post=None, r=None, h=matrix(qe)), dict(h=matrix(qe)), dict(col=blocked(qe, 4, fmt=1)), dict(col=blocked(qe, 4, block_rows=128)),
+                dict(y=None, post=None, r=None, h=matrix(qe)), dict(h=matrix(qe)), dict(h=matrix(qe), col=None, row=None),
+                dict(r=matrix(qe, data=48, ld=41), y=matrix(qe, data=48)), dict(r=matrix(qe, dtype=1)), dict(h=matrix(qe, data=48, dtype=1), y=matrix(qe, data=48)),
+                dict(col=blocked(qe, 4, fmt=1)), dict(col=blocked(qe, 4, block_rows=128)),
                 dict(col=blocked(qe, 4, ld=3))):
         assert norm(**bad) == "INVALID_ARG", bad  # (h over x or r, which the transposed codes are made from)
     assert norm(rows=0) == "OK" and norm(cols=0) == "OK"
@@ -104,9 +106,9 @@ def test_norm_grad_refuses():
     qe = need_lib()
 
     def grad(rows=4, cols=40, dr="", dh="", r="", y="", d="", post=16, pre=16, dx="", dy="", dpost=16, dpre=16, dgate=16, ld=40, mode=0, ws=16):
-        m = lambda v: matrix(qe) if v == "" else v  # noqa: E731
-        return qe.qe_residual_norm_grad(m(dr), m(dh), m(r), m(y), rows, cols, desc(qe) if d == "" else d, post, pre, m(dx), m(dy), dpost, dpre,
-                                        dgate, mode, ws, ld, stream=0)
+        m = lambda v, at: matrix(qe, data=at) if v == "" else v  # noqa: E731
+        return qe.qe_residual_norm_grad(m(dr, 16), m(dh, 32), m(r, 48), m(y, 64), rows, cols, desc(qe) if d == "" else d, post, pre, m(dx, 80), m(dy, 96),
+                                        dpost, dpre, dgate, mode, ws, ld, stream=0)
     for bad in BAD_DESC:
         assert grad(d=desc(qe, **bad)) == "INVALID_ARG", bad
     for bad in BAD_MATRIX:
@@ -115,7 +117,10 @@ def test_norm_grad_refuses():
     for bad in (dict(d=None), dict(dr=None, dh=None), dict(rows=-1), dict(cols=16385), dict(d=desc(qe, pre_norm=False)), dict(r=None), dict(pre=None),
                 dict(post=None), dict(y=None), dict(y=None, dy=None), dict(mode=2), dict(dh=None), dict(d=desc(qe, pre_weight=None)),
                 dict(d=desc(qe, post_weight=None)), dict(d=desc(qe, post_norm=False)), dict(d=desc(qe, gate=None)), dict(ld=39), dict(ws=None),
-                dict(ws=18), dict(dpost=18), dict(dpre=18), dict(dgate=18), dict(post=18), dict(pre=18), dict(rows=1 << 27)):
+                dict(ws=18), dict(dpost=18), dict(dpre=18), dict(dgate=18), dict(post=18), dict(pre=18), dict(rows=1 << 27),
+                dict(dx=matrix(qe, data=16, dtype=1)), dict(dx=matrix(qe, data=32, ld=41)), dict(dy=matrix(qe, data=16, ld=48)),
+                dict(dx=matrix(qe, data=48)), dict(dx=matrix(qe, data=64)), dict(dy=matrix(qe, data=48)), dict(dy=matrix(qe, data=64)),
+                dict(dx=matrix(qe, data=96))):
         assert grad(**bad) == "INVALID_ARG", bad
 
 
@@ -132,8 +137,8 @@ def launches(qe, hip, cases):
         elif kind == "norm":
             st = qe.qe_residual_norm(m, m, rows, cols, d, m, None, b(cols), b(rows) if args.get("col") else None, ADDR, ADDR, stream=0)
         else:
-            o = qe.make_matrix(2 * ADDR, max(cols, 1), qe.BF16)
-            st = qe.qe_residual_norm_grad(m, m, m, m, rows, cols, d, ADDR, ADDR, o, o, ADDR if args.get("sums") else None,
+            o, o2 = (qe.make_matrix(i * ADDR, max(cols, 1), qe.BF16) for i in (2, 3))
+            st = qe.qe_residual_norm_grad(m, m, m, m, rows, cols, d, ADDR, ADDR, o, o2, ADDR if args.get("sums") else None,
                                           ADDR if args.get("sums") else None, ADDR if args.get("gate") else None, qe.INIT, ADDR, stream=0)
         assert st == "OK", st
         got.append([w[2].split("kernel")[0].lstrip("_ZN2qe1GLOBAL").lstrip("_0123456789") for w in hip.log("launch")])
@@ -151,6 +156,46 @@ def test_launches():
     sums, apart = ["residual_grad", "column_grad"], ["residual_grad", "column_sums", "column_grad"]
     assert [[n.rstrip("_") for n in g] for g in got] == [["block_cast"], [], ["residual_norm"], ["residual_norm", "block_cast"], ["residual_grad"],
                                                          sums, sums + ["post_grad"], sums, apart, apart, sums, sums, ["column_grad"], []]
+
+
+def grids(qe, hip, cases):
+    got = []
+    for kind, *args in cases:
+        hip.clear()
+        if kind == "product":
+            m, n, k = args
+            a, b = (qe.make_blocked(ADDR, (k + 15) // 16 * 16, ADDR, (k + 511) // 512 * 4, 0, rows) for rows in (1, 128))
+            st = qe.qe_fp8_gemm_block(a, b, m, n, k, None, ADDR, qe.BF16, n, stream=0)
+        else:
+            rows, cols, gate_rows = args
+            ms = [qe.make_matrix(i * ADDR, cols, qe.BF16) for i in range(1, 7)]
+            d = qe.make_residual(post_norm=True, post_weight=ADDR, pre_norm=True, pre_weight=ADDR, gate=ADDR, ld_gate=cols, gate_rows=gate_rows)
+            st = qe.qe_residual_norm_grad(*ms[:4], rows, cols, d, ADDR, ADDR, *ms[4:], ADDR, ADDR, ADDR, qe.INIT, ADDR, stream=0)
+        assert st == "OK", st
+        got.append([[w[2], int(w[3].split("=")[1])] for w in hip.log("launch")])
+    return got
+
+
+@pytest.mark.parametrize("units", [64, 256])
+def test_products_get_their_kernels(units, monkeypatch):
+    """Blocks of 16 x 16 up to 16 rows, or where they fill the units once after 1025 (twice after 12289) columns; else tiles."""
+    monkeypatch.setenv("FAKE_HIP_UNITS", str(units))
+    n = units
+    got = calls(grids, [["product", m, nn, k] for m, nn, k in ((16, 64 * n, 128), (256, n, 1025), (257, n, 1025), (256, n, 1024), (512, n, 12289),
+                                                               (513, n, 12289), (8192, 8192, 8192))])
+    assert ["block_rows_kernel" in g[0][0] for g in got] == [True, True, False, False, True, False, False]
+    assert "block_large_kernel" in got[-1][0][0] and "block_ring_kernel" in got[2][0][0]
+
+
+def test_launches_hold_less_than_2_to_32_lanes():
+    """Kernels with 512 lanes a workgroup (rows of products) and 1024 (sums of columns) at the largest sizes that are accepted."""
+    got = calls(grids, [["product", 16, (1 << 27) - 16, 2048], ["product", 16, 1 << 27, 2048], ["product", 1, (1 << 29) - 32, 128],
+                        ["grad", (1 << 22) - 1, 8192, 1], ["grad", (1 << 22) - 1, 16384, 1], ["grad", 8 * 272, 256, 272], ["grad", 8 * 256, 256, 256]])
+    assert "block_rows_kernel" in got[0][0][0] and got[0][0][1] == (1 << 23) - 1
+    assert "block_rows_kernel" not in got[1][0][0] and got[2][0][1] * 256 < 1 << 32
+    for g in got[3:5]:
+        assert [n for n, _ in g if "column_grad" in n] and all(w * 1024 < 1 << 32 for _, w in g)
+    assert [[w for n, w in g if "column_grad" in n] for g in got[5:]] == [[4 + 8 * 4], [4 + 2]]  # 17 chunks a group, and 16: a wave each
 
 
 def test_struct_sizes():

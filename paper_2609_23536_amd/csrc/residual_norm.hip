@@ -533,22 +533,21 @@ __global__ __launch_bounds__(64 * kGradRows) void column_sums_kernel(ResidualGra
     if (e < n) out[e] = scale * s[e];
 }
 
-// The sum over i < count of a[i stride], a column a lane: the waves take every `waves`th i
-// each, and the first adds theirs up; always in that order.
+// The sum over i < count of a[i stride], a column a lane, in their order.
 constexpr int kSumWaves = 16;
-__device__ __forceinline__ float column_sum(const float *a, int64_t count, int64_t stride, bool live, int waves, float *part) {
+__device__ __forceinline__ float column_sum(const float *a, int64_t count, int64_t stride, int64_t first = 0, int step = 1) {
   float s = 0.0f;
-  const int wave = waves > 1 ? int(threadIdx.x >> 6) : 0;
-  if (live) {
 #pragma unroll 8
-    for (int64_t i = wave; i < count; i += waves) s += a[i * stride];
-  }
-  if (waves == 1) return s;
+  for (int64_t i = first; i < count; i += step) s += a[i * stride];
+  return s;
+}
+
+// The waves' sums, in their order, in the first one.
+__device__ __forceinline__ float join_waves(float s, float *part) {
   __syncthreads();  // the last sum's parts have been read
   part[threadIdx.x] = s;
   __syncthreads();
   if (threadIdx.x < 64) {
-    s = part[threadIdx.x];
 #pragma unroll
     for (int w = 1; w < kSumWaves; ++w) s += part[64 * w + threadIdx.x];
   }
@@ -559,41 +558,58 @@ __device__ __forceinline__ float value_at(const void *p, bool bf16, int64_t at) 
   return bf16 ? bf16_to_f32(static_cast<const uint16_t *>(p)[at]) : static_cast<const float *>(p)[at];
 }
 
-// Blocks of 64 columns: first those of dw_pre (pre_blocks of them, or none), then those
-// of each group's S: dgate, and S gate in the place of the group's first chunk, or
-// straight into dw_post where there is one group.  A group of few chunks is a wave's, and
-// sixteen of its kind a workgroup's.  A launch holds less than 2^32 lanes: a workgroup may
-// have to take more than one block.
+// How the chunks of groups are added up.
+enum GroupSums {
+  kByWorkgroup,  // a group, for 64 columns, is a workgroup's
+  kByWave,       // .. a wave's
+  kTogether,     // .. a wave's, and all groups a workgroup's, which adds up dw_post
+};
+
+// Blocks of 64 columns: first those of dw_pre (pre_blocks of them, or none), then those of
+// S (post_blocks: of each group, or kTogether of all): dgate, and dw_post where one
+// workgroup has all of it, else S gate in the place of the group's first chunk.  A launch
+// holds less than 2^32 lanes: a workgroup may have to take more than one block.
 __global__ __launch_bounds__(64 * kSumWaves) void column_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks, int64_t blocks_c,
-                                                                     int64_t pre_blocks, int64_t post_blocks, int waves) {
+                                                                     int64_t pre_blocks, int64_t post_blocks, int how) {
   __shared__ float part[64 * kSumWaves];
-  const int64_t per_workgroup = kSumWaves / waves, total = pre_blocks + (post_blocks + per_workgroup - 1) / per_workgroup;
+  const int64_t per_workgroup = how == kByWave ? kSumWaves : 1, total = pre_blocks + (post_blocks + per_workgroup - 1) / per_workgroup;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll 1
-  for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
-    const bool pre = at < pre_blocks;
-    const int of = pre ? kSumWaves : waves;
-    const int64_t block = pre ? at : (at - pre_blocks) * per_workgroup + (waves > 1 ? 0 : wave);
-    const int64_t group = pre ? 0 : block / blocks_c, c = block % blocks_c * 64 + lane;
-    const bool live = c < p.cols && (pre || block < post_blocks);
-    float *a = p.sums + (pre ? 0 : (chunks + group * per_group) * p.cols) + c;
-    const float s = column_sum(a, pre ? chunks : per_group, p.cols, live, of, part);
-    if (!live || (of > 1 && wave != 0)) continue;
-    if (pre) {
-      p.dpre[c] = p.accumulate ? p.dpre[c] + s : s;
-      continue;
-    }
+  auto of_group = [&](int64_t group, int64_t c, float s) {  // S -> S gate, and dgate
     if (p.dgate != nullptr) {
       const float w = p.post_norm && p.post_weight != nullptr ? p.offset + value_at(p.post_weight, p.weight_bf16 != 0, c) : 1.0f;
       float *d = p.dgate + group * p.ld_dgate + c;
       *d = p.accumulate ? *d + s * w : s * w;
     }
-    if (p.dpost == nullptr) continue;
-    const float v = p.gate != nullptr ? s * value_at(p.gate, p.gate_bf16 != 0, group * p.ld_gate + c) : s;
-    if (p.groups > 1)
-      *a = v;
+    return p.gate != nullptr ? s * value_at(p.gate, p.gate_bf16 != 0, group * p.ld_gate + c) : s;
+  };
+#pragma unroll 1
+  for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
+    const bool pre = at < pre_blocks;
+    const int64_t block = pre ? at : (at - pre_blocks) * per_workgroup + (how == kByWave ? wave : 0);
+    const int64_t group = block / blocks_c, c = block % blocks_c * 64 + lane;
+    const bool live = c < p.cols && (pre || block < post_blocks);
+    float *a = p.sums + (pre ? 0 : chunks * p.cols) + c, s = 0.0f;
+    if (pre) {
+      s = join_waves(live ? column_sum(a, chunks, p.cols, wave, kSumWaves) : 0.0f, part);
+    } else if (how == kTogether) {
+      if (live)
+        for (int64_t g = wave; g < p.groups; g += kSumWaves) s += of_group(g, c, column_sum(a + g * per_group * p.cols, per_group, p.cols));
+      s = join_waves(s, part);
+    } else {
+      a += group * per_group * p.cols;
+      if (how == kByWave)
+        s = live ? column_sum(a, per_group, p.cols) : 0.0f;
+      else
+        s = join_waves(live ? column_sum(a, per_group, p.cols, wave, kSumWaves) : 0.0f, part);
+    }
+    if (!live || ((pre || how != kByWave) && wave != 0)) continue;
+    if (!pre && how != kTogether) s = of_group(group, c, s);
+    float *out = pre ? p.dpre : p.dpost;
+    if (out == nullptr) continue;
+    if (!pre && how != kTogether && p.groups > 1)
+      *a = s;
     else
-      p.dpost[c] = p.accumulate ? p.dpost[c] + v : v;
+      out[c] = p.accumulate ? out[c] + s : s;
   }
 }
 
@@ -601,7 +617,8 @@ __global__ __launch_bounds__(64 * kSumWaves) void column_grad_kernel(ResidualGra
 __global__ __launch_bounds__(64 * kSumWaves) void post_grad_kernel(ResidualGradParams p, int64_t per_group, int64_t chunks) {
   __shared__ float part[64 * kSumWaves];
   const int64_t c = int64_t(blockIdx.x) * 64 + (threadIdx.x & 63);
-  const float s = column_sum(p.sums + chunks * p.cols + c, p.groups, per_group * p.cols, c < p.cols, kSumWaves, part);
+  const float *a = p.sums + chunks * p.cols + c;
+  const float s = join_waves(c < p.cols ? column_sum(a, p.groups, per_group * p.cols, threadIdx.x >> 6, kSumWaves) : 0.0f, part);
   if (threadIdx.x < 64 && c < p.cols) p.dpost[c] = p.accumulate ? p.dpost[c] + s : s;
 }
 
@@ -609,6 +626,7 @@ __global__ __launch_bounds__(64 * kSumWaves) void post_grad_kernel(ResidualGradP
 // waves a group / one: 8192 x 8192 with a row of gates for 256 rows (16 chunks) 191 / 173,
 // 64 rows (4) 261 / 182, 16 rows (1) 545 / 224; 2048 x 2048, 128 rows (8) 24.4 / 23.0.
 constexpr int64_t kFewChunks = 16;
+constexpr int64_t kFewGroups = 256;  // (sixteen a wave) that are added up together
 
 // Lanes and vectors of eight values a lane for a row.
 struct RowShape {
@@ -693,16 +711,18 @@ hipError_t launch_residual_grad(const ResidualGradParams &p, hipStream_t s) {
   }
   const int64_t blocks_c = (p.cols + 63) / 64, pre_blocks = p.dpre != nullptr ? blocks_c : 0;
   // (without rows one group of no chunks, whose sums are zero)
-  const int64_t post_blocks = p.dpost != nullptr || (p.dgate != nullptr && p.groups > 0) ? std::max<int64_t>(p.groups, 1) * blocks_c : 0;
+  const bool post = p.dpost != nullptr || (p.dgate != nullptr && p.groups > 0);
+  const bool together = p.dpost != nullptr && p.groups > 1 && p.groups <= kFewGroups && per_group <= kFewChunks;
+  const int how = per_group > kFewChunks ? kByWorkgroup : together ? kTogether : kByWave;
+  const int64_t post_blocks = !post ? 0 : together ? blocks_c : std::max<int64_t>(p.groups, 1) * blocks_c;
   if (pre_blocks + post_blocks == 0) return hipSuccess;
   ResidualGradParams q = p;
   if (p.groups == 0) q.dgate = nullptr, q.gate = nullptr;
   const dim3 block(64 * kSumWaves);
-  const int waves = per_group > kFewChunks ? kSumWaves : 1;
-  const int64_t blocks = pre_blocks + (post_blocks * waves + kSumWaves - 1) / kSumWaves, most = (int64_t(1) << 22) - 1;
+  const int64_t blocks = pre_blocks + (how == kByWave ? (post_blocks + kSumWaves - 1) / kSumWaves : post_blocks), most = (int64_t(1) << 22) - 1;
   hipError_t e = klaunch(column_grad_kernel, dim3(unsigned(std::min(blocks, most))), block, 0, s, q, chunks > 0 ? per_group : 0, chunks, blocks_c,
-                         pre_blocks, post_blocks, waves);
-  if (e == hipSuccess && p.groups > 1 && p.dpost != nullptr)
+                         pre_blocks, post_blocks, how);
+  if (e == hipSuccess && p.groups > 1 && p.dpost != nullptr && !together)
     e = klaunch(post_grad_kernel, dim3(unsigned(blocks_c)), block, 0, s, p, per_group, chunks);
   return e;
 }

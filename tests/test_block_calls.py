@@ -147,15 +147,18 @@ def launches(qe, hip, cases):
 
 def test_launches():
     """A cast is one kernel, a norm one and one more for its transposed codes; a gradient one, one more for the sums of columns, one
-    for the sums over the rows of gates, and one where few long rows leave the columns to it."""
+    for the sums over the rows of gates where they are more than 256 or have more than 16 chunks, and one where few long rows leave
+    the columns to it."""
     got = calls(launches, [["cast", 100, 300, {"col": 1}], ["cast", 100, 300, {"row": False}], ["norm", 100, 300, {}], ["norm", 100, 300, {"col": 1}],
                            ["grad", 100, 300, {}], ["grad", 100, 300, {"sums": 1}], ["grad", 100, 300, {"sums": 1, "gate": 30}],
                            ["grad", 100, 300, {"sums": 1, "gate": 100}], ["grad", 100, 4096, {"sums": 1}], ["grad", 1360, 4096, {"sums": 1}],
                            ["grad", 1361, 4096, {"sums": 1}], ["grad", 100, 4097, {"sums": 1}], ["grad", 0, 300, {"sums": 1}],
+                           ["grad", 300, 300, {"sums": 1, "gate": 1}], ["grad", 544, 300, {"sums": 1, "gate": 272}],
                            ["norm", 0, 300, {"col": 1}]])
     sums, apart = ["residual_grad", "column_grad"], ["residual_grad", "column_sums", "column_grad"]
     assert [[n.rstrip("_") for n in g] for g in got] == [["block_cast"], [], ["residual_norm"], ["residual_norm", "block_cast"], ["residual_grad"],
-                                                         sums, sums + ["post_grad"], sums, apart, apart, sums, sums, ["column_grad"], []]
+                                                         sums, sums, sums, apart, apart, sums, sums, ["column_grad"],
+                                                         sums + ["post_grad"], sums + ["post_grad"], []]
 
 
 def grids(qe, hip, cases):
@@ -190,12 +193,14 @@ def test_products_get_their_kernels(units, monkeypatch):
 def test_launches_hold_less_than_2_to_32_lanes():
     """Kernels with 512 lanes a workgroup (rows of products) and 1024 (sums of columns) at the largest sizes that are accepted."""
     got = calls(grids, [["product", 16, (1 << 27) - 16, 2048], ["product", 16, 1 << 27, 2048], ["product", 1, (1 << 29) - 32, 128],
-                        ["grad", (1 << 22) - 1, 8192, 1], ["grad", (1 << 22) - 1, 16384, 1], ["grad", 8 * 272, 256, 272], ["grad", 8 * 256, 256, 256]])
+                        ["grad", (1 << 22) - 1, 8192, 1], ["grad", (1 << 22) - 1, 16384, 1], ["grad", 8 * 272, 256, 272], ["grad", 8 * 256, 256, 256],
+                        ["grad", 257 * 16, 256, 16]])
     assert "block_rows_kernel" in got[0][0][0] and got[0][0][1] == (1 << 23) - 1
     assert "block_rows_kernel" not in got[1][0][0] and got[2][0][1] * 256 < 1 << 32
     for g in got[3:5]:
         assert [n for n, _ in g if "column_grad" in n] and all(w * 1024 < 1 << 32 for _, w in g)
-    assert [[w for n, w in g if "column_grad" in n] for g in got[5:]] == [[4 + 8 * 4], [4 + 2]]  # 17 chunks a group, and 16: a wave each
+    assert [[w for n, w in g if "column_grad" in n] for g in got[5:]] == [
+        [4 + 8 * 4], [4 + 4], [4 + 65]]  # groups of 17 chunks, of 16: together, a wave each; more than 256 groups: sixteen a workgroup
 
 
 def test_struct_sizes():

@@ -265,6 +265,14 @@ def test_gradient_options(form, how):
         check_grad(Case(need_lib(), dev(), *shape, 8, **form), **how)
 
 
+@pytest.mark.parametrize("shape,gate_rows", [((8704, 70), 1088), ((600, 200), 2), ((257, 64), 1), ((1028, 130), 4), ((4096, 520), 16), ((2176, 64), 272)],
+                         ids=ids)
+def test_gradient_of_many_groups_and_chunks(shape, gate_rows):
+    """Groups of more than 16 chunks, more than 256 groups, and 256 of one chunk."""
+    check_grad(Case(need_lib(), dev(), *shape, 9, gate_rows=gate_rows, weights="f32"))
+    check_grad(Case(need_lib(), dev(), *shape, 10, gate_rows=gate_rows, weights="f32", post=False), mode=1)
+
+
 def test_no_rows():
     """Nothing but the weights' gradients, which INIT clears and ACCUM keeps."""
     qe, d = need_lib(), dev()

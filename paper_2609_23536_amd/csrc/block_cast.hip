@@ -10,7 +10,8 @@
 // the scale itself and converts two values: two of a row, or, for the transposed codes,
 // the same column's of two rows, so that a lane has eight neighbouring codes of each of
 // its columns.  Those go through LDS, column by column, and leave as 128-byte runs.  The
-// values may be a norm's output, computed on the fly from its input and the rows' factors.
+// values may be a norm's output, computed on the fly from its input and the rows' factors
+// (for the transposed codes alone: the row-wise ones left with the norm).
 //
 // Of BF16 values the maxima are taken on pairs of 16-bit patterns with the sign off,
 // which order like the values (NaN above infinity), and no value is widened at all.
@@ -83,8 +84,11 @@ __device__ __forceinline__ void load_weights4(const BlockCastParams &p, int64_t 
   for (int e = 0; e < 4; ++e) f[e] += p.offset;
 }
 
+// How a launch goes about its tiles.
+enum CastHow { kByXcd = 1, kRowLines = 2, kColLines = 4 };
+
 template <bool BF16, int FMT, bool SQUARE, bool NORM, bool EDGE>
-__device__ __forceinline__ void cast_tile(const BlockCastParams &p, int tr, int tc, uint8_t *tile, uint32_t *part) {
+__device__ __forceinline__ void cast_tile(const BlockCastParams &p, int tr, int tc, int how, uint8_t *tile, uint32_t *part) {
   constexpr bool PACKED = BF16 && !NORM;
   constexpr int HI = BF16 ? 4 : 64;  // from a lane's first quad of columns to its second
   const int tid = threadIdx.x, wave = tid >> 6, rg = tid >> 4, cl = (tid & 15) * (BF16 ? 8 : 4);
@@ -206,12 +210,12 @@ __device__ __forceinline__ void cast_tile(const BlockCastParams &p, int tr, int 
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float a = __builtin_fabsf(v.f(s, e));
-        row_max[s] = nan_max(row_max[s], a);
+        if (!NORM) row_max[s] = nan_max(row_max[s], a);
         if (!SQUARE) col_max[e] = nan_max(col_max[e], a);
       }
       if constexpr (SQUARE)
         all = nan_max(all, row_max[s]);
-      else
+      else if constexpr (!NORM)
         row_byte[s] = block_byte<FMT>(max_lanes16(row_max[s]));
     }
     if constexpr (SQUARE) {
@@ -273,7 +277,7 @@ __device__ __forceinline__ void cast_tile(const BlockCastParams &p, int tr, int 
   }
 
   // Row-wise codes.
-  if (p.row.data != nullptr) {
+  if (!NORM && p.row.data != nullptr) {
 #pragma unroll
     for (int s = 0; s < kRows; ++s) {
       const int row = rg * kRows + s;
@@ -291,7 +295,7 @@ __device__ __forceinline__ void cast_tile(const BlockCastParams &p, int tr, int 
       uint8_t *dst = p.row.data + (r0 + row) * p.row.ld + c0 + cl;
       if (!EDGE || cl + HI + 4 <= cols) {
         if constexpr (BF16) {
-          *reinterpret_cast<u32x2_out *>(dst) = u32x2_out{q[0], q[1]};
+          store_out(dst, u32x2_out{q[0], q[1]}, (how & kRowLines) != 0);
         } else {
           *reinterpret_cast<u32_out *>(dst) = q[0];
           *reinterpret_cast<u32_out *>(dst + HI) = q[1];
@@ -333,7 +337,7 @@ __device__ __forceinline__ void cast_tile(const BlockCastParams &p, int tr, int 
     const uint4 w4 = *reinterpret_cast<const uint4 *>(tile + turned(c, chunk));
     uint8_t *dst = p.col.data + (c0 + c) * p.col.ld + r0 + chunk * 16;
     if (!EDGE || left >= 16) {
-      *reinterpret_cast<u32x4_out *>(dst) = u32x4_out{w4.x, w4.y, w4.z, w4.w};
+      store_out(dst, u32x4_out{w4.x, w4.y, w4.z, w4.w}, (how & kColLines) != 0);
     } else {
       const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
@@ -344,31 +348,35 @@ __device__ __forceinline__ void cast_tile(const BlockCastParams &p, int tr, int 
 }
 
 template <bool BF16, int FMT, bool SQUARE, bool NORM>
-__global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastParams p, int tiles_r, int tiles_c, int by_xcd) {
+__global__ __launch_bounds__(kThreads) void block_cast_kernel(BlockCastParams p, int tiles_r, int tiles_c, int how) {
   __shared__ __attribute__((aligned(16))) uint8_t tile[kTile * kTile];
   __shared__ __attribute__((aligned(16))) uint32_t part[4 * kTile];
-  const int id = by_xcd ? xcd_remap(int(blockIdx.x), tiles_r * tiles_c) : int(blockIdx.x);
+  const int id = how & kByXcd ? xcd_remap(int(blockIdx.x), tiles_r * tiles_c) : int(blockIdx.x);
   const int tr = id / tiles_c, tc = id % tiles_c;
   if (int64_t(tr + 1) * kTile <= p.rows && int64_t(tc + 1) * kTile <= p.cols)
-    cast_tile<BF16, FMT, SQUARE, NORM, false>(p, tr, tc, tile, part);
+    cast_tile<BF16, FMT, SQUARE, NORM, false>(p, tr, tc, how, tile, part);
   else
-    cast_tile<BF16, FMT, SQUARE, NORM, true>(p, tr, tc, tile, part);
+    cast_tile<BF16, FMT, SQUARE, NORM, true>(p, tr, tc, how, tile, part);
 }
 
 template <bool BF16, int FMT>
 hipError_t launch_fmt(const BlockCastParams &p, hipStream_t s) {
   const int64_t tiles_r = (p.rows + kTile - 1) / kTile, tiles_c = (p.cols + kTile - 1) / kTile;
   const dim3 grid{unsigned(tiles_r * tiles_c)}, block(kThreads);
-  // Rows of tiles that stay on one XCD: their bytes of a row share lines of its L2.  The
-  // cast of both orders, MI355X, us, without / so: BF16 8192 x 28672 209 / 200, 57344 x
-  // 8192 in square blocks 364 / 352, 4096 x 14336 54.4 / 54.2; row-wise only 36.9 / 38.8
-  // and FP32 8192 x 8192 82.8 / 93.8, so not there, nor where the values are
-  // a norm's (8192 x 8192, right after the kernel that wrote its input: 47 / 55).
-  const int by_xcd = BF16 && p.col.data != nullptr && p.rstd == nullptr ? 1 : 0;
+  // Rows of tiles that stay on one XCD: neighbours write one line of codes, or of bytes, to
+  // its L2.  The cast of BF16 in both orders, MI355X, us, over all XCDs / so: where lines of
+  // codes are shared, 8008 x 8040 93 / 86, 1500 x 4099 13.2 / 11.8; with whole lines 4096 x
+  // 4096 16.7 / 18.4, 8192 x 8192 57.5 / 65.6, 16384 x 16384 252 / 258, but 4096 x 28672
+  // 107 / 100, 8192 x 28672 203 / 195, 57344 x 8192 in square blocks 362 / 348.  Row-wise
+  // only it is 36.9 / 38.8, FP32 8192 x 8192 87 / 93, a norm's values 8192 x 8192, right after
+  // the kernel that wrote its input, 121 / 134 (with that kernel): not there.
+  const bool lines = whole_lines(p.col) && (p.row.data == nullptr || whole_lines(p.row));
+  const bool by_xcd = BF16 && p.col.data != nullptr && p.rstd == nullptr && (!lines || p.cols > 16384 || p.rows * p.cols > int64_t(1) << 28);
+  const int how = (by_xcd ? kByXcd : 0) | (whole_lines(p.row) ? kRowLines : 0) | (whole_lines(p.col) ? kColLines : 0);
   const bool square = (p.row.data != nullptr ? p.row : p.col).row_shift != 0;
-  if (p.rstd != nullptr) return klaunch(block_cast_kernel<BF16, FMT, false, true>, grid, block, 0, s, p, int(tiles_r), int(tiles_c), by_xcd);
-  return square ? klaunch(block_cast_kernel<BF16, FMT, true, false>, grid, block, 0, s, p, int(tiles_r), int(tiles_c), by_xcd)
-                : klaunch(block_cast_kernel<BF16, FMT, false, false>, grid, block, 0, s, p, int(tiles_r), int(tiles_c), by_xcd);
+  if (p.rstd != nullptr) return klaunch(block_cast_kernel<BF16, FMT, false, true>, grid, block, 0, s, p, int(tiles_r), int(tiles_c), how);
+  return square ? klaunch(block_cast_kernel<BF16, FMT, true, false>, grid, block, 0, s, p, int(tiles_r), int(tiles_c), how)
+                : klaunch(block_cast_kernel<BF16, FMT, false, false>, grid, block, 0, s, p, int(tiles_r), int(tiles_c), how);
 }
 
 }  // namespace

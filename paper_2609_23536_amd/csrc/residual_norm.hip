@@ -148,7 +148,7 @@ __device__ __forceinline__ void branch_factors(const P &p, int64_t group, const 
 // A workgroup takes rows blockIdx.x, + gridDim.x, .. of the launch.
 // NV 1: 64 registers, so that a unit holds two workgroups of 1024 lanes.
 template <int NV, bool BF16>
-__global__ __launch_bounds__(kLanes, NV == 1 ? 8 : 4) void residual_norm_kernel(ResidualParams p) {
+__global__ __launch_bounds__(kLanes, NV == 1 ? 8 : 4) void residual_norm_kernel(ResidualParams p, int row_lines) {
   __shared__ float reds[4][kLanes / 64];
   const int tid = threadIdx.x, waves = int(blockDim.x) >> 6;
   const float inv_cols = 1.0f / float(p.cols);
@@ -262,9 +262,9 @@ __global__ __launch_bounds__(kLanes, NV == 1 ? 8 : 4) void residual_norm_kernel(
         const uint32_t byte = p.row.fmt == 0 ? block_byte<0>(a) : block_byte<1>(a);
         const float step = block_step(byte);
         if (p.row.fmt == 0)
-          store_codes8(dst, c.n[v], block_codes<0>(h, step), block_codes<0>(h + 4, step));
+          store_codes8(dst, c.n[v], block_codes<0>(h, step), block_codes<0>(h + 4, step), row_lines != 0);
         else
-          store_codes8(dst, c.n[v], block_codes<1>(h, step), block_codes<1>(h + 4, step));
+          store_codes8(dst, c.n[v], block_codes<1>(h, step), block_codes<1>(h + 4, step), row_lines != 0);
         if ((tid & 15) == 0 && c.n[v] > 0) (p.row.exps + row * p.row.ld_exps)[c.col[v] / kBlock] = uint8_t(byte);
       }
     }
@@ -670,9 +670,10 @@ hipError_t launch_residual_norm(const ResidualParams &p, hipStream_t s) {
   // as many workgroups as the units hold at once (2048 lanes each), each with the rows it then has
   const int64_t most = int64_t(compute_units()) * (2048 / sh.lanes);
   const dim3 grid{unsigned(std::min(p.rows, most))}, block{unsigned(sh.lanes)};
-  if (sh.vectors == 1)
-    return bf16 ? klaunch(residual_norm_kernel<1, true>, grid, block, 0, s, p) : klaunch(residual_norm_kernel<1, false>, grid, block, 0, s, p);
-  return bf16 ? klaunch(residual_norm_kernel<2, true>, grid, block, 0, s, p) : klaunch(residual_norm_kernel<2, false>, grid, block, 0, s, p);
+  const int lines = whole_lines(p.row) ? 1 : 0;
+  return klaunch(sh.vectors == 1 ? (bf16 ? residual_norm_kernel<1, true> : residual_norm_kernel<1, false>)
+                                 : (bf16 ? residual_norm_kernel<2, true> : residual_norm_kernel<2, false>),
+                 grid, block, 0, s, p, lines);
 }
 
 hipError_t launch_residual_grad(const ResidualGradParams &p, hipStream_t s) {

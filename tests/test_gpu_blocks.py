@@ -67,7 +67,7 @@ def check_cast(qe, d, x, fmt, block_rows, row=True, col=True, pad=0, t="f32"):
     return r, c
 
 
-CAST_SHAPES = [(1, 1), (1, 128), (1, 513), (3, 130), (127, 129), (128, 128), (129, 255), (250, 300), (16, 1000), (300, 7)]
+CAST_SHAPES = [(1, 1), (1, 128), (256, 384), (131, 512), (1, 513), (3, 130), (127, 129), (128, 128), (129, 255), (250, 300), (16, 1000), (300, 7)]
 
 
 @pytest.mark.parametrize("how", [("f32", 0, 1, 0), ("bf16", 0, 1, 0), ("bf16", 1, 1, 3), ("f32", 1, 1, 1), ("bf16", 0, 128, 0), ("f32", 1, 128, 5)],

@@ -18,9 +18,10 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libqe.so")
 
-HIP_SOURCES = ["api.hip", "quantize.hip", "scale_update.hip", "gemm_fp8.hip", "gemm_ring.hip", "gemm_dispatch.hip",
-               "grad_copy.hip", "amax.hip", "act_gemm.hip", "act_grad.hip", "act_save.hip", "block_cast.hip", "block_gemm.hip",
-               "residual_norm.hip"]
+HIP_SOURCES = ["act_gemm.hip", "gemm_fp8.hip", "gemm_ring.hip", "block_gemm_e4m3_e4m3.hip", "block_gemm_e5m2_e4m3.hip",
+               "block_gemm_e4m3_e5m2.hip", "block_gemm_e5m2_e5m2.hip", "act_grad.hip",  # the longest to compile first
+               "api.hip", "quantize.hip", "scale_update.hip", "gemm_dispatch.hip", "grad_copy.hip", "amax.hip", "act_save.hip",
+               "block_gemm.hip", "block_cast.hip", "residual_norm.hip"]
 CXX_SOURCES = ["contract.cpp"]
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",

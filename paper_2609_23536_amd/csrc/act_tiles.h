@@ -367,7 +367,91 @@ __device__ __forceinline__ int b_row(int r) {
   return GATED ? (r >> 5) * 16 + (r & 15) : r;
 }
 
-template <bool GATED, int FA, int FB, int BM, int BN, typename P>
+// Sums that are only rounded or added to a residual, of a whole wave's block of TM rows
+// x 128 columns: 16 rows at a time through LDS and out in whole row runs, every address a
+// scalar row offset and one of the lane's (with one wave a SIMD the instructions are the
+// time).  The residual, of the output's type, is read in the order of the stores, 16 rows
+// ahead.  RES: there may be one, `has` says whether (two variants of FP32 spill).  MI355X,
+// us, block scales, by the general epilogue / so: BF16 6144 x 4096 x 2048 62.3 / 48.9, with a
+// residual 75.4 / 58.9; 4096 x 14336 x 4096 with one 261 / 214.
+template <int TM, bool BF16, bool RES>
+__device__ __forceinline__ void store_sums(const ActGemmParams &g, const v4f (&acc)[TM / 16][8], uint8_t *ls, int lane, int64_t row0, int64_t col0,
+                                           bool has) {
+  constexpr int ES = BF16 ? 2 : 4;                                         // bytes an element
+  constexpr int LPR = BF16 ? 16 : 32, STEP = 64 / LPR, STEPS = 16 / STEP;  // lanes a row, rows and steps
+  constexpr bool NARROW = BF16 && !RES;                                    // rounded before the trip
+  constexpr int PITCH = NARROW ? (128 + 8) * 2 : (128 + 4) * 4;
+  auto rsrc = [&](const void *p, int64_t ld) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(uniform(static_cast<const uint8_t *>(p) + (row0 * ld + col0) * ES)), short(0), 0x7fffffff, 0x00020000);
+  };
+  const __amdgpu_buffer_rsrc_t out = rsrc(g.c, g.ldc), in = RES && has ? rsrc(g.residual, g.ld_residual) : out;
+  const int pitch = int(g.ldc) * ES, in_pitch = int(g.ld_residual) * ES;
+  const uint32_t at = uint32_t(lane / LPR) * uint32_t(pitch) + lane % LPR * 16, in_at = uint32_t(lane / LPR) * uint32_t(in_pitch) + lane % LPR * 16;
+  v4i res[2][RES ? STEPS : 1] = {};
+  auto fetch = [&](auto block) {
+    constexpr int i = decltype(block)::value;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) res[i % 2][s] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(in, in_at, (16 * i + STEP * s) * in_pitch, kNT));
+  };
+  if constexpr (RES)
+    if (has) fetch(std::integral_constant<int, 0>{});
+  static_for<TM / 16>([&](auto block) {
+    constexpr int i = decltype(block)::value;
+    if constexpr (RES && i + 1 < TM / 16)
+      if (has) fetch(std::integral_constant<int, i + 1>{});
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const v4f a = acc[i][j];
+      uint8_t *to = ls + (lane & 15) * PITCH + (16 * j + 4 * (lane >> 4)) * (NARROW ? 2 : 4);
+      if constexpr (NARROW)
+        *reinterpret_cast<uint2 *>(to) = make_uint2(bf16x2_bits(a[0], a[1]), bf16x2_bits(a[2], a[3]));
+      else
+        *reinterpret_cast<v4f *>(to) = a;
+    }
+    // (LDS operations of one wave complete in order)
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const uint8_t *from = ls + (lane / LPR + STEP * s) * PITCH + lane % LPR * (128 / LPR) * (NARROW ? 2 : 4);
+      v4i w;
+      if constexpr (NARROW) {
+        w = *reinterpret_cast<const v4i *>(from);
+      } else {
+        float f[128 / LPR];
+#pragma unroll
+        for (int q = 0; q < 32 / LPR; ++q) {
+          const v4f v = *reinterpret_cast<const v4f *>(from + 16 * q);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[4 * q + e] = v[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 128 / LPR; ++e)
+          if constexpr (RES) {
+            const uint32_t r = uint32_t(res[i % 2][s][BF16 ? e / 2 : e]);
+            const float sum = f[e] + __uint_as_float(!BF16 ? r : (e % 2 == 0 ? r << 16 : r & 0xffff0000u));
+            f[e] = has ? sum : f[e];
+          }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = BF16 ? int(bf16x2_bits(f[BF16 ? 2 * e : 0], f[BF16 ? 2 * e + 1 : 0])) : int(__float_as_uint(f[e]));
+      }
+      __builtin_amdgcn_raw_buffer_store_b128(w, out, at, (16 * i + STEP * s) * pitch, kNT);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+
+// Whether a product's sums can go that way: no more than a residual of the output's type in
+// the epilogue, rows of both aligned to four elements, and a tile's rows within 2^31 bytes.
+__device__ __forceinline__ bool only_sums(const ActGemmParams &g, int rows) {
+  const int es = g.c_bf16 ? 2 : 4;
+  auto fits = [&](const void *p, int64_t ld) { return ld % 4 == 0 && uintptr_t(p) % (4 * es) == 0 && ld * es * (rows + 4) < int64_t(1) << 31; };
+  return g.act == kActNone && g.bias == nullptr && g.z.kind == kSavedNone && fits(g.c, g.ldc) &&
+         (g.residual == nullptr || ((g.residual_bf16 != 0) == (g.c_bf16 != 0) && fits(g.residual, g.ld_residual)));
+}
+
+// OUT: the output's type where the kernel is one type's, which then stores bare sums by
+// store_sums.
+enum TileOut { kEither, kF32, kBF16 };
+template <bool GATED, int FA, int FB, int BM, int BN, TileOut OUT = kEither, typename P>
 __device__ __forceinline__ void act_large_tile(const P &g, int tiles_m, int tiles_n) {
   constexpr int NW = 4, TM = BM / 2, TN = BN / 2, BNO = GATED ? BN / 2 : BN;
   constexpr int I = TM / 16, J = TN / 16;
@@ -414,6 +498,13 @@ __device__ __forceinline__ void act_large_tile(const P &g, int tiles_m, int tile
   uint8_t *ls_c = GATED ? ls_u + 16 * NR * Rows<QV, 2>::PITCH : ls_u;  // D last: at most FP32
   static_assert(16 * NR * ((GATED ? 2 : 1) * Rows<QV, 2>::PITCH + Rows<QV, 4>::PITCH) <= STAGE / 2, "the blocks staged fit");
   const bool has_res = !GATED && g.residual != nullptr, res_bf16 = g.residual_bf16 != 0;
+  if constexpr (OUT != kEither) {
+    static_assert(TN == 128 && !GATED, "blocks of 128 columns a wave");
+    if (rows_left >= TM && cols >= TN && only_sums(g, TM)) {
+      if (OUT == kBF16 && !has_res) return store_sums<TM, true, false>(g, acc, ls, lane, wrow, wcol, false);
+      return store_sums<TM, OUT == kBF16, true>(g, acc, ls, lane, wrow, wcol, OUT == kBF16 || has_res);
+    }
+  }
   const bool i8 = g.z.kind == kSavedI8, kept = g.z.kind == kSavedBF16;
   auto finish = [&](auto edge) {
     constexpr bool EDGE = decltype(edge)::value;  // part of the wave's block does not exist
@@ -493,7 +584,7 @@ __device__ __forceinline__ void act_large_tile(const P &g, int tiles_m, int tile
         if constexpr (GATED)
           store_staged<EDGE, QV, NR, 2>(ls_u, lane, static_cast<uint16_t *>(g.u.data) + row * g.u.ld + wcol, g.u.ld * 2, rows, cols);
       }
-      if (g.c_bf16) {
+      if (OUT == kEither ? g.c_bf16 != 0 : OUT == kBF16) {
         stage_block<QV, NR, true>(ls_c, lane, z);
         store_staged<EDGE, QV, NR, 2>(ls_c, lane, static_cast<uint16_t *>(g.c) + row * g.ldc + wcol, g.ldc * 2, rows, cols);
       } else {

@@ -3,30 +3,20 @@
 //     D = act(Z) + residual
 // The kernels are those of the products with one scale per operand (act_tiles.h);
 // the matrix instruction applies the scales, powers of two, to its products by
-// itself (LdsScales in gemm_loops.h), so nothing is added to the sums' arithmetic.
-#include "act_tiles.h"
+// itself (LdsScales in gemm_loops.h), so nothing is added to the sums' arithmetic.  A
+// row's bytes are a 128th of its codes: from LDS, a word for four K tiles, they cost the
+// large tiles 4%, the small ones, which read single bytes, up to 11% of their time.
+// Bound by the matrix instructions from K = 4096 on (MI355X: 8192 x 8192 x 28672 1310 us,
+// 2.9 PFLOP/s; 4096 x 4096 x 28672 325 us, one round of tiles), by each round's prologue
+// and stores below (6144 x 4096 x 2048 with a residual 59 us, 1.75 PFLOP/s), for a few
+// rows by the other operand's bytes (1 x 4096 x 14336 12.9 us, 4.6 TB/s).
+#include "block_gemm.h"
+#include "gemm_util.h"
 
 namespace qe {
 namespace {
 
-template <int FA, int FB, int OB, int W>
-__global__ __launch_bounds__(64 * W) void block_rows_kernel(BlockGemmParams g, int blocks_n) {
-  act_rows_tile<false, FA, FB, OB, W>(g, blocks_n);
-}
-
-template <int FA, int FB, int BM, int BN>
-__global__ __launch_bounds__(256) void block_large_kernel(BlockGemmParams g, int tiles_m, int tiles_n) {
-  act_large_tile<false, FA, FB, BM, BN>(g, tiles_m, tiles_n);
-}
-
-template <int FA, int FB, int BM, int BN, int S>
-__global__ __launch_bounds__(256, (BM + BN) * BK * S > 81920 ? 1 : 2) void block_ring_kernel(BlockGemmParams g, int tiles_m,
-                                                                                             int tiles_n) {
-  act_ring_tile<false, FA, FB, BM, BN, S>(g, tiles_m, tiles_n);
-}
-
 constexpr int64_t kFewRows = 16;
-constexpr int kFewRowsTile = 0;  // in place of a GemmTile
 
 // As for one scale per operand (few_blocks in act_gemm.hip); a launch holds less than
 // 2^32 lanes, 512 of them a block.
@@ -36,39 +26,6 @@ bool few_blocks(const BlockGemmParams &p) {
   if (p.m <= kFewRows) return blocks < int64_t(1) << 23;
   if (p.k <= 1024) return false;
   return blocks <= cus || (blocks <= 2 * cus && p.k > 12288 && !wide);
-}
-
-template <int FA, int FB>
-hipError_t launch_rows(const BlockGemmParams &p, hipStream_t s) {
-  const bool wide = p.z.kind == kSavedI8, few = p.k <= 16 * BK;
-  const int blocks_n = int((p.n + (wide ? 31 : 15)) / (wide ? 32 : 16));
-  const dim3 grid(unsigned((p.m + 15) / 16) * unsigned(blocks_n));
-  if (wide)
-    return few ? klaunch(block_rows_kernel<FA, FB, 2, 4>, grid, dim3(256), 0, s, p, blocks_n)
-               : klaunch(block_rows_kernel<FA, FB, 2, 8>, grid, dim3(512), 0, s, p, blocks_n);
-  return few ? klaunch(block_rows_kernel<FA, FB, 1, 4>, grid, dim3(256), 0, s, p, blocks_n)
-             : klaunch(block_rows_kernel<FA, FB, 1, 8>, grid, dim3(512), 0, s, p, blocks_n);
-}
-
-template <int FA, int FB>
-hipError_t launch_tile(int tile, const BlockGemmParams &p, hipStream_t s) {
-  if (tile == kFewRowsTile) return launch_rows<FA, FB>(p, s);
-  const dim3 block(256);
-  auto tiles = [&](auto *kernel, int bm, int bn) {
-    const int tm = int((p.m + bm - 1) / bm), tn = int((p.n + bn - 1) / bn);
-    return klaunch(kernel, dim3(unsigned(tm) * unsigned(tn)), block, 0, s, p, tm, tn);
-  };
-  switch (tile) {
-    case kTile64x64: return tiles(block_ring_kernel<FA, FB, 64, 64, 4>, 64, 64);
-    case kTile128x64: return tiles(block_ring_kernel<FA, FB, 128, 64, 3>, 128, 64);
-    case kTile128x64Deep: return tiles(block_ring_kernel<FA, FB, 128, 64, 6>, 128, 64);
-    case kTile64x128: return tiles(block_ring_kernel<FA, FB, 64, 128, 3>, 64, 128);
-    case kTile64x128Deep: return tiles(block_ring_kernel<FA, FB, 64, 128, 6>, 64, 128);
-    case kTile128x128: return tiles(block_ring_kernel<FA, FB, 128, 128, 2>, 128, 128);
-    case kTile128x128Deep: return tiles(block_ring_kernel<FA, FB, 128, 128, 4>, 128, 128);
-    case kTile192x256: return tiles(block_large_kernel<FA, FB, 192, 256>, 192, 256);
-    default: return tiles(block_large_kernel<FA, FB, 256, 256>, 256, 256);
-  }
 }
 
 }  // namespace
@@ -90,10 +47,10 @@ hipError_t launch_block_gemm(const BlockGemmParams &p, hipStream_t s) {
   const int force = gemm_tile_override();
   const int tile = force == kTileAuto ? (few_blocks(p) ? kFewRowsTile : choose_gemm_tile(g, kShapes))
                                       : (force == kTile192x256 ? kTile192x256 : kTile256x256);
-  if (p.fmt_a == 0 && p.fmt_b == 0) return launch_tile<0, 0>(tile, p, s);
-  if (p.fmt_a == 1 && p.fmt_b == 0) return launch_tile<1, 0>(tile, p, s);
-  if (p.fmt_a == 0 && p.fmt_b == 1) return launch_tile<0, 1>(tile, p, s);
-  return launch_tile<1, 1>(tile, p, s);
+  if (p.fmt_a == 0 && p.fmt_b == 0) return launch_block_tile<0, 0>(tile, p, s);
+  if (p.fmt_a == 1 && p.fmt_b == 0) return launch_block_tile<1, 0>(tile, p, s);
+  if (p.fmt_a == 0 && p.fmt_b == 1) return launch_block_tile<0, 1>(tile, p, s);
+  return launch_block_tile<1, 1>(tile, p, s);
 }
 
 }  // namespace qe

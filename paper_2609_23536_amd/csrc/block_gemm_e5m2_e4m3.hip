@@ -1,0 +1,8 @@
+// Block-scaled products of E5M2 by E4M3.
+#include "block_gemm_tiles.h"
+
+namespace qe {
+
+template hipError_t launch_block_tile<1, 0>(int, const BlockGemmParams &, hipStream_t);
+
+}  // namespace qe

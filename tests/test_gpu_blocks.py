@@ -210,6 +210,21 @@ def test_large_tiles(tile, shape):
         assert qe.qe_set_gemm_tile(qe.TILE_AUTO) == "OK"
 
 
+@pytest.mark.parametrize("tile", ["TILE_256x256", "TILE_192x256"])
+@pytest.mark.parametrize("out,residual", [("bf16", "none"), ("bf16", "bf16"), ("f32", "none"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")])
+def test_bare_sums_of_large_tiles(tile, out, residual):
+    """Whole tiles of sums with at most a residual of their type, in place and apart, beside tiles at the edges; odd rows."""
+    qe, d = need_lib(), dev()
+    assert qe.qe_set_gemm_tile(getattr(qe, tile)) == "OK"
+    try:
+        for shape, pad in (((520, 516, 300), 0), ((520, 516, 1100), 4), ((260, 513, 129), 2)):
+            check_product(qe, d, shape, 4, out=out, residual=residual, bb=1, pad=pad)
+            if residual == out:
+                check_product(qe, d, shape, 5, out=out, residual=residual, fa=1, pad=pad, in_place=True)
+    finally:
+        assert qe.qe_set_gemm_tile(qe.TILE_AUTO) == "OK"
+
+
 def test_random_codes_against_float64():
     """Ordinary values: FP32 sums of 128 products which the instruction aligns to their largest; the plain product's tests allow 1e-3 of the largest."""
     qe, d = need_lib(), dev()

@@ -453,7 +453,8 @@ qe_status qe_residual_norm(const qe_matrix *x_host, const qe_matrix *y_host, int
  * receive those gradients (QE_PLACE_INIT) or are increased by them (QE_PLACE_ACCUM), in
  * FP32 and in an order that does not change from call to call; workspace then holds
  * 2 * cols * G * ceil(min(gate_rows, rows) / 16) floats, G the rows of gates (without
- * gates 2 * cols * ceil(rows / 16)), whose contents do not matter before or after.
+ * gates 2 * cols * ceil(rows / 16)), whose contents do not matter before or after and which
+ * no other call may use at the same time.
  * dpre_weight without dh, dpost_weight without y or its norm, and dgate without y or a
  * gate are refused.  Sizes as above, and with or without a workspace what it holds below
  * 2^23 rows of cols floats (rows 0: INIT clears the weights' gradients).

@@ -15,6 +15,8 @@
 //
 // Of BF16 values the maxima are taken on pairs of 16-bit patterns with the sign off,
 // which order like the values (NaN above infinity), and no value is widened at all.
+// Bound by memory: MI355X, both orders, BF16 4096 x 14336 51.5 us (4.6 TB/s), 57344 x 8192
+// in square blocks 347 (5.4 TB/s).
 #include "block_scale.h"
 #include "gemm_util.h"
 

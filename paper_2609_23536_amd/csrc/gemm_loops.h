@@ -327,37 +327,46 @@ __device__ __forceinline__ void large_k_loop(const uint8_t *a, const uint8_t *b,
     // be in flight: the counter completes in order
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
     __syncthreads();                       // tile 1 published; tile 0 fully read
-    auto step = [&](int t, int buf, auto byte) {
-      constexpr std::integral_constant<int, (decltype(byte)::value + 1) % 4> next{};
-      const bool dma = t + 2 < KT;
-      if (t + 2 < T && !dma) issue(t + 2, buf);
-      // The next group's scales, into the buffer whose last reads were of tile t - 1.
-      // They are older than the B part below, so the wait at this step's end covers
-      // them: three steps before they are read.
-      if constexpr (SC::kOn) {
+    if constexpr (SC::kOn) {  // four tiles a turn: which byte is part of the instruction
+      auto step = [&](int t, int buf, auto byte) {  // as below
+        constexpr std::integral_constant<int, (decltype(byte)::value + 1) % 4> next{};
+        const bool dma = t + 2 < KT;
+        if (t + 2 < T && !dma) issue(t + 2, buf);
+        // The next group's scales, into the buffer whose last reads were of tile t - 1.
+        // They are older than the B part below, so the wait at this step's end covers
+        // them: three steps before they are read.
         if constexpr (decltype(byte)::value == 0) sc.load(smem, wave, t / 4 + 1);
         if constexpr (decltype(next)::value == 0) scales_at(t / 4 + 1);
-      }
-      // phase B of tile t, with tile t+2's A part; reads of tile t+1 (in the
-      // last iteration they read a stale stage that is never used: always in
-      // bounds, and branch-free here)
-      phase_b(byte, buf ^ 1, dma, t + 2, buf, fa, fb);
-      if (t + 1 < T) {
-        __syncthreads();                   // tile t+1's B fragments read by every wave
-        phase_a(next, buf ^ 1, t + 3 < KT, t + 3, fa, fb);  // with tile t+3's B part
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
-        __syncthreads();                   // tile t+2 published; tile t+1 fully read
-      }
-    };
-    if constexpr (SC::kOn) {  // four tiles a turn: which byte is part of the instruction
+        phase_b(byte, buf ^ 1, dma, t + 2, buf, fa, fb);
+        if (t + 1 < T) {
+          __syncthreads();
+          phase_a(next, buf ^ 1, t + 3 < KT, t + 3, fa, fb);
+          asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
+          __syncthreads();
+        }
+      };
       for (int t = 0; t < T; t += 4) {
         step(t, 0, first);
         if (t + 1 < T) step(t + 1, 1, std::integral_constant<int, 1>{});
         if (t + 2 < T) step(t + 2, 0, std::integral_constant<int, 2>{});
         if (t + 3 < T) step(t + 3, 1, std::integral_constant<int, 3>{});
       }
-    } else {
-      for (int t = 0; t < T; ++t) step(t, t & 1, first);
+    } else {  // (through step the loop has three more branches a tile: 1% on large products)
+      for (int t = 0; t < T; ++t) {
+        const int buf = t & 1;
+        const bool dma = t + 2 < KT;
+        if (t + 2 < T && !dma) issue(t + 2, buf);
+        // phase B of tile t, with tile t+2's A part; reads of tile t+1 (in the
+        // last iteration they read a stale stage that is never used: always in
+        // bounds, and branch-free here)
+        phase_b(first, buf ^ 1, dma, t + 2, buf, fa, fb);
+        if (t + 1 < T) {
+          __syncthreads();                   // tile t+1's B fragments read by every wave
+          phase_a(first, buf ^ 1, t + 3 < KT, t + 3, fa, fb);  // with tile t+3's B part
+          asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHB) : "memory");
+          __syncthreads();                   // tile t+2 published; tile t+1 fully read
+        }
+      }
     }
     settle<SC::kOn>(acc);
   }

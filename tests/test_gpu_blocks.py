@@ -225,6 +225,34 @@ def test_bare_sums_of_large_tiles(tile, out, residual):
         assert qe.qe_set_gemm_tile(qe.TILE_AUTO) == "OK"
 
 
+@pytest.mark.parametrize("m,tile", [(3, "TILE_AUTO"), (130, "TILE_AUTO"), (520, "TILE_256x256"), (520, "TILE_192x256")])
+def test_products_of_long_strides(m, tile):
+    """Rows as far apart as they may be, outputs and residuals past 2^31 elements: the bits of the same call on packed rows."""
+    qe, d = need_lib(), dev()
+    rng = np.random.default_rng(3)
+    n, k, ld = 512, 384, 2 ** 23 - 16
+    qa, ea, _, ha = operand(qe, rng, m, k, 0, 1, d)
+    qb, eb, _, hb = operand(qe, rng, n, k, 1, 128, d)
+    wide = []
+    for q, e, br, fmt in ((qa, ea, 1, 0), (qb, eb, 128, 1)):
+        t = torch.empty((q.shape[0], ld), dtype=torch.uint8, device=d)
+        t[:, :k] = q[:, :k]
+        wide.append((t, qe.make_blocked(t, ld, e, e.shape[1], fmt, br)))
+    assert qe.qe_set_gemm_tile(getattr(qe, tile)) == "OK"
+    try:
+        for ldc in (2 ** 22, 2 ** 23 + 8):  # 2^22: whole tiles of bare sums, 128 rows of which stay below 2^31 bytes
+            res = torch.from_numpy(rng.normal(size=(m, n))).to(d).bfloat16()
+            c, far, far_res = torch.zeros((m, n), dtype=torch.bfloat16, device=d), *(torch.empty((m, ldc), dtype=torch.bfloat16, device=d) for _ in range(2))
+            far_res[:, :n], far[:, n:n + 8] = res, 3.0
+            assert qe.qe_fp8_gemm_block(ha, hb, m, n, k, qe.make_epilogue(residual=res, residual_dtype=qe.BF16, ld_residual=n), c, qe.BF16, n) == "OK"
+            assert qe.qe_fp8_gemm_block(wide[0][1], wide[1][1], m, n, k, qe.make_epilogue(residual=far_res, residual_dtype=qe.BF16, ld_residual=ldc),
+                                        far, qe.BF16, ldc) == "OK"
+            assert torch.equal(far[:, :n], c) and bool((far[:, n:n + 8] == 3).all())
+            del far, far_res
+    finally:
+        assert qe.qe_set_gemm_tile(qe.TILE_AUTO) == "OK"
+
+
 def test_random_codes_against_float64():
     """Ordinary values: FP32 sums of 128 products which the instruction aligns to their largest; the plain product's tests allow 1e-3 of the largest."""
     qe, d = need_lib(), dev()

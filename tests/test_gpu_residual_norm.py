@@ -286,6 +286,41 @@ def test_no_rows():
         assert bool((a == left).all()) and bool((b == left).all())
 
 
+@pytest.mark.parametrize("shape", [(300, 264), (20, 8200)], ids=ids)
+def test_rows_of_long_strides(shape):
+    """Rows so far apart that elements are past 2^31: the bits of the same calls on packed rows."""
+    qe, d = need_lib(), dev()
+    rows, cols = shape
+    ld = 2 ** 32 // rows + 7
+    g = torch.Generator(device=d)
+    g.manual_seed(4)
+    w, groups = torch.randn(cols, device=d, generator=g), -(-rows // 7)
+    gate = torch.randn((groups, cols), device=d, generator=g)
+    packed = [torch.randn(shape, device=d, generator=g).bfloat16() for _ in range(4)]  # x, y, dr, dh
+    got = []
+    for far in (False, True):
+        new = lambda: torch.empty((rows, ld), dtype=torch.bfloat16, device=d) if far else torch.empty(shape, dtype=torch.bfloat16, device=d)  # noqa: E731
+        ins = []
+        for t in packed:
+            ins.append(new())
+            ins[-1][:, :cols] = t
+        x, y, dr, dh = ins
+        r, h = new(), new()
+        f1, f2 = torch.zeros(rows, device=d), torch.zeros(rows, device=d)
+        sums = [torch.zeros(cols, device=d), torch.zeros(cols, device=d), torch.zeros((groups, cols), device=d)]
+        ws = torch.zeros(2 * cols * groups, device=d)
+        m = lambda t: qe.make_matrix(t, t.stride(0), qe.BF16)  # noqa: E731
+        desc = qe.make_residual(1.0, 0.5, True, w, EPS, True, w, EPS, qe.F32, 0.0, gate, qe.F32, cols, 7)
+        row, col = Blocks(qe, rows, cols, 0, 1, d), Blocks(qe, cols, rows, 0, 1, d)
+        assert qe.qe_residual_norm(m(x), m(y), rows, cols, desc, m(r), m(h), row.h, col.h, f1, f2) == "OK"
+        # in the place of dr and dh
+        assert qe.qe_residual_norm_grad(m(dr), m(dh), m(r), m(y), rows, cols, desc, f1, f2, m(dr), m(dh), *sums, qe.INIT, ws) == "OK"
+        torch.cuda.synchronize()
+        got.append([t[:, :cols].clone() for t in (r, h, dr, dh)] + [f1, f2, *sums, row.q, row.e, col.q, col.e])
+        del ins, x, y, dr, dh, r, h
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_gradients_repeat_their_bits_and_replay():
     """Captured with the forward and replayed on new inputs between eager calls: every replay gives the eager bits."""
     qe, d = need_lib(), dev()

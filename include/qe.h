@@ -456,7 +456,8 @@ qe_status qe_residual_norm(const qe_matrix *x_host, const qe_matrix *y_host, int
  * gates 2 * cols * ceil(rows / 16)), whose contents do not matter before or after and which
  * no other call may use at the same time.
  * dpre_weight without dh, dpost_weight without y or its norm, and dgate without y or a
- * gate are refused.  Sizes as above, and with or without a workspace what it holds below
+ * gate are refused, and so is one address for two of them (norms that share a weight: two
+ * gradients, to be added).  Sizes as above, and with or without a workspace what it holds below
  * 2^23 rows of cols floats (rows 0: INIT clears the weights' gradients).
  * Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
 qe_status qe_residual_norm_grad(const qe_matrix *dr_host, const qe_matrix *dh_host, const qe_matrix *r_host,

@@ -1274,7 +1274,7 @@ qe_status qe_residual_norm(const qe_matrix *x_host, const qe_matrix *y_host, int
   if (!d.pre_norm && (h_host != nullptr || row_host != nullptr || col_host != nullptr || pre_rstd != nullptr))
     return QE_ERR_INVALID_ARG;
   if (post_rstd != nullptr && (!d.post_norm || y_host == nullptr)) return QE_ERR_INVALID_ARG;
-  if (uintptr_t(post_rstd) % 4 || uintptr_t(pre_rstd) % 4) return QE_ERR_INVALID_ARG;
+  if (uintptr_t(post_rstd) % 4 || uintptr_t(pre_rstd) % 4 || (post_rstd != nullptr && post_rstd == pre_rstd)) return QE_ERR_INVALID_ARG;
   if ((row_host != nullptr && row_host->block_rows != 1) || (col_host != nullptr && col_host->block_rows != 1) ||
       (row_host != nullptr && col_host != nullptr && row_host->fmt != col_host->fmt))
     return QE_ERR_INVALID_ARG;
@@ -1349,6 +1349,9 @@ qe_status qe_residual_norm_grad(const qe_matrix *dr_host, const qe_matrix *dh_ho
   if (dgate != nullptr && (y_host == nullptr || d.gate == nullptr || ld_dgate < cols)) return QE_ERR_INVALID_ARG;
   if (uintptr_t(post_rstd) % 4 || uintptr_t(pre_rstd) % 4 || uintptr_t(dpost_weight) % 4 || uintptr_t(dpre_weight) % 4 ||
       uintptr_t(dgate) % 4 || uintptr_t(workspace) % 4)
+    return QE_ERR_INVALID_ARG;
+  // (different workgroups write them)
+  if ((dpost_weight != nullptr && (dpost_weight == dpre_weight || dpost_weight == dgate)) || (dgate != nullptr && dgate == dpre_weight))
     return QE_ERR_INVALID_ARG;
   const bool sums = dpost_weight != nullptr || dpre_weight != nullptr || dgate != nullptr;
   qe::ResidualGradParams p;

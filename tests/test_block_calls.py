@@ -78,7 +78,7 @@ BAD_DESC = [dict(post_eps=0.0), dict(pre_eps=-1.0), dict(post_eps=float("nan")),
 def test_norm_refuses():
     qe = need_lib()
 
-    def norm(rows=4, cols=40, x="", y="", d="", r="", h="", row="", col="", post=16, pre=16):
+    def norm(rows=4, cols=40, x="", y="", d="", r="", h="", row="", col="", post=16, pre=32):
         m = lambda v: matrix(qe) if v == "" else v  # noqa: E731
         return qe.qe_residual_norm(m(x), m(y), rows, cols, desc(qe) if d == "" else d, m(r),
                                    matrix(qe, data=32) if h == "" else h, blocked(qe) if row == "" else row, blocked(qe, 4) if col == "" else col, post, pre,
@@ -93,7 +93,7 @@ def test_norm_refuses():
     plain = desc(qe, post_norm=False, pre_norm=False)
     for bad in (dict(d=None), dict(x=None, y=None), dict(rows=-1), dict(cols=16385, x=matrix(qe, 16385)), dict(rows=1 << 31),
                 dict(d=plain), dict(d=plain, h=None, row=None, col=None, post=None), dict(y=None, post=16), dict(d=desc(qe, post_norm=False)),
-                dict(post=18), dict(pre=18), dict(pre=None), dict(r=None), dict(y=None, post=None, r=None, d=desc(qe, x_scale=0.5)),
+                dict(post=18), dict(pre=18), dict(post=32), dict(pre=None), dict(r=None), dict(y=None, post=None, r=None, d=desc(qe, x_scale=0.5)),
                 dict(y=None, post=None, r=None, h=matrix(qe)), dict(h=matrix(qe)), dict(h=matrix(qe), col=None, row=None),
                 dict(r=matrix(qe, data=48, ld=41), y=matrix(qe, data=48)), dict(r=matrix(qe, dtype=1)), dict(h=matrix(qe, data=48, dtype=1), y=matrix(qe, data=48)),
                 dict(col=blocked(qe, 4, fmt=1)), dict(col=blocked(qe, 4, block_rows=128)),
@@ -105,7 +105,7 @@ def test_norm_refuses():
 def test_norm_grad_refuses():
     qe = need_lib()
 
-    def grad(rows=4, cols=40, dr="", dh="", r="", y="", d="", post=16, pre=16, dx="", dy="", dpost=16, dpre=16, dgate=16, ld=40, mode=0, ws=16):
+    def grad(rows=4, cols=40, dr="", dh="", r="", y="", d="", post=16, pre=16, dx="", dy="", dpost=16, dpre=32, dgate=48, ld=40, mode=0, ws=16):
         m = lambda v, at: matrix(qe, data=at) if v == "" else v  # noqa: E731
         return qe.qe_residual_norm_grad(m(dr, 16), m(dh, 32), m(r, 48), m(y, 64), rows, cols, desc(qe) if d == "" else d, post, pre, m(dx, 80), m(dy, 96),
                                         dpost, dpre, dgate, mode, ws, ld, stream=0)
@@ -120,7 +120,7 @@ def test_norm_grad_refuses():
                 dict(ws=18), dict(dpost=18), dict(dpre=18), dict(dgate=18), dict(post=18), dict(pre=18), dict(rows=1 << 27),
                 dict(dx=matrix(qe, data=16, dtype=1)), dict(dx=matrix(qe, data=32, ld=41)), dict(dy=matrix(qe, data=16, ld=48)),
                 dict(dx=matrix(qe, data=48)), dict(dx=matrix(qe, data=64)), dict(dy=matrix(qe, data=48)), dict(dy=matrix(qe, data=64)),
-                dict(dx=matrix(qe, data=96))):
+                dict(dx=matrix(qe, data=96)), dict(dpost=32), dict(dpost=48), dict(dgate=32)):
         assert grad(**bad) == "INVALID_ARG", bad
 
 
@@ -135,11 +135,11 @@ def launches(qe, hip, cases):
         if kind == "cast":
             st = qe.qe_quantize_fp8_block(m, rows, cols, b(cols) if args.get("row", True) else None, b(rows) if args.get("col") else None, stream=0)
         elif kind == "norm":
-            st = qe.qe_residual_norm(m, m, rows, cols, d, m, None, b(cols), b(rows) if args.get("col") else None, ADDR, ADDR, stream=0)
+            st = qe.qe_residual_norm(m, m, rows, cols, d, m, None, b(cols), b(rows) if args.get("col") else None, ADDR, 2 * ADDR, stream=0)
         else:
             o, o2 = (qe.make_matrix(i * ADDR, max(cols, 1), qe.BF16) for i in (2, 3))
             st = qe.qe_residual_norm_grad(m, m, m, m, rows, cols, d, ADDR, ADDR, o, o2, ADDR if args.get("sums") else None,
-                                          ADDR if args.get("sums") else None, ADDR if args.get("gate") else None, qe.INIT, ADDR, stream=0)
+                                          2 * ADDR if args.get("sums") else None, 3 * ADDR if args.get("gate") else None, qe.INIT, ADDR, stream=0)
         assert st == "OK", st
         got.append([w[2].split("kernel")[0].lstrip("_ZN2qe1GLOBAL").lstrip("_0123456789") for w in hip.log("launch")])
     return got
@@ -173,7 +173,7 @@ def grids(qe, hip, cases):
             rows, cols, gate_rows = args
             ms = [qe.make_matrix(i * ADDR, cols, qe.BF16) for i in range(1, 7)]
             d = qe.make_residual(post_norm=True, post_weight=ADDR, pre_norm=True, pre_weight=ADDR, gate=ADDR, ld_gate=cols, gate_rows=gate_rows)
-            st = qe.qe_residual_norm_grad(*ms[:4], rows, cols, d, ADDR, ADDR, *ms[4:], ADDR, ADDR, ADDR, qe.INIT, ADDR, stream=0)
+            st = qe.qe_residual_norm_grad(*ms[:4], rows, cols, d, ADDR, ADDR, *ms[4:], ADDR, 2 * ADDR, 3 * ADDR, qe.INIT, ADDR, stream=0)
         assert st == "OK", st
         got.append([[w[2], int(w[3].split("=")[1])] for w in hip.log("launch")])
     return got

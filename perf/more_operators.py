@@ -255,7 +255,7 @@ def _decode(o):
 
 def _coded(codes, exps):
     """Codes and scales as the values they stand for."""
-    return {"codes": codes, "scales": exps.view(torch.float8_e8m0fnu)}
+    return {"codes": codes, "scales": exps.contiguous().view(torch.float8_e8m0fnu)}
 
 
 def _plain_cast(s):

@@ -839,6 +839,12 @@ bool epilogue_ok(const qe_epilogue &e, int64_t m, int64_t n, qe::ActGemmParams *
   return true;
 }
 
+// A residual in the output's place lies as the output does: one tile's stores would else
+// change what another has yet to read.  (Of one row no stride is used.)
+bool residual_in_place_ok(const qe::ActGemmParams &p) {
+  return p.residual == nullptr || p.residual != p.c || (p.residual_bf16 == p.c_bf16 && (p.ld_residual == p.ldc || p.m == 1));
+}
+
 // ------------------------------------------------------------------ blocks of 128
 constexpr int64_t kMaxRows = int64_t(1) << 31;
 constexpr int64_t kMaxGroups = int64_t(1) << 24;  // workgroups of 256 lanes: a launch has less than 2^32 lanes
@@ -1084,7 +1090,7 @@ qe_status qe_fp8_gemm_act(const uint8_t *a, qe_fp8_fmt fmt_a, int64_t lda, const
   p.c_bf16 = c_dtype == QE_BF16;
   p.fmt_a = fmt_a;
   p.fmt_b = fmt_b;
-  if (!act_gemm_ok(p)) return QE_ERR_INVALID_ARG;
+  if (!act_gemm_ok(p) || !residual_in_place_ok(p)) return QE_ERR_INVALID_ARG;
   return qe::launch_act_gemm(p, static_cast<hipStream_t>(stream)) == hipSuccess ? QE_OK : QE_ERR_HIP;
 }
 
@@ -1254,6 +1260,7 @@ qe_status qe_fp8_gemm_block(const qe_blocked *a_host, const qe_blocked *b_host, 
   p.c = c;
   p.ldc = ldc;
   p.c_bf16 = c_dtype == QE_BF16;
+  if (!residual_in_place_ok(p)) return QE_ERR_INVALID_ARG;
   p.fmt_a = a_host->fmt;
   p.fmt_b = b_host->fmt;
   p.a_exps = a_host->exps;

@@ -71,6 +71,8 @@ struct LdsScales {
 // 140).  The assembler adds no waits: s_nop 1 stands for what a vector instruction
 // that wrote an operand needs, products of the same accumulator are at least three
 // others apart in the loops, and settle() comes before anything else reads them.
+// Nothing here keeps the compiler from copying a sum in between: tests/test_mfma_waits.py
+// follows the built kernels' paths and finds an instruction that touches one too early.
 // BYTE: which byte of sa, sb is the K tile's.
 #define QE_MFMA_SCALED(SEL)                                                                                       \
   asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 " SEL " cbsz:%5 blgp:%6"       \

@@ -684,12 +684,14 @@ hipError_t launch_residual_grad(const ResidualGradParams &p, hipStream_t s) {
     const RowShape sh = row_shape(p.cols);
     if (sh.vectors > 2) return hipErrorInvalidValue;
     const bool bf16 = all_bf16({&p.dr, &p.dh, &p.r, &p.y, &p.dx, &p.dy});
-    // A unit holds one workgroup: as many chunks as units, of 16 rows at least where they
-    // leave sums, which the workspace's size allows for.
+    // A unit holds one workgroup: as many chunks as units, or a few less where groups share
+    // them (a chunk more than units is another round), of 16 rows at least where they leave
+    // sums, which the workspace's size allows for.  MI355X, us, BF16 8192 x 8192 in 3, 5 and 7
+    // groups, a chunk more / less: 263, 261, 264 / 178, 192, 182; 4096 x 8192 in 3: 142 / 99.
     const int64_t units = compute_units(), smallest = (p.gate_rows + kGradRows - 1) / kGradRows;
     const bool own_sums = p.sums != nullptr && sums_apart(p, smallest * p.groups);
     auto chunks_of = [&](int64_t least) {  // rows a chunk, and chunks a group
-      const int64_t most = (p.gate_rows + least - 1) / least, n = std::min(most, (units + p.groups - 1) / p.groups);
+      const int64_t most = (p.gate_rows + least - 1) / least, n = std::min(most, std::max<int64_t>(units / p.groups, 1));
       const int64_t rows = (p.gate_rows + n - 1) / n;
       return std::make_pair(rows, (p.gate_rows + rows - 1) / rows);
     };

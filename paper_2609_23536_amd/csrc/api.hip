@@ -1397,7 +1397,6 @@ qe_status qe_residual_norm_grad(const qe_matrix *dr_host, const qe_matrix *dh_ho
   p.dgate = dgate;
   p.ld_dgate = ld_dgate;
   p.post_norm = post;
-  p.pre_norm = d.pre_norm;
   p.weight_bf16 = d.weight_dtype == QE_BF16;
   p.gate_bf16 = d.gate_dtype == QE_BF16;
   p.offset = d.weight_offset;

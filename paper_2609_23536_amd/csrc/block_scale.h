@@ -116,7 +116,6 @@ __device__ __forceinline__ void store8(void *base, bool bf16, uint32_t at, int n
   }
 }
 
-// Eight codes of a row, n of which exist.
 // Codes that leave in whole lines of 128 bytes go past the caches, and what is read stays
 // there; codes that share lines do not.  MI355X, us, cached / past them: cast of BF16 4096 x
 // 4096 18.5 / 18.2, its input in the caches 12.6 / 9.4; 4096 x 14336 54.2 / 51.6; 8192 x
@@ -135,6 +134,7 @@ __device__ __forceinline__ void store_out(uint8_t *p, V v, bool past) {
   }
 }
 
+// Eight codes of a row, n of which exist.
 __device__ __forceinline__ void store_codes8(uint8_t *p, int n, uint32_t lo, uint32_t hi, bool past) {
   if (n >= 8) {
     store_out(p, u32x2_out{lo, hi}, past);

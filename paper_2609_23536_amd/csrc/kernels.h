@@ -272,9 +272,9 @@ struct ResidualGradParams {
   float *sums;
   float *dpost, *dpre, *dgate;
   int64_t ld_dgate;
-  int32_t post_norm, pre_norm, weight_bf16, gate_bf16;
+  int32_t post_norm, weight_bf16, gate_bf16, accumulate;
   float offset, x_scale, y_scale;
-  int32_t accumulate;
+  int32_t pad;
 };
 
 // An activation stored in, or restored from, an 8-bit checkpoint.

@@ -386,6 +386,7 @@ typedef struct {
  * for a = 0), code = x 2^e rounded to nearest even and byte = 127 - e: the largest
  * value's code is in (fmax / 2, fmax], none saturates.  A block that holds a NaN or an
  * infinity gets byte 255 and NaN codes.  A last block may be shorter than 128.
+ * Outputs may not overlap the input or each other.
  * Layout rules: ld >= the codes' columns, ld_exps >= ceil(columns / 128), any
  * alignment.  (The products below want more.)  rows, cols below 2^31, 128 x 128 blocks
  * below 2^24; rows or cols may be 0.
@@ -399,8 +400,9 @@ qe_status qe_quantize_fp8_block(const qe_matrix *in_host, int64_t rows, int64_t 
  * a_host: [m, k], b_host: [n, k].  F (Y = X W^T) and dI (dX = dY W) read a weight with
  * block_rows 128 (its codes, or its transposed codes), dW (dW = dY^T X) two operands
  * with block_rows 1; any combination is accepted.  The scales are applied in the matrix
- * instruction, exactly; the sums are otherwise as described for qe_fp8_gemm_act, and so
- * is epi_host (may be NULL).  With residual = c the product is accumulated in place, as
+ * instruction, exactly; the sums are otherwise those of qe_fp8_gemm_act, to the bit on
+ * one tile shape (off by 3.4e-5 of their size where one channel in a thousand is twenty
+ * times larger than the others), and epi_host (may be NULL) is as there.  With residual = c the product is accumulated in place, as
  * QE_PLACE_ACCUM does (a BF16 c is rounded by each call).
  * Layout rules: data 16-byte aligned, ld a multiple of 16, >= k rounded up to 16 and
  * below 2^23; exps 4-byte aligned, ld_exps a multiple of 4, >= ceil(k / 128) rounded up

@@ -372,8 +372,8 @@ __device__ __forceinline__ int b_row(int r) {
 // scalar row offset and one of the lane's (with one wave a SIMD the instructions are the
 // time).  The residual, of the output's type, is read in the order of the stores, 16 rows
 // ahead.  RES: there may be one, `has` says whether (two variants of FP32 spill).  MI355X,
-// us, block scales, by the general epilogue / so: BF16 6144 x 4096 x 2048 62.3 / 48.9, with a
-// residual 75.4 / 58.9; 4096 x 14336 x 4096 with one 261 / 214.
+// us, block scales, by the general epilogue / so: BF16 6144 x 4096 x 2048 57 / 50, with a
+// residual 78 / 59; 4096 x 14336 x 4096 210 / 191, with one 261 / 211.
 template <int TM, bool BF16, bool RES>
 __device__ __forceinline__ void store_sums(const ActGemmParams &g, const v4f (&acc)[TM / 16][8], uint8_t *ls, int lane, int64_t row0, int64_t col0,
                                            bool has) {

@@ -14,12 +14,16 @@
 //     dgate = S (o + w_post),   dw_post = sum over the gates' rows of S gate
 // so one sum of columns serves both.
 //
-// Both are bound by memory (MI355X, 8192 x 8192 BF16: 85 us to r and row-wise codes, 5.5
-// TB/s; the gradient 157, 5.1 TB/s), and next by their vector instructions.  A workgroup takes
-// one row after the other, each by a team of lanes that hold eight neighbouring values
-// (or twice eight) of it in registers from the loads to the stores; what a column's
-// weights and gates come to is kept in registers from row to row, and the next row is
-// loaded before this one's sums are taken.
+// Rows of more than 2048 columns are bound by memory (MI355X, 8192 x 8192 BF16: 86 us to r and
+// row-wise codes, 5.5 TB/s, 98 to r and h; FP32 199, 5.4 TB/s; an FP32 stream with a BF16
+// branch 151, 5.3 TB/s; the gradient 157, 5.1 TB/s, with its sums 167, FP32 323), and next by
+// their vector instructions; rows of sixteen values a lane less so (4096 x 16384 BF16 110 and
+// 221).  A workgroup takes one row after the other, each by a team of lanes that hold eight
+// neighbouring values (or twice eight) of it in registers from the loads to the stores.
+// With eight values a lane, what a column's weights and gates come to is kept from row to
+// row.  BF16 rows are loaded a row ahead, before this one's sums are taken (the gradient's
+// with eight values a lane only); others when they are used, or, in the gradient with eight
+// values a lane, when their row begins.
 #include "block_scale.h"
 
 #include <algorithm>
@@ -668,7 +672,12 @@ hipError_t launch_residual_norm(const ResidualParams &p, hipStream_t s) {
   const RowShape sh = row_shape(p.cols);
   if (sh.vectors > 2) return hipErrorInvalidValue;
   const bool bf16 = all_bf16({&p.x, &p.y, &p.r, &p.h});
-  // as many workgroups as the units hold at once (2048 lanes each), each with the rows it then has
+  // 2048 lanes a unit, and each workgroup the rows it then has.  A unit holds them all with
+  // eight values a lane and more than 2048 columns; half of them with sixteen (97 registers).
+  // Of shorter rows it holds four workgroups, by the 32 KB that `slots` has for any number of
+  // lanes, and the rest follow: MI355X, us, 16384 rows of BF16 with both norms, and the bytes
+  // at 6.28 TB/s: 128 columns 42 / 2.7, 512 45 / 10.7, 1024 47 / 21.4, 2048 53 / 42.7, 4096
+  // 101 / 85.5.
   const int64_t most = int64_t(compute_units()) * (2048 / sh.lanes);
   const dim3 grid{unsigned(std::min(p.rows, most))}, block{unsigned(sh.lanes)};
   const int lines = whole_lines(p.row) ? 1 : 0;

@@ -299,8 +299,7 @@ typedef struct {
  * products are off by 1e-7.  A code of an 8-bit checkpoint of Z is then a step off
  * the exact sum's for about one value in 2000.  epi_host == NULL: the sum alone.  c may be the
  * residual itself (refused if of another type or stride); it may not overlap it
- * otherwise.  Operands and layout rules as for
- * qe_fp8_gemm_tn, except that lda and ldb are below 2^23 and m, n below 2^31;
+ * otherwise.  Operands and layout rules as for qe_fp8_gemm_tn, except that lda and ldb are below 2^23 and m, n below 2^31;
  * operands of any total size run in one launch.  A row of c is one token: m may
  * be 1.  Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
 qe_status qe_fp8_gemm_act(const uint8_t *a, qe_fp8_fmt fmt_a, int64_t lda, const uint8_t *b, qe_fp8_fmt fmt_b, int64_t ldb,
@@ -402,8 +401,9 @@ qe_status qe_quantize_fp8_block(const qe_matrix *in_host, int64_t rows, int64_t 
  * with block_rows 1; any combination is accepted.  The scales are applied in the matrix
  * instruction, exactly; the sums are otherwise those of qe_fp8_gemm_act, to the bit on
  * one tile shape (off by 3.4e-5 of their size where one channel in a thousand is twenty
- * times larger than the others), and epi_host (may be NULL) is as there.  With residual = c the product is accumulated in place, as
- * QE_PLACE_ACCUM does (a BF16 c is rounded by each call).
+ * times larger than the others), and epi_host (may be NULL) is as there.  With
+ * residual = c the product is accumulated in place, as QE_PLACE_ACCUM does (a BF16 c is
+ * rounded by each call).
  * Layout rules: data 16-byte aligned, ld a multiple of 16, >= k rounded up to 16 and
  * below 2^23; exps 4-byte aligned, ld_exps a multiple of 4, >= ceil(k / 128) rounded up
  * to 4 and below 2^23 (the bytes past ceil(k / 128) are read and not used); ldc >= n; c

@@ -299,9 +299,9 @@ typedef struct {
  * products are off by 1e-7.  A code of an 8-bit checkpoint of Z is then a step off
  * the exact sum's for about one value in 2000.  epi_host == NULL: the sum alone.  c may be the
  * residual itself (refused if of another type or stride); it may not overlap it
- * otherwise.  Operands and layout rules as for qe_fp8_gemm_tn, except that lda and ldb are below 2^23 and m, n below 2^31;
- * operands of any total size run in one launch.  A row of c is one token: m may
- * be 1.  Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
+ * otherwise.  Operands and layout rules as for qe_fp8_gemm_tn, except that lda and
+ * ldb are below 2^23 and m, n below 2^31; operands of any total size run in one
+ * launch.  A row of c is one token: m may be 1.  Errors: QE_ERR_INVALID_ARG; QE_ERR_HIP. */
 qe_status qe_fp8_gemm_act(const uint8_t *a, qe_fp8_fmt fmt_a, int64_t lda, const uint8_t *b, qe_fp8_fmt fmt_b, int64_t ldb,
                           int64_t m, int64_t n, int64_t k, const float *a_scale_inv, const float *b_scale_inv,
                           const qe_epilogue *epi_host, void *c, qe_dtype c_dtype, int64_t ldc, qe_stream stream);
